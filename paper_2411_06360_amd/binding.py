@@ -144,6 +144,16 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     L.rsr_dense_table_bytes.restype = i64
     L.rsr_dense_destroy.argtypes = [vp]
     L.rsr_dense_destroy.restype = None
+    L.rsr_tree_attention_workspace.argtypes = [vp, vp, ci]
+    L.rsr_tree_attention_workspace.restype = i64
+    L.rsr_tree_attention.argtypes = [vp, vp, vp, i64, vp, vp, i64, vp, i64, ci, ci, ctypes.c_float, vp, i64, vp]
+    L.rsr_tree_attention.restype = ci
+    L.rsr_cache_slots.argtypes = [vp, vp, ci, vp, ci, ci, vp, vp, vp, vp, i64, vp, vp, vp]
+    L.rsr_cache_slots.restype = ci
+    L.rsr_cache_append.argtypes = [vp, vp, vp, i64, i64, ci, vp, vp, i64, vp]
+    L.rsr_cache_append.restype = ci
+    L.rsr_tree_masks.argtypes = [vp, vp, ci, ci, vp, vp, vp]
+    L.rsr_tree_masks.restype = ci
     _lib = L
     return L
 
@@ -295,6 +305,124 @@ def rsr_dense_table_bytes(handle: int) -> int:
 def rsr_dense_destroy(handle: Optional[int]) -> None:
     if handle:
         load().rsr_dense_destroy(handle)
+
+
+# ---- the paged cache and the attention over it (include/rsr_cache.h) ----
+RSR_F32, RSR_F16, RSR_BF16 = 0, 1, 2
+
+
+class RsrCache(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class RsrStep(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p), ("held", ctypes.c_void_p), ("start", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+        ("requests", ctypes.c_int32), ("tokens", ctypes.c_int32), ("max_new", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+    ]
+
+
+def _dtype(x) -> int:
+    name = str(x.dtype)
+    if name not in _DTYPES:
+        raise TypeError(f"float32, float16 or bfloat16 wanted, not {name}")
+    return _DTYPES[name]
+
+
+_DTYPES = {"torch.float32": RSR_F32, "torch.float16": RSR_F16, "torch.bfloat16": RSR_BF16}
+
+
+def _rows(x, like=None) -> int:
+    """Stride of a 2-D tensor of rows whose elements lie side by side."""
+    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+        raise ValueError("a 2-D tensor with contiguous rows is wanted")
+    if like is not None and (x.dtype != like.dtype or x.shape != like.shape or (x.stride(0) != like.stride(0) and x.shape[0] > 1)):
+        raise ValueError("keys and values must have the same type, shape and stride")
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1])
+
+
+def _whole(x, dtypes, count=None):
+    """A contiguous tensor of one of the given types, with at least `count` elements."""
+    if str(x.dtype) not in dtypes or not x.is_contiguous() or (count is not None and x.numel() < count):
+        raise ValueError(f"a contiguous tensor of {dtypes[0]}" + (f" with {count} elements" if count is not None else "") + " is wanted")
+    return x
+
+
+_I32, _U64 = ("torch.int32",), ("torch.uint64", "torch.int64")
+
+
+def make_cache(k, v) -> RsrCache:
+    """rsr_cache_t of device tensors ``[pages][kv_heads][page_size][head_dim]`` (any strides between rows; keep the tensors alive)."""
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(3) != 1:
+        raise ValueError("two 4-D tensors of the same type, shape and strides, with contiguous rows, are wanted")
+    pages, kv_heads, page_size, head_dim = k.shape
+    return RsrCache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), _dtype(k), pages, page_size, kv_heads, head_dim, 0)
+
+
+def make_step(table, held, start, tokens: int, max_new: int, mask=None) -> RsrStep:
+    """rsr_step_t of device tensors: ``table [requests][max_pages]``, ``held [requests]``, ``start [requests+1]`` (int32) and
+    ``mask [tokens]`` (64 bits) or None.  Keep the tensors alive; what they hold may change between calls."""
+    requests = held.numel()
+    _whole(table, _I32), _whole(held, _I32), _whole(start, _I32, requests + 1)
+    if table.dim() != 2 or table.shape[0] != requests:
+        raise ValueError("the table has a row for each request")
+    if mask is not None:
+        _whole(mask, _U64, tokens)
+    return RsrStep(table.data_ptr(), held.data_ptr(), start.data_ptr(), _addr(mask), requests, int(tokens), int(max_new), table.shape[1])
+
+
+def rsr_tree_attention_workspace(cache: RsrCache, step: RsrStep, heads: int) -> int:
+    """Bytes of workspace that rsr_tree_attention takes (zero it once)."""
+    n = load().rsr_tree_attention_workspace(ctypes.addressof(cache), ctypes.addressof(step), int(heads))
+    if n < 0:
+        raise RsrError(n, rsr_last_error())
+    return n
+
+
+def rsr_tree_attention(cache: RsrCache, step: RsrStep, q, k, v, out, heads: int, scale: float, workspace, stream=None) -> None:
+    """``q``, ``out``: device ``[tokens][heads * head_dim]``; ``k``, ``v``: ``[tokens][kv_heads * head_dim]`` (slices of wider rows
+    will do), all float32 or of the cache's type; ``workspace``: device bytes that were zero at first."""
+    width, kv_width = heads * cache.head_dim, cache.kv_heads * cache.head_dim
+    if q.shape != (step.tokens, width) or out.shape != q.shape or out.dtype != q.dtype or k.shape != (step.tokens, kv_width) or k.dtype != q.dtype:
+        raise ValueError("q and out are [tokens][heads * head_dim], k and v [tokens][kv_heads * head_dim], all of one type")
+    _check(load().rsr_tree_attention(ctypes.addressof(cache), ctypes.addressof(step), q.data_ptr(), _rows(q), k.data_ptr(), v.data_ptr(), _rows(k, v),
+                                     out.data_ptr(), _rows(out), _dtype(q), heads, scale, workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _addr(stream)))
+
+
+def rsr_cache_slots(held, add, table, page_size: int, free_pages, free_count, slots, start, now, free_left, stream=None) -> None:
+    """Pages and slots for the next ``add[r]`` tokens of every request; all device int32, see the header."""
+    requests = held.numel()
+    for x, count in ((held, None), (add, requests), (table, None), (free_pages, None), (free_count, 1), (slots, None), (start, requests + 1), (now, requests), (free_left, 1)):
+        _whole(x, _I32, count)
+    if table.dim() != 2 or table.shape[0] != requests:
+        raise ValueError("the table has a row for each request")
+    _check(load().rsr_cache_slots(held.data_ptr(), add.data_ptr(), requests, table.data_ptr(), table.shape[1], int(page_size), free_pages.data_ptr(),
+                                  free_count.data_ptr(), free_left.data_ptr(), slots.data_ptr(), slots.numel(), start.data_ptr(), now.data_ptr(),
+                                  _addr(stream)))
+
+
+def rsr_cache_append(cache: RsrCache, k, v, slots, rows=None, stream=None) -> None:
+    """Row ``rows[i]`` (None: row ``i``) of ``k`` and ``v`` (``[nrows][kv_heads * head_dim]``) goes to ``slots[i]``."""
+    if k.dim() != 2 or k.shape[1] != cache.kv_heads * cache.head_dim:
+        raise ValueError("k and v are [rows][kv_heads * head_dim]")
+    _whole(slots, _I32)
+    if rows is not None:
+        _whole(rows, _I32, slots.numel())
+    _check(load().rsr_cache_append(ctypes.addressof(cache), k.data_ptr(), v.data_ptr(), _rows(k, v), k.shape[0], _dtype(k), _addr(rows),
+                                   slots.data_ptr(), slots.numel(), _addr(stream)))
+
+
+def rsr_tree_masks(parent, start, mask, depth, stream=None) -> None:
+    """``mask`` (64 bits) and ``depth`` (int32) of the drafted tokens from their ``parent`` (int32, -1: hangs on the cache)."""
+    tokens, requests = parent.numel(), start.numel() - 1
+    _whole(parent, _I32), _whole(start, _I32), _whole(mask, _U64, tokens), _whole(depth, _I32, tokens)
+    _check(load().rsr_tree_masks(parent.data_ptr(), start.data_ptr(), requests, tokens, mask.data_ptr(), depth.data_ptr(), _addr(stream)))
 
 
 class RsrJob(ctypes.Structure):

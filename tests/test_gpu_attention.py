@@ -1,0 +1,333 @@
+"""rsr_tree_attention (include/rsr_cache.h) against the definition in float64."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_06360_amd as R
+from tests.cache_util import DTYPES, Step, plain
+
+pytestmark = pytest.mark.gpu
+KINDS = [("f32", "bf16"), ("f32", "f16"), ("bf16", "bf16"), ("f16", "f16")]
+
+
+def say(*what):
+    print(*what, flush=True)
+
+
+@pytest.mark.parametrize("act,cache", KINDS)
+@pytest.mark.parametrize("dim", [8, 40, 64, 80, 96, 128, 136, 192, 256])
+def test_head_dims_and_types(act, cache, dim):
+    say("dims", act, cache, dim)
+    Step([77, 0, 300], [5, 3, 16], dim=dim, act=act, cache=cache, seed=1).check()
+
+
+@pytest.mark.parametrize("act,cache", KINDS)
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (5, 5), (8, 1), (12, 3), (64, 1)])
+def test_head_layouts(act, cache, heads, kv_heads):
+    say("heads", act, cache, heads, kv_heads)
+    Step([130, 31], [7, 1], heads=heads, kv_heads=kv_heads, act=act, cache=cache, seed=2).check()
+
+
+@pytest.mark.parametrize("held", [0, 1, 7, 8, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257, 511, 1023, 1025, 4097])
+def test_cached_lengths_around_every_edge(held):
+    say("held", held)
+    for act, cache in (("f32", "f16"), ("bf16", "bf16")):
+        Step([held], [1], act=act, cache=cache, seed=3).check()
+        Step([held], [16], act=act, cache=cache, heads=2, kv_heads=2, dim=128, seed=4).check()
+
+
+@pytest.mark.parametrize("new", [1, 2, 15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 64])
+@pytest.mark.parametrize("group", [1, 3, 4])
+def test_numbers_of_drafted_tokens(new, group):
+    say("new", new, group)
+    for act, cache in (("f32", "bf16"), ("f16", "f16")):
+        Step([70], [new], heads=2 * group, kv_heads=2, act=act, cache=cache, seed=5).check()
+
+
+@pytest.mark.parametrize("new", [1, 33, 64, 65, 200, 333])
+@pytest.mark.parametrize("held", [0, 50, 256])
+def test_chains(new, held):
+    say("chain", new, held)
+    for act, cache in (("f32", "bf16"), ("bf16", "bf16"), ("f32", "f16")):
+        Step([held, 3], [new, 2], act=act, cache=cache, tree=False, heads=2, kv_heads=1, seed=6).check()
+
+
+@pytest.mark.parametrize("page", [8, 16, 32, 64, 128, 256, 1024])
+def test_page_sizes(page):
+    say("page", page)
+    Step([1, 2 * page, 2 * page + 5, 3 * page - 1], [2, 1, 3, 4], page=page, seed=7).check()
+
+
+def test_ragged_batches():
+    rng = np.random.default_rng(8)
+    for act, cache in KINDS:
+        held = [int(x) for x in rng.integers(0, 900, 40)]
+        new = [int(x) for x in rng.integers(0, 12, 40)]
+        held[3], held[17], new[5], new[20], new[39] = 0, 4000, 0, 64, 0
+        say("ragged", act, cache, held, new)
+        Step(held, new, act=act, cache=cache, heads=4, kv_heads=2, seed=8).check()
+
+
+@pytest.mark.parametrize("requests", [255, 256, 257, 600, 1500])
+def test_many_requests(requests):
+    rng = np.random.default_rng(requests)
+    held, new = [int(x) for x in rng.integers(0, 40, requests)], [int(x) for x in rng.integers(0, 4, requests)]
+    say("requests", requests)
+    Step(held, new, heads=1, kv_heads=1, dim=32, act="f16", cache="f16", page=8, seed=9).check()
+
+
+def test_a_long_cache_is_split_and_joined():
+    for act, cache in (("f32", "f16"), ("bf16", "bf16")):
+        say("long", act, cache)
+        Step([70001], [3], heads=2, kv_heads=1, act=act, cache=cache, page=64, seed=10).check()
+        Step([30011, 5, 20000], [17, 2, 33], heads=1, kv_heads=1, dim=128, act=act, cache=cache, page=16, seed=11).check()
+
+
+def test_tokens_that_see_nothing_get_zeros():
+    say("empty rows")
+    s = Step([0, 40, 0], [4, 4, 1], seed=12)
+    s.mask[1] = 0
+    s.mask[3] = 0
+    s.mask[8] = 0
+    got = s.check()
+    assert (got[[1, 3, 8]] == 0).all() and (got[0] != 0).any()
+
+
+def test_bits_of_tokens_that_are_not_there_mean_nothing():
+    say("loose bits")
+    s = Step([20, 0], [5, 3], seed=13)
+    want = s.check().copy()
+    s.mask[:5] |= ~((1 << 5) - 1)
+    s.mask[5:] |= ~((1 << 3) - 1)
+    assert np.array_equal(s.run(), want)
+
+
+@pytest.mark.parametrize("act,cache", KINDS)
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), -float("inf"), "lowest"])
+def test_what_is_not_seen_is_not_touched(act, cache, junk):
+    """Junk in everything that no row sees: places behind the last cached token, pages that no table names, pages that were
+    given up; and in drafted tokens that some rows see and others do not."""
+    say("unseen", act, cache, junk)
+    s = Step([37, 90, 0], [6, 9, 3], act=act, cache=cache, heads=4, kv_heads=2, dim=128, seed=14)
+    s.table[1, 2] = -1
+    s.table[1, 4] = 10**6
+    named = torch.zeros(s.cache_k.shape[0] * s.page, dtype=torch.bool)
+    for r, held in enumerate(s.held.tolist()):
+        for t in range(held):
+            page = int(s.table[r, t // s.page])
+            if 0 <= page < s.cache_k.shape[0]:
+                named[page * s.page + t % s.page] = True
+    want = s.check().copy()
+    for x in (s.cache_k, s.cache_v):
+        value = torch.finfo(x.dtype).min if junk == "lowest" else junk
+        flat = x.transpose(1, 2).reshape(-1, s.kv_heads, s.dim)
+        flat[~named.cuda()] = value
+        x.copy_(flat.view(-1, s.page, s.kv_heads, s.dim).transpose(1, 2))
+    assert np.array_equal(s.run(), want)
+    token = 2  # of the first request
+    s.k[token], s.v[token] = (torch.finfo(s.k.dtype).min if junk == "lowest" else junk,) * 2
+    got = s.run()
+    sees = np.zeros(s.tokens, bool)
+    sees[:6] = [bool(int(m) >> token & 1) for m in s.mask[:6].tolist()]
+    assert sees.any() and not sees[:6].all()
+    assert np.array_equal(got[~sees], want[~sees])
+    if junk != "lowest":
+        assert not np.isfinite(got[sees]).all()
+
+
+def test_infinite_values_of_seen_tokens_arrive():
+    """An infinite value of a seen token is what the mean becomes; the rows that do not see it keep their own."""
+    for act, cache in KINDS:
+        say("infinite value", act, cache)
+        s = Step([20], [8], act=act, cache=cache, heads=2, kv_heads=2, dim=64, seed=15)
+        want = s.check().copy()
+        s.v[3, 5] = float("inf")
+        s.v[3, 9] = -float("inf")
+        got = s.run()
+        sees = np.array([bool(int(m) >> 3 & 1) for m in s.mask.tolist()])
+        assert (got[sees][:, 5] == np.inf).all() and (got[sees][:, 9] == -np.inf).all()
+        got[:, [5, 9]] = want[:, [5, 9]]
+        assert np.array_equal(got, want)
+
+
+def test_steep_and_flat_scores():
+    for act, cache in KINDS:
+        for scale in (0.0, 1e-3, 3.0, -2.0):
+            say("scale", act, cache, scale)
+            s = Step([500, 65], [4, 9], act=act, cache=cache, dim=128, seed=16)
+            s.scale = scale
+            s.check()
+
+
+def test_large_and_small_queries():
+    """Float queries far outside the range of the cache's type are products like others."""
+    for cache in ("f16", "bf16"):
+        for size in (1e6, 1e-6, 1e-30, 1e30):
+            say("queries", cache, size)
+            s = Step([100], [5], cache=cache, seed=17)
+            s.q *= size
+            s.scale /= size
+            s.check()
+
+
+def test_strides_and_orders_of_the_cache():
+    """Pages of [page_size][kv_heads][dim], keys and values side by side, pages far apart: wherever the strides say."""
+    for act, cache in (("f32", "bf16"), ("f16", "f16")):
+        say("strides", act, cache)
+        s = Step([100, 33], [5, 2], act=act, cache=cache, dim=80, seed=18)
+        want = s.check().copy()
+        pages, kv, page, dim = s.cache_k.shape
+        both = torch.full((pages + 1, page, kv, 2, dim + 16), float("nan"), dtype=s.cache_k.dtype, device="cuda")
+        both[:pages, :, :, 0, 8:8 + dim] = s.cache_k.transpose(1, 2)
+        both[:pages, :, :, 1, 8:8 + dim] = s.cache_v.transpose(1, 2)
+        s.cache_k, s.cache_v = (both[:pages, :, :, i, 8:8 + dim].transpose(1, 2) for i in range(2))
+        assert np.array_equal(s.run(), want)
+
+
+def test_offsets_beyond_32_bits():
+    """Elements beyond 2^32 of the cache: pages that lie 2^26 elements apart."""
+    say("far pages")
+    s = Step([16 * 70], [3], heads=2, kv_heads=1, dim=128, cache="f16", act="f16", seed=19)
+    want = s.check().copy()
+    pages, kv, page, dim = s.cache_k.shape
+    gap = 1 << 26
+    for name in ("cache_k", "cache_v"):
+        far = torch.empty(pages * gap, dtype=torch.float16, device="cuda").as_strided((pages, kv, page, dim), (gap, page * dim, dim, 1))
+        far.copy_(getattr(s, name))
+        setattr(s, name, far)
+    assert pages * gap > 2**32
+    assert np.array_equal(s.run(), want)
+
+
+def test_rows_of_no_request_are_left_alone():
+    say("gaps")
+    s = Step([40, 10, 5], [4, 6, 3], seed=20)
+    s.start[0] = 2      # rows 0 and 1 belong to none
+    s.start[3] = 11     # nor do the last two
+    s.check()
+    s = Step([40, 10, 5], [4, 6, 3], seed=20)
+    s.max_new = 4       # what goes beyond is left out
+    s.check()
+
+
+def test_lengths_out_of_range_are_clamped():
+    say("lengths")
+    s = Step([40, 10, 5], [4, 6, 3], seed=21)
+    s.held[0], s.held[1] = 10**9, -5
+    s.check()
+    s.start[1], s.start[3] = -7, 10**9
+    s.out.fill_(float("nan"))
+    s.check()
+
+
+def test_results_are_reproducible_and_do_not_depend_on_the_batch():
+    for act, cache in KINDS:
+        say("again", act, cache)
+        s = Step([3000, 70, 0], [9, 5, 2], act=act, cache=cache, heads=4, kv_heads=2, dim=128, seed=22)
+        first = s.run().copy()
+        for _ in range(3):
+            s.out.fill_(float("nan"))
+            assert np.array_equal(s.run(), first)
+
+
+def test_a_tree_equals_its_paths_decoded_one_by_one():
+    """Verification is what decoding would have done: the kept path of a tree, appended token by token, gives the same
+    results within the rounding of a different order of additions."""
+    say("tree against path")
+    s = Step([45], [12], act="f32", cache="bf16", heads=4, kv_heads=2, dim=128, seed=23, spare=2)
+    s.table[0, 3:5] = torch.tensor([s.cache_k.shape[0] - 2, s.cache_k.shape[0] - 1])
+    used = set(s.table[0, :3].tolist())
+    free = [p for p in range(s.cache_k.shape[0]) if p not in used]
+    s.table[0, 3:5] = torch.tensor(free[:2], dtype=torch.int32)
+    tree = s.check().copy()
+    leaf = max(range(12), key=lambda i: bin(int(s.mask[i])).count("1"))
+    path = [j for j in range(12) if int(s.mask[leaf]) >> j & 1]
+    cache = R.make_cache(s.cache_k, s.cache_v)
+    for depth, token in enumerate(path):
+        one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+        out = torch.empty((1, s.heads * s.dim), device="cuda")
+        held = torch.tensor([45 + depth], dtype=torch.int32, device="cuda")
+        step = R.make_step(s.table, held, one, 1, 1)
+        space = torch.zeros(R.rsr_tree_attention_workspace(cache, step, s.heads), dtype=torch.uint8, device="cuda")
+        row = slice(token, token + 1)
+        R.rsr_tree_attention(cache, step, s.q[row], s.k[row], s.v[row], out, s.heads, s.scale, space, torch.cuda.current_stream().cuda_stream)
+        at = 45 + depth
+        slot = int(s.table[0, at // 16]) * 16 + at % 16
+        R.rsr_cache_append(cache, s.k, s.v, torch.tensor([slot], dtype=torch.int32, device="cuda"), torch.tensor([token], dtype=torch.int32, device="cuda"),
+                           torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert np.abs(plain(out)[0] - tree[token]).max() <= 1e-5
+
+
+def test_another_stream_and_a_graph():
+    """The call on a stream of its own, and replayed from a graph with new contents in the same buffers."""
+    s = Step([2000, 17], [6, 3], act="f32", cache="f16", heads=4, kv_heads=2, dim=128, seed=24)
+    want = s.check().copy()
+    side = torch.cuda.Stream()
+    s.out.fill_(float("nan"))
+    side.wait_stream(torch.cuda.current_stream())
+    s.call(side.cuda_stream)
+    side.synchronize()
+    assert np.array_equal(plain(s.out), want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.call()
+    for turn in range(3):
+        say("replay", turn)
+        s.held.copy_(torch.tensor([2000 - 700 * turn, 17 + turn % 2], dtype=torch.int32))
+        s.q.mul_(0.9)
+        s.out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = plain(s.out).copy()
+        assert np.array_equal(replayed, s.run())
+        s.check()
+
+
+def refused(s, code=-1, **changes):
+    for name, value in changes.items():
+        setattr(s, name, value)
+    with pytest.raises(R.RsrError) as e:
+        s.call()
+    assert e.value.code == code and e.value.message
+
+
+def test_refusals_leave_the_output_alone():
+    def fresh():
+        return Step([40], [4], dim=64, act="f16", cache="f16", seed=25)
+
+    refused(fresh(), scale=float("inf"))
+    refused(fresh(), scale=float("nan"))
+    s = fresh()
+    refused(s, max_new=65)
+    s = fresh()
+    refused(s, workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))
+    s = fresh()
+    rows = torch.zeros((s.tokens, 8 * 64 + 4), dtype=torch.float16, device="cuda")
+    refused(s, q=rows[:, 4:4 + 256])                      # not 16-byte aligned
+    s = fresh()
+    refused(s, q=torch.zeros((4, 260), dtype=torch.float16, device="cuda")[:, :256])  # rows 520 bytes apart
+    s = fresh()
+    refused(s, q=s.q.bfloat16(), k=s.k.bfloat16(), v=s.v.bfloat16(), out=s.out.bfloat16())  # not the cache's type
+    s = fresh()
+    refused(s, heads=64 * 2 + 2, q=torch.zeros((4, 130 * 64), dtype=torch.float16, device="cuda"), out=torch.zeros((4, 130 * 64), dtype=torch.float16, device="cuda"))
+    s = fresh()
+    s.cache_k, s.cache_v = (torch.zeros((5, 2, 24, 64), dtype=torch.float16, device="cuda") for _ in range(2))
+    refused(s)                                            # pages of 24
+    s = fresh()
+    s.cache_k, s.cache_v = (torch.zeros((5, 2, 16, 68), dtype=torch.float16, device="cuda")[..., :64] for _ in range(2))
+    refused(s)                                            # rows of the cache not 16-byte aligned
+    s.run = None
+    assert torch.isnan(s.out).all()
+
+
+def test_nothing_to_do():
+    s = Step([], [], seed=26)
+    s.call()
+    s = Step([5, 6], [0, 0], seed=27)
+    s.call()
+    torch.cuda.synchronize()
+
+
+def test_all_types_are_covered():
+    assert {a for a, _ in KINDS} == set(DTYPES)
