@@ -40,7 +40,7 @@ enum { RSR_F32 = 0, RSR_F16 = 1, RSR_BF16 = 2 };
  *
  *   k, v        DEVICE, 16-byte aligned; owned by the caller.  Element (page, head, offset, d) is at
  *               page * page_stride + head * head_stride + offset * token_stride + d (in elements), in both.
- *               Strides are multiples of 8.  Pages of [kv_heads][page_size][head_dim] are read fastest.
+ *               Strides are multiples of 8, page_stride below 2^31 and token_stride below 2^24.  Pages of [kv_heads][page_size][head_dim] are read fastest.
  *   dtype       RSR_F16 or RSR_BF16
  *   pages       >= 1, pages * page_size < 2^31
  *   page_size   a power of two, 8 .. 1024

@@ -1,18 +1,23 @@
 // Attention of a step's new tokens over the paged cache and over each other (include/rsr_cache.h).
 //
 // The scores of 16 query rows (a row: one new token, one query head) and 32 positions are S^T = K Q^T on the matrix cores, the
-// result is O^T += V^T P^T with P = 2^(S - m), and a running maximum m and sum l per row (one pass over the cache).
+// result is O^T += V^T P^T with P = 2^(S - m), and a running maximum m and sum l per row: one pass over the cache.
 // Transposed, because the positions of a score tile then lie along a lane's registers: what S^T leaves in a lane, eight
-// consecutive positions of one row, is the operand that V^T P^T wants there.  Keys and values go from the cache straight into
-// registers (a wavefront reads whole rows of 16 or 32 tokens, no two wavefronts read the same), values change their two halves
-// of dwords with v_perm_b32; LDS serves to join the four wavefronts of a workgroup at the end.
+// consecutive positions of one row, is the operand that V^T P^T wants there, and P never leaves its registers.  l is one more
+// row of the result, with ones for values.
 //
 // Position order.  Lane (n, g) = (lane & 15, lane >> 4) holds of S^T the rows 4g .. 4g+3 of two tiles of 16 keys.  With key
 // 8 (x >> 2) + (x & 3) in row x of the first tile and that plus 4 in the second, these are the positions 8g .. 8g+7.
+// Values: the lane reads eight dimensions of each of these positions (whole rows side by side) and has, after exchanging halves
+// of dwords with v_perm_b32, eight positions of each dimension, the other operand.
 //
-// Work split.  The positions of a request (tiles of 32: first the cached ones, then the new ones) are cut into as many pieces
-// as keep the chip busy; a workgroup takes a piece for the rows of one key head, its wavefronts a quarter of the piece each.
-// The pieces of a row meet in the workspace, where the workgroup that comes last joins them in their order.
+// Two kernels, by the rows that a key head has (new tokens times query heads of the group):
+//   attend_split  up to 16: the four wavefronts of a workgroup take the same rows and different positions, keys and values go
+//                 from the cache straight into registers, LDS serves to join the wavefronts at the end
+//   attend_shared more: the wavefronts take different rows and the same positions, which come through LDS
+// The positions of a request (tiles of 32: first the cached ones, then the new ones) are cut into as many pieces as keep the chip
+// busy, a workgroup per piece.  The pieces of a row meet in the workspace, where the workgroup that comes last joins them in
+// their order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -28,9 +33,9 @@ using rsr_internal::set_error;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kTile = 32;        // positions of a tile
-constexpr int kLeastTiles = 4;   // of a piece: one for each wavefront
+constexpr int kLeastTiles = 4;   // of a piece
 constexpr float kBias = 7.f;     // weights are 2^(s - m + 7): as float16 they keep their bits down to 2^-21 of the largest
-constexpr float kSlack = 8.f;    // m follows the maximum when it is left behind by more: weights stay below 2^15
+constexpr float kLimit = 15.f;   // m follows the maximum when a weight would pass 2^15, so that it seldom does
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
@@ -44,8 +49,11 @@ struct Args {
   const uint64_t* mask;
   uint32_t* counters;
   float* partial;
-  int64_t q_stride, kv_stride, out_stride, page_stride, head_stride, token_stride;
-  int32_t requests, tokens, max_new, max_pages, log2_page, pages, kv_heads, dim, group, target;
+  int64_t q_stride, kv_stride, out_stride, head_stride;
+  uint32_t page_stride, token_stride;
+  int32_t requests, tokens, max_new, max_pages, log2_page, pages, kv_heads, dim, group;
+  uint32_t group_inverse;  // ceil(2^32 / group), 0 for 1
+  double per_target;       // 1 / pieces that are aimed at
   float scale;
 };
 
@@ -55,6 +63,7 @@ template <> struct Half<_Float16> {
   typedef _Float16 v8 __attribute__((ext_vector_type(8)));
   typedef _Float16 v2 __attribute__((ext_vector_type(2)));
   static constexpr int kTerms = 2;  // of a float: 22 bits
+  static constexpr uint32_t kExponent = 0x7c00, kOnes = 0x3c003c00;
   static __device__ f4 mfma(u4 a, u4 b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
@@ -63,10 +72,15 @@ template <> struct Half<__bf16> {
   typedef __bf16 v8 __attribute__((ext_vector_type(8)));
   typedef __bf16 v2 __attribute__((ext_vector_type(2)));
   static constexpr int kTerms = 3;  // of a float: all 24 bits
+  static constexpr uint32_t kExponent = 0x7f80, kOnes = 0x3f803f80;
   static __device__ f4 mfma(u4 a, u4 b, f4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
   }
 };
+
+template <typename CT> __device__ inline uint32_t pair_of(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, typename Half<CT>::v2{(CT)lo, (CT)hi});
+}
 
 // Eight floats as the sum of TERMS operands, each the rounding of what the ones before leave.
 template <typename CT, int TERMS> __device__ inline void split(const float (&x)[8], u4 (&t)[TERMS]) {
@@ -83,17 +97,47 @@ template <typename CT, int TERMS> __device__ inline void split(const float (&x)[
     }
 }
 
-// The largest / the sum over the four lanes n, n + 16, n + 32, n + 48.
+// Eight activations in the cache's type, from eight in memory.
+template <typename CT, bool FLOAT> struct Eight {
+  u4 raw[FLOAT ? 2 : 1];
+  __device__ void load(const void* p, int64_t at) {
+    const u4* from = reinterpret_cast<const u4*>(static_cast<const char*>(p) + at * (FLOAT ? 4 : 2));
+    raw[0] = from[0];
+    if constexpr (FLOAT) raw[1] = from[1];
+  }
+  __device__ u4 rounded() const {
+    if constexpr (!FLOAT) return raw[0];
+    else {
+      const f4 lo = __builtin_bit_cast(f4, raw[0]), hi = __builtin_bit_cast(f4, raw[1]);
+      return u4{pair_of<CT>(lo[0], lo[1]), pair_of<CT>(lo[2], lo[3]), pair_of<CT>(hi[0], hi[1]), pair_of<CT>(hi[2], hi[3])};
+    }
+  }
+};
+
+// x, of which the compiler knows nothing more: what follows from a lane's number is then worked out where it is used and does not
+// fill registers through the loops before.
+__device__ inline int hidden(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The largest over the four lanes n, n + 16, n + 32, n + 48.
 __device__ inline float over_groups_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
 }
-__device__ inline float over_groups_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+
+__device__ inline float max3(float x, float y, float z) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+  return r;
 }
 
+__device__ inline int eight_bits(int count) { return (1 << max(min(count, 8), 0)) - 1; }  // the lowest `count`
+
 // ---- which piece of work ------------------------------------------------------------------------------------
+__device__ inline int tiles_of(int n) { return (n + kTile - 1) / kTile; }
+
 struct Request {
   int64_t first;  // row of its first new token
   int32_t fresh;  // new tokens
@@ -104,263 +148,435 @@ __device__ inline Request request_of(const Args& a, int r) {
   const int64_t first = a.start[r], end = min((int64_t)a.start[r + 1], (int64_t)a.tokens);
   const int64_t fresh = first < 0 ? 0 : max(min(end - first, (int64_t)a.max_new), (int64_t)0);
   const int64_t held = min((int64_t)max(a.held[r], 0), (int64_t)a.max_pages << a.log2_page);
-  return {first, (int32_t)fresh, (int32_t)min(held, (int64_t)INT32_MAX - 1024)};
+  return {first, (int32_t)fresh, (int32_t)min(held, (int64_t)INT32_MAX - 65536 - 1024)};
 }
 
-__device__ inline int tiles_of(int n) { return (n + kTile - 1) / kTile; }
+template <typename T> __device__ inline T from_lane(T x, int lane) {
+  if constexpr (sizeof(T) == 8) {
+    const uint64_t v = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
+    return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+  } else {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+  }
+}
 
-struct Counts {
-  int64_t units;           // pieces
-  int32_t slots, groups;   // pieces of rows that are cut, and such sets of rows
+struct Unit {
+  Request q;
+  int32_t r, head, row0, rows;  // request, key head, first row and rows
+  int32_t piece, pieces;
+  int32_t slot, set;            // of the piece in the workspace; of its rows among those that are cut
+  int32_t tile0, tile1, cached; // its tiles; tiles of cached tokens (those behind hold new ones)
 };
 
-// Pieces of a request when a piece is `most` tiles at most.
-__device__ inline Counts counts_of(const Request& q, int rows_per_unit, int group, int kv_heads, int64_t most, int* blocks, int* pieces) {
-  *blocks = (int)(((int64_t)q.fresh * group + rows_per_unit - 1) / rows_per_unit);
-  const int64_t tiles = tiles_of(q.held) + tiles_of(q.fresh);
-  *pieces = (int)((tiles + most - 1) / most);
-  const int64_t sets = (int64_t)*blocks * kv_heads;
-  if (*pieces < 2) return {sets * *pieces, 0, 0};
-  return {sets * *pieces, (int32_t)(sets * *pieces), (int32_t)sets};
-}
+// Every wavefront counts the pieces of all requests by itself, a run of requests per lane, without a barrier.
+template <int ROWS> struct Plan {
+  int64_t end, units;  // pieces up to the lane's last request; of all
+  uint64_t cut;        // before the lane's first request: pieces of rows that are cut << 32 | sets of such rows
+  Request q;           // the lane's first request
+  int32_t run, most;   // requests per lane, tiles of a piece
 
-template <int DP> constexpr int stride_of_partial() { return DP + 4; }
-
-template <typename CT, bool FLOAT, int DP, int MT>
-__global__ void __launch_bounds__(kThreads) attend_kernel(Args a) {
-  constexpr int kTerms = FLOAT ? Half<CT>::kTerms : 1;
-  constexpr int kRows = 16 * MT;                   // rows of a unit
-  constexpr int kSteps = DP / 32;                  // of a score's sum
-  constexpr int kEach = DP / 16 < 8 ? DP / 16 : 8; // neighbouring dimensions of a lane's piece of a value
-  constexpr int kParts = DP / (16 * kEach);        // such pieces
-  constexpr int kLine = DP + 4;                    // floats between rows in LDS
-
-  __shared__ int64_t unit_end[kThreads];
-  __shared__ int32_t slot_end[kThreads], group_end[kThreads];
-  __shared__ int64_t sums[kWaves];
-  __shared__ int32_t more[kWaves][2];
-  __shared__ float row_m[kWaves][kRows], row_l[kWaves][kRows];
-  __shared__ __align__(16) float joined[kWaves][16][kLine];
-  __shared__ uint32_t arrived;
-
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-
-  // -- every workgroup counts the pieces of all requests, a run of requests per thread
-  const int run = (a.requests + kThreads - 1) / kThreads, run0 = min(tid * run, a.requests), run1 = min(run0 + run, a.requests);
-  int64_t work = 0;
-  for (int r = run0; r < run1; ++r) {
-    const Request q = request_of(a, r);
-    work += (((int64_t)q.fresh * a.group + kRows - 1) / kRows) * a.kv_heads * (tiles_of(q.held) + tiles_of(q.fresh));
+  static __device__ int blocks_of(const Args& a, const Request& q) { return (q.fresh * a.group + ROWS - 1) / ROWS; }
+  static __device__ int tiles_in(const Request& q) { return tiles_of(q.held) + tiles_of(q.fresh); }
+  __device__ int pieces_of(const Request& q) const {
+    const uint32_t tiles = tiles_in(q);
+    return tiles <= (uint32_t)most ? 1 : (tiles + most - 1) / (uint32_t)most;
   }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d);
-  if (lane == 0) sums[wave] = work;
-  __syncthreads();
-  work = sums[0] + sums[1] + sums[2] + sums[3];
-  const int64_t most = max((work + a.target - 1) / a.target, (int64_t)kLeastTiles);
-  Counts mine{0, 0, 0};
-  for (int r = run0; r < run1; ++r) {
-    int blocks, pieces;
-    const Counts c = counts_of(request_of(a, r), kRows, a.group, a.kv_heads, most, &blocks, &pieces);
-    mine.units += c.units, mine.slots += c.slots, mine.groups += c.groups;
+  __device__ void count(const Args& a, const Request& q, int64_t& units, uint64_t& cut) const {
+    const int pieces = pieces_of(q);
+    const int64_t sets = (int64_t)blocks_of(a, q) * a.kv_heads;
+    units += sets * pieces;
+    if (pieces > 1) cut += (uint64_t)(sets * pieces) << 32 | (uint64_t)sets;
   }
-  const Counts own = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t u = __shfl_up(mine.units, d);
-    const int s = __shfl_up(mine.slots, d), o = __shfl_up(mine.groups, d);
-    if (lane >= d) mine.units += u, mine.slots += s, mine.groups += o;
-  }
-  __syncthreads();
-  if (lane == 63) sums[wave] = mine.units, more[wave][0] = mine.slots, more[wave][1] = mine.groups;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) mine.units += sums[w], mine.slots += more[w][0], mine.groups += more[w][1];
-  unit_end[tid] = mine.units, slot_end[tid] = mine.slots - own.slots, group_end[tid] = mine.groups - own.groups;
-  __syncthreads();
-  const int64_t units = unit_end[kThreads - 1];
 
-  // consecutive pieces (the same cached tokens for other rows) go to workgroups of one XCD (blockIdx % 8)
-  const int grid = gridDim.x, eighth = grid / 8;
-  const int64_t first_unit = grid % 8 ? blockIdx.x : (int64_t)(blockIdx.x % 8) * eighth + blockIdx.x / 8;
-
-  for (int64_t unit = first_unit; unit < units; unit += grid) {
-    // -- which request, key head, piece and rows
-    int lo = 0, hi = kThreads - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (unit_end[mid] > unit) hi = mid;
-      else lo = mid + 1;
-    }
-    int64_t at = unit - (lo ? unit_end[lo - 1] : 0);
-    int r = lo * run, blocks, pieces, slot = slot_end[lo], set = group_end[lo];
-    Request q;
-    for (;; ++r) {
+  __device__ explicit Plan(const Args& a, int lane) {
+    run = (a.requests + 63) / 64;
+    const int r0 = min(lane * run, a.requests), r1 = min(r0 + run, a.requests);
+    int64_t work = 0;
+    q = {0, 0, 0};
+    for (int r = r1 - 1; r >= r0; --r) {
       q = request_of(a, r);
-      const Counts c = counts_of(q, kRows, a.group, a.kv_heads, most, &blocks, &pieces);
-      if (at < c.units) break;
-      at -= c.units, slot += c.slots, set += c.groups;
+      work += (int64_t)blocks_of(a, q) * a.kv_heads * tiles_in(q);
     }
-    const int block = (int)(at % blocks), piece = (int)(at / blocks % pieces), head = (int)(at / blocks / pieces);
-    set += head * blocks + block;
-    slot += (head * blocks + block) * pieces + piece;
-    const int row0 = block * kRows, rows = min(kRows, q.fresh * a.group - row0);
-    const int cached = tiles_of(q.held);
-    const int last_token = (row0 + rows - 1) / a.group;
-    const int tiles = cached + (a.mask ? tiles_of(q.fresh) : tiles_of(last_token + 1));
-    const int begin = (int)((int64_t)tiles * piece / pieces), end = (int)((int64_t)tiles * (piece + 1) / pieces);
-    const int t0 = begin + (end - begin) * wave / kWaves, t1 = begin + (end - begin) * (wave + 1) / kWaves;
+    if (a.requests > 1) {
+#pragma unroll
+      for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d);
+    } else {
+      work = from_lane(work, 0);
+    }
+    most = max((int)((double)work * a.per_target) + 1, kLeastTiles);
+    int64_t mine = 0;
+    uint64_t mine_cut = 0;
+    if (run == 1) {
+      if (r0 < r1) count(a, q, mine, mine_cut);
+    } else {
+      for (int r = r0; r < r1; ++r) count(a, request_of(a, r), mine, mine_cut);
+    }
+    end = mine, cut = mine_cut;
+    if (a.requests > 1) {
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int64_t u = __shfl_up(end, d);
+        const uint64_t c = __shfl_up(cut, d);
+        if (lane >= d) end += u, cut += c;
+      }
+    } else {
+      end = from_lane(end, 0);
+    }
+    cut -= mine_cut;
+    units = from_lane(end, 63);
+  }
 
-    // -- queries: operand B of the scores, zeros behind the last dimension and the last row
-    u4 query[MT][kSteps][kTerms];
-    float factor[MT];  // of a score to its exponent of two
-    int token[MT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int row = row0 + mt * 16 + n;
-      const bool there = mt * 16 + n < rows;
-      token[mt] = there ? row / a.group : 0;
-      const int64_t from = (q.first + token[mt]) * a.q_stride + (int64_t)(head * a.group + (there ? row - token[mt] * a.group : 0)) * a.dim;
-      factor[mt] = a.scale * 1.44269504088896341f;
-      if constexpr (!FLOAT) {
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          const int d = 32 * s + 8 * g;
-          u4 x{0, 0, 0, 0};
-          if (there && d < a.dim) x = *reinterpret_cast<const u4*>(static_cast<const uint16_t*>(a.q) + from + d);
-          query[mt][s][0] = x;
-        }
-      } else {
-        float x[kSteps][8];
-        float top = 0.f;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          const int d = 32 * s + 8 * g;
-          f4 lo4{0, 0, 0, 0}, hi4{0, 0, 0, 0};
-          if (there && d < a.dim) {
-            const f4* p = reinterpret_cast<const f4*>(static_cast<const float*>(a.q) + from + d);
-            lo4 = p[0], hi4 = p[1];
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[s][j] = lo4[j], x[s][4 + j] = hi4[j];
-            top = fmaxf(top, fmaxf(fabsf(lo4[j]), fabsf(hi4[j])));
-          }
-        }
-        if constexpr (sizeof(CT) == 2 && Half<CT>::kTerms == 2) {
-          // float16 has not the range of float: the row's largest query becomes 2^14 (exact, taken back by the factor)
-          top = over_groups_max(top);
-          const int e = top > 0.f && top < INFINITY ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
-#pragma unroll
-          for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[s][j] = ldexpf(x[s][j], e);
-          factor[mt] = ldexpf(factor[mt], -e);
-        }
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) split<CT, kTerms>(x[s], query[mt][s]);
+  __device__ Unit find(const Args& a, int64_t unit) const {
+    Unit u;
+    const int lane = __builtin_amdgcn_readfirstlane(__builtin_ctzll(__ballot(end > unit)));
+    int64_t at = unit - (lane ? from_lane(end, lane - 1) : 0);
+    uint64_t before = from_lane(cut, lane);
+    u.r = lane * run;
+    if (run == 1) {
+      u.q = {from_lane(q.first, lane), from_lane(q.fresh, lane), from_lane(q.held, lane)};
+    } else {
+      for (;; ++u.r) {
+        const Request q = request_of(a, u.r);
+        u.q = {from_lane(q.first, 0), from_lane(q.fresh, 0), from_lane(q.held, 0)};
+        int64_t n = 0;
+        uint64_t c = 0;
+        count(a, u.q, n, c);
+        if (at < n) break;
+        at -= n, before += c;
       }
     }
+    const uint32_t blocks = blocks_of(a, u.q), in = (uint32_t)at, block = in % blocks, rest = in / blocks;
+    u.pieces = pieces_of(u.q);
+    u.piece = rest % (uint32_t)u.pieces, u.head = rest / (uint32_t)u.pieces;
+    u.set = (int)(uint32_t)before + u.head * blocks + block;
+    u.slot = (int)(before >> 32) + (u.head * blocks + block) * u.pieces + u.piece;
+    u.row0 = block * ROWS, u.rows = min(ROWS, u.q.fresh * a.group - u.row0);
+    u.cached = tiles_of(u.q.held);
+    const int tiles = u.cached + tiles_of(a.mask ? u.q.fresh : (u.row0 + u.rows - 1) / a.group + 1);  // (a chain's rows see no further)
+    // pieces as even as can be
+    const int each = tiles / u.pieces, more = tiles - each * u.pieces;
+    u.tile0 = each * u.piece + min(u.piece, more), u.tile1 = u.tile0 + each + (u.piece < more);
+    return u;
+  }
+};
 
-    f4 acc[MT][kParts * kEach];
-    float m[MT], base[MT], l[MT];  // base: what is taken off an exponent
+// Consecutive pieces (the same cached tokens for other rows) go to workgroups of one XCD (blockIdx % 8).
+__device__ inline int64_t first_unit() {
+  return gridDim.x % 8 ? blockIdx.x : (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+}
+
+__device__ inline int token_of(const Args& a, int row) { return a.group_inverse ? (int)__umulhi((uint32_t)row, a.group_inverse) : row; }
+
+// The first of `count` dimensions: where the head ends before them the last ones it has (they meet zeros of the query, or a
+// result that nobody wants).  FULL: the head has as many dimensions as the kernel.
+template <bool FULL> __device__ inline int within(const Args& a, int d, int count) { return FULL ? d : min(d, a.dim - count); }
+
+// ---- the rows of a wavefront --------------------------------------------------------------------------------
+template <typename CT, bool FLOAT, int DP> struct Rows {
+  static constexpr int kTerms = FLOAT ? Half<CT>::kTerms : 1;
+  static constexpr int kSteps = DP / 32;                   // of a score's sum
+  static constexpr int kEach = DP / 16 < 8 ? DP / 16 : 8;  // neighbouring dimensions of a lane's piece of a value
+  static constexpr int kParts = DP / (16 * kEach);         // such pieces
+
+  f4 acc[kParts * kEach], sum;
+  float factor;  // of a score to its exponent of two
+  float base;    // taken off the exponents: m - kBias
+  float limit;   // of an exponent: kLimit, and -infinity before the row has seen anything
+  int token;
+
+  // Queries of the 16 rows from `first` on: operand B of the scores, zeros behind the last dimension and the last row.
+  __device__ void begin(const Args& a, const Unit& u, int first, int n, int g, u4 (&query)[kSteps][kTerms]) {
+    const int in = first + n, row = u.row0 + in;
+    const bool there = in < u.rows;
+    token = there ? token_of(a, row) : 0;
+    const int64_t from = (u.q.first + token) * a.q_stride + (int64_t)(u.head * a.group + (there ? row - token * a.group : 0)) * a.dim;
+    factor = a.scale * 1.44269504088896341f;
+    base = 0.f, limit = -INFINITY;
+    sum = f4{0, 0, 0, 0};
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      m[mt] = -INFINITY, base[mt] = 0.f, l[mt] = 0.f;
+    for (int j = 0; j < kParts * kEach; ++j) acc[j] = f4{0, 0, 0, 0};
+    if constexpr (!FLOAT) {
 #pragma unroll
-      for (int j = 0; j < kParts * kEach; ++j) acc[mt][j] = f4{0, 0, 0, 0};
+      for (int s = 0; s < kSteps; ++s) {
+        const int d = 32 * s + 8 * g;
+        u4 x{0, 0, 0, 0};
+        if (there && d < a.dim) x = *reinterpret_cast<const u4*>(static_cast<const uint16_t*>(a.q) + from + d);
+        query[s][0] = x;
+      }
+    } else {
+      float x[kSteps][8];
+      float top = 0.f;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const int d = 32 * s + 8 * g;
+        f4 lo{0, 0, 0, 0}, hi{0, 0, 0, 0};
+        if (there && d < a.dim) {
+          const f4* p = reinterpret_cast<const f4*>(static_cast<const float*>(a.q) + from + d);
+          lo = p[0], hi = p[1];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[s][j] = lo[j], x[s][4 + j] = hi[j];
+          top = fmaxf(top, fmaxf(fabsf(lo[j]), fabsf(hi[j])));
+        }
+      }
+      if constexpr (Half<CT>::kTerms == 2) {
+        // float16 has not the range of float: the row's largest query becomes 2^14 (exact, taken back by the factor)
+        top = over_groups_max(top);
+        const int e = top > 0.f && top < INFINITY ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[s][j] = ldexpf(x[s][j], e);
+        factor = ldexpf(factor, -e);
+      }
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) split<CT, kTerms>(x[s], query[s]);
     }
+  }
 
-    u4 key[2][kSteps];
-    uint32_t value[kParts][8][kEach / 2];  // [token][pair of dimensions]
+  // Scores of two tiles of 16 keys, a step of 32 dimensions.
+  static __device__ void add_score(u4 lo, u4 hi, const u4 (&query)[kTerms], f4 (&x)[2]) {
+#pragma unroll
+    for (int t = kTerms - 1; t >= 0; --t) {
+      x[0] = Half<CT>::mfma(lo, query[t], x[0]);
+      x[1] = Half<CT>::mfma(hi, query[t], x[1]);
+    }
+  }
 
-    auto scores = [&](int mt, float (&s)[8]) {
-      f4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  __device__ void exponents(const f4 (&x)[2], float (&s)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = fmaf(x[j >> 2][j & 3], factor, -base);
+  }
+
+  // Exponents to weights and to operand B of the result.
+  __device__ void weigh(float (&s)[8], u4 (&p)[kTerms]) {
+    float top = max3(max3(max3(s[0], s[1], s[2]), s[3], s[4]), max3(s[5], s[6], s[7]), -INFINITY);
+    if (__ballot(top > limit)) {
+      // the maximum follows where it is left behind: a row's matter alone, so that no other row's scores move it
+      top = over_groups_max(top);
+      if (top > limit) {
+        const float up = top - kBias, back = limit == kLimit ? exp2f(-up) : 0.f;
+        base += up;
+        limit = kLimit;
+        sum *= back;
+#pragma unroll
+        for (int j = 0; j < kParts * kEach; ++j) acc[j] *= back;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] -= up;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = __builtin_amdgcn_exp2f(s[j]);
+    split<CT, kTerms>(s, p);
+    const u4 ones{Half<CT>::kOnes, Half<CT>::kOnes, Half<CT>::kOnes, Half<CT>::kOnes};
+#pragma unroll
+    for (int t = kTerms - 1; t >= 0; --t) sum = Half<CT>::mfma(ones, p[t], sum);
+  }
+
+  // Of eight positions the dimension that is number j of the lane's piece.
+  static __device__ u4 column(const uint32_t (&value)[8][kEach / 2], int j) {
+    u4 x;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) x[t] = __builtin_amdgcn_perm(value[2 * t + 1][j >> 1], value[2 * t][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+    return x;
+  }
+  // Values of part `part`: [position][pair of dimensions].
+  __device__ void add_values(int part, const uint32_t (&value)[8][kEach / 2], const u4 (&p)[kTerms]) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const u4 x = column(value, j);
+#pragma unroll
+      for (int t = kTerms - 1; t >= 0; --t) acc[part * kEach + j] = Half<CT>::mfma(x, p[t], acc[part * kEach + j]);
+    }
+  }
+
+  // Which of eight new tokens from number j0 on the row sees, a bit each.
+  __device__ int seen_new(const Args& a, const Unit& u, bool row, int j0) const {
+    int bits = 255;
+    if (row) bits = a.mask ? (int)(a.mask[u.q.first + token] >> min(j0, 63)) & 255 : eight_bits(token + 1 - j0);
+    return bits & eight_bits(u.q.fresh - j0);
+  }
+
+  // A value that is not finite must not reach the rows that do not see it (0 times infinity is NaN).  Does the lane hold one?
+  static __device__ bool is_odd(uint32_t half) { return (half & Half<CT>::kExponent) == Half<CT>::kExponent; }
+  static __device__ bool has_odd(const uint32_t (&value)[8][kEach / 2]) {
+    bool odd = false;
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+#pragma unroll
+      for (int j = 0; j < kEach / 2; ++j) odd |= is_odd(value[t][j]) || is_odd(value[t][j] >> 16);
+    return odd;
+  }
+  // As add_values, for such values: they are left out of the product, and sums of the weights of the positions that have
+  // +infinity or NaN, and -infinity or NaN, say where the result becomes what.
+  __device__ void add_odd_values(int part, const uint32_t (&value)[8][kEach / 2], const u4 (&p)[kTerms]) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      u4 x = column(value, j), up, down;
+      const uint32_t exponent = hidden(Half<CT>::kExponent), ones = hidden(Half<CT>::kOnes);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        uint32_t kept = x[t], more = 0, less = 0;
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+          const uint32_t half = x[t] >> h & 0xffff, one = ones & 0xffffu << h;
+          const bool nan = (half & 0x7fff) > exponent;
+          if ((half & exponent) == exponent) kept &= ~(0xffffu << h);
+          if (nan || half == exponent) more |= one;
+          if (nan || half == (exponent | 0x8000)) less |= one;
+        }
+        x[t] = kept, up[t] = more, down[t] = less;
+      }
+      f4& to = acc[part * kEach + j];
+#pragma unroll
+      for (int t = kTerms - 1; t >= 0; --t) to = Half<CT>::mfma(x, p[t], to);
+      const f4 plus = Half<CT>::mfma(up, p[0], f4{0, 0, 0, 0}), minus = Half<CT>::mfma(down, p[0], f4{0, 0, 0, 0});
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[i] += (plus[i] > 0.f ? INFINITY : 0.f) + (minus[i] > 0.f ? -INFINITY : 0.f);
+      __builtin_amdgcn_sched_barrier(0);  // (seldom taken: let it need few registers)
+    }
+  }
+
+  __device__ float maximum() const { return limit == kLimit ? base + kBias : -INFINITY; }
+  // Four dimensions from dimension 16 * kEach * part + kEach * (4 * g + i) + j on.
+  __device__ f4 four(int part, int i, int j) const {
+    return f4{acc[part * kEach + j][i], acc[part * kEach + j + 1][i], acc[part * kEach + j + 2][i], acc[part * kEach + j + 3][i]};
+  }
+};
+
+// ---- results ------------------------------------------------------------------------------------------------
+template <typename CT, bool FLOAT> __device__ inline void store(const Args& a, const Unit& u, int in, int d, f4 x, float total) {
+  const int row = u.row0 + in, token = token_of(a, row);
+  const int64_t to = (u.q.first + token) * a.out_stride + (int64_t)(u.head * a.group + row - token * a.group) * a.dim + d;
+  const f4 o = total == 0.f ? f4{0, 0, 0, 0} : x / total;
+  if constexpr (FLOAT) *reinterpret_cast<f4*>(static_cast<float*>(a.out) + to) = o;
+  else *reinterpret_cast<u2*>(static_cast<uint16_t*>(a.out) + to) = u2{pair_of<CT>(o[0], o[1]), pair_of<CT>(o[2], o[3])};
+}
+
+// A piece in the workspace: of every row DP values, their maximum and their sum of weights.
+template <int DP, int ROWS> struct Partial {
+  static constexpr int kRow = DP + 4, kPiece = ROWS * kRow;
+  static __device__ float* row(const Args& a, int slot, int in) { return a.partial + (int64_t)slot * kPiece + in * kRow; }
+};
+
+// Writes of a piece go past the L2 of the XCD, to where all XCDs read: no write-back of a whole L2 has to follow them.
+__device__ inline void write_through(float* to, float x, float y) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), __builtin_bit_cast(uint64_t, u2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)}),
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline void write_through(float* to, f4 x) { write_through(to, x[0], x[1]), write_through(to + 2, x[2], x[3]); }
+
+// 2^(m - top) for a maximum that may be that of nothing
+__device__ inline float behind(float m, float top) { return m == -INFINITY ? 0.f : exp2f(m - top); }
+
+// The workgroup that comes last joins the pieces of its rows, in their order.  What the others wrote is there: every wavefront
+// waits until its writes, which go through all caches, are done, then the workgroup counts itself; the last one drops what its own
+// caches may hold before it reads.
+template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inline void join(const Args& a, const Unit& u, int tid, uint32_t& arrived) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) arrived = __hip_atomic_fetch_add(&a.counters[u.set], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  const bool last = arrived == (uint32_t)u.pieces - 1;
+  __syncthreads();
+  if (!last) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  if (tid == 0) __hip_atomic_store(&a.counters[u.set], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  typedef Partial<DP, ROWS> P;
+  for (int e = tid; e < u.rows * (DP / 4); e += THREADS) {
+    const int in = e / (DP / 4), d = e % (DP / 4) * 4;
+    if (d >= a.dim) continue;
+    const float* from = P::row(a, u.slot - u.piece, in);
+    float top = -INFINITY, total = 0.f;
+#pragma unroll 8
+    for (int c = 0; c < u.pieces; ++c) top = fmaxf(top, from[c * P::kPiece + DP]);
+    f4 x{0, 0, 0, 0};
+#pragma unroll 8
+    for (int c = 0; c < u.pieces; ++c) {
+      const float* p = from + c * P::kPiece;
+      const float w = behind(p[DP], top);
+      total += p[DP] == -INFINITY ? p[DP + 1] : p[DP + 1] * w;  // (without a maximum: 0, or NaN)
+      x += *reinterpret_cast<const f4*>(p + d) * w;
+    }
+    store<CT, FLOAT>(a, u, in, d, x, total);
+  }
+}
+
+// ---- few rows: the wavefronts split the positions -----------------------------------------------------------
+template <typename CT, bool FLOAT, int DP, bool FULL>
+__global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
+  typedef Rows<CT, FLOAT, DP> R;
+  constexpr int kRows = 16, kSteps = R::kSteps, kEach = R::kEach, kParts = R::kParts, kTerms = R::kTerms;
+  constexpr int kLine = DP + 4;  // floats between rows in LDS
+  __shared__ float row_m[kWaves][kRows], row_l[kWaves][kRows];
+  __shared__ __align__(16) float joined[kWaves][16][kLine];
+  __shared__ __align__(16) u4 queries[FLOAT ? kSteps : 1][FLOAT ? kTerms : 1][64];  // the operands of floats fill too many registers
+  __shared__ uint32_t arrived;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Plan<kRows> plan(a, threadIdx.x & 63);
+
+  for (int64_t unit = first_unit(); unit < plan.units; unit += gridDim.x) {
+    const int tid = hidden(threadIdx.x), lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const Unit u = plan.find(a, unit);
+    const int t0 = u.tile0 + (u.tile1 - u.tile0) * wave / kWaves, t1 = u.tile0 + (u.tile1 - u.tile0) * (wave + 1) / kWaves;
+    R rows;
+    u4 query[kSteps][kTerms];
+    rows.begin(a, u, 0, n, g, query);
+    if constexpr (FLOAT) {
+      // (all wavefronts have the same rows, and write the same)
 #pragma unroll
       for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-        for (int t = kTerms - 1; t >= 0; --t)
+        for (int t = 0; t < kTerms; ++t) queries[k][t][lane] = query[k][t];
+      asm volatile("" ::: "memory");
+    }
+    u4 key[2][kSteps];
+    uint32_t value[kParts][8][kEach / 2];
+    auto scores = [&](f4 (&x)[2]) {
+      x[0] = x[1] = f4{0, 0, 0, 0};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) x[h] = Half<CT>::mfma(key[h][k], query[mt][k][t], x[h]);
+      for (int k = 0; k < kSteps; ++k) {
+        if constexpr (FLOAT) {
+          u4 q[kTerms];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = x[j >> 2][j & 3] * factor[mt];
-    };
-    // m follows the maximum of the row where it is left behind
-    auto follow = [&](int mt, const float (&s)[8]) {
-      float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-      if (__ballot(top > m[mt] + kSlack)) {
-        top = over_groups_max(top);
-        if (top > m[mt] + kSlack) {
-          const float back = exp2f(m[mt] - top);  // (0 at first)
-          m[mt] = top, base[mt] = top - kBias;
-          l[mt] *= back;
-#pragma unroll
-          for (int j = 0; j < kParts * kEach; ++j) acc[mt][j] *= back;
+          for (int t = 0; t < kTerms; ++t) q[t] = queries[k][t][lane];
+          R::add_score(key[0][k], key[1][k], q, x);
+        } else {
+          R::add_score(key[0][k], key[1][k], query[k], x);
         }
       }
     };
-    auto weights = [&](int mt, float (&s)[8]) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = __builtin_amdgcn_exp2f(s[j] - base[mt]);
-      l[mt] += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
-    };
-    // operand A of the result: of eight tokens the dimension that is number j of the lane's piece
-    auto transposed = [&](int part, int j) {
-      u4 x;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        x[t] = __builtin_amdgcn_perm(value[part][2 * t + 1][j >> 1], value[part][2 * t][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
-      return x;
-    };
-    auto add_values = [&](const u4 (&p)[MT][kTerms]) {
-#pragma unroll
-      for (int part = 0; part < kParts; ++part)
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const u4 x = transposed(part, j);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int t = kTerms - 1; t >= 0; --t) acc[mt][part * kEach + j] = Half<CT>::mfma(x, p[mt][t], acc[mt][part * kEach + j]);
-        }
-    };
 
-    // ---- cached tokens
-    const int c1 = min(t1, cached);
+    // ---- cached tokens.  Loads run ahead by a tile, their pages by two; the last ones are loaded again instead of none,
+    // so that the order of loads is the same in every turn and none waits for a later one.
+    const int c1 = min(t1, u.cached);
     if (t0 < c1) {
-      const int last_page = (q.held - 1) >> a.log2_page;
-      const int32_t* table = a.table + (int64_t)r * a.max_pages;
-      int window = (t0 * kTile) >> a.log2_page;  // the lanes hold the entries of the table from here on, and the 64 after those
-      auto entry = [&](int at) { return at <= last_page ? table[at] : -1; };
-      int now = entry(window + lane), next = entry(window + 64 + lane);
-      const int64_t head_at = (int64_t)head * a.head_stride, in_page = (int64_t(1) << a.log2_page) - 1;
-      auto page_for = [&](int position) { return __shfl(now, (position >> a.log2_page) - window); };
-      auto advance = [&](int tile) {
-        if (((tile * kTile + kTile - 1) >> a.log2_page) - window >= 64) {
-          window += 64;  // (a tile that begins inside the window ends inside it: both begin at a multiple of a tile's pages)
-          now = next;
-          next = entry(window + 64 + lane);
-        }
+      const int last_page = (u.q.held - 1) >> a.log2_page, in_page = (1 << a.log2_page) - 1;
+      const int32_t* table = a.table + (int64_t)u.r * a.max_pages;
+      const int key_at = 8 * (n >> 2), value_at = 8 * g;  // (eight positions from a multiple of eight lie on one page)
+      auto page = [&](int tile, int at) { return table[min((tile * kTile + at) >> a.log2_page, last_page)]; };
+      // a tile's first position on its page times the stride; the lane's own part is the same for all tiles
+      auto row_of = [&](const uint16_t* cache, int tile, int page, uint32_t lane_part) {
+        const uint16_t* p = cache + (int64_t)u.head * a.head_stride + (int64_t)((tile * kTile) & in_page) * a.token_stride;
+        return p + (uint64_t)((uint32_t)page < (uint32_t)a.pages ? (uint32_t)page : 0u) * a.page_stride + lane_part;
       };
-      auto load_keys = [&](int tile) {
-        const int position = tile * kTile + 8 * (n >> 2) + (n & 3);
-        const int page = page_for(position);
-        const uint16_t* p = a.cache_k + ((uint32_t)page < (uint32_t)a.pages ? page : 0) * a.page_stride + head_at + (position & in_page) * a.token_stride;
+      const uint32_t key_lane = ((key_at & in_page) + (n & 3)) * a.token_stride, value_lane = (value_at & in_page) * a.token_stride;
+      auto load_keys = [&](int tile, int page) {
+        const uint16_t* p = row_of(a.cache_k, tile, page, key_lane);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int k = 0; k < kSteps; ++k) key[h][k] = *reinterpret_cast<const u4*>(p + 4 * h * a.token_stride + min(32 * k + 8 * g, a.dim - 8));
+          for (int k = 0; k < kSteps; ++k) key[h][k] = *reinterpret_cast<const u4*>(p + 4 * h * a.token_stride + within<FULL>(a, 32 * k + 8 * g, 8));
       };
-      auto load_values = [&](int tile, int& seen) {
-        const int position = tile * kTile + 8 * g;
-        const int page = page_for(position);
-        const bool there = (uint32_t)page < (uint32_t)a.pages;
-        seen = there ? (1 << max(min(q.held - position, 8), 0)) - 1 : 0;
-        const uint16_t* p = a.cache_v + (there ? page : 0) * a.page_stride + head_at + (position & in_page) * a.token_stride;
+      auto load_values = [&](int tile, int page) {
+        const uint16_t* p = row_of(a.cache_v, tile, page, value_lane);
 #pragma unroll
         for (int part = 0; part < kParts; ++part)
 #pragma unroll
           for (int t = 0; t < 8; ++t) {
-            const uint16_t* from = p + t * a.token_stride + min(part * 16 * kEach + kEach * n, a.dim - kEach);
+            const uint16_t* from = p + t * a.token_stride + within<FULL>(a, part * 16 * kEach + kEach * n, kEach);
             if constexpr (kEach == 8) {
               const u4 x = *reinterpret_cast<const u4*>(from);
 #pragma unroll
@@ -370,252 +586,272 @@ __global__ void __launch_bounds__(kThreads) attend_kernel(Args a) {
               value[part][t][0] = x[0], value[part][t][1] = x[1];
             }
           }
+        return (uint32_t)page < (uint32_t)a.pages ? eight_bits(u.q.held - tile * kTile - value_at) : 0;
       };
-      int seen;
-      advance(t0);
-      load_keys(t0);
-      load_values(t0, seen);
+      int key_page = page(t0, key_at), value_page = page(t0, value_at);
+      int next_key_page = page(min(t0 + 1, c1 - 1), key_at), next_value_page = page(min(t0 + 1, c1 - 1), value_at);
+      load_keys(t0, key_page);
+      int seen = load_values(t0, value_page);
       for (int tile = t0; tile < c1; ++tile) {
-        const bool whole = __ballot(seen != 255) == 0;
-        u4 p[MT][kTerms];
-        float s[MT][8];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) scores(mt, s[mt]);
-        if (tile + 1 < c1) {
-          advance(tile + 1);
-          load_keys(tile + 1);
-        }
-        if (!whole) {
+        f4 x[2];
+        scores(x);
+        key_page = next_key_page, value_page = next_value_page;
+        next_key_page = page(min(tile + 2, c1 - 1), key_at), next_value_page = page(min(tile + 2, c1 - 1), value_at);
+        load_keys(min(tile + 1, c1 - 1), key_page);
+        float s[8];
+        u4 p[kTerms];
+        rows.exponents(x, s);
+        if (__ballot(seen != 255)) {
 #pragma unroll
           for (int t = 0; t < 8; ++t) {
             const bool is = seen >> t & 1;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) s[mt][t] = is ? s[mt][t] : -INFINITY;
+            s[t] = is ? s[t] : -INFINITY;
 #pragma unroll
             for (int part = 0; part < kParts; ++part)
 #pragma unroll
               for (int j = 0; j < kEach / 2; ++j) value[part][t][j] = is ? value[part][t][j] : 0u;
           }
         }
+        rows.weigh(s, p);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          follow(mt, s[mt]);
-          weights(mt, s[mt]);
-          split<CT, kTerms>(s[mt], p[mt]);
-        }
-        add_values(p);
-        if (tile + 1 < c1) load_values(tile + 1, seen);
+        for (int part = 0; part < kParts; ++part) rows.add_values(part, value[part], p);
+        seen = load_values(min(tile + 1, c1 - 1), value_page);
       }
     }
 
     // ---- new tokens
-    for (int tile = max(t0, cached); tile < t1; ++tile) {
-      const int j0 = (tile - cached) * kTile;
-      const int64_t kv_at = (int64_t)head * a.dim;
-      auto load8 = [&](const void* p, int64_t at) {
-        if constexpr (!FLOAT) return *reinterpret_cast<const u4*>(static_cast<const uint16_t*>(p) + at);
-        else {
-          const f4* f = reinterpret_cast<const f4*>(static_cast<const float*>(p) + at);
-          const f4 lo4 = f[0], hi4 = f[1];
-          const float x[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]};
-          u4 t[1];
-          split<CT, 1>(x, t);
-          return t[0];
-        }
-      };
-      const int j_key = j0 + 8 * (n >> 2) + (n & 3), j_value = j0 + 8 * g;
+    for (int tile = max(t0, u.cached); tile < t1; ++tile) {
+      const int j0 = (tile - u.cached) * kTile;
+      const int64_t in_row = (int64_t)u.head * a.dim;
+      Eight<CT, FLOAT> e;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int64_t from = (q.first + min(j_key + 4 * h, q.fresh - 1)) * a.kv_stride + kv_at;
+        const int64_t from = (u.q.first + min(j0 + 8 * (n >> 2) + (n & 3) + 4 * h, u.q.fresh - 1)) * a.kv_stride + in_row;
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) key[h][k] = load8(a.k, from + min(32 * k + 8 * g, a.dim - 8));
+        for (int k = 0; k < kSteps; ++k) {
+          e.load(a.k, from + within<FULL>(a, 32 * k + 8 * g, 8));
+          key[h][k] = e.rounded();
+        }
       }
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const bool there = j_value + t < q.fresh;
-        const int64_t from = (q.first + min(j_value + t, q.fresh - 1)) * a.kv_stride + kv_at;
+        const bool there = j0 + 8 * g + t < u.q.fresh;
+        const int64_t from = (u.q.first + min(j0 + 8 * g + t, u.q.fresh - 1)) * a.kv_stride + in_row;
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-          if constexpr (kEach == 8) {
-            const u4 x = load8(a.v, from + min(part * 128 + 8 * n, a.dim - 8));
+          const int d = within<FULL>(a, part * 16 * kEach + kEach * n, kEach);
+          e.load(a.v, from + (d & ~7));  // (of eight dimensions the lane may take four)
+          const u4 x = e.rounded();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) value[part][t][j] = there ? x[j] : 0u;
-          } else {
-            const int d = min(4 * n, a.dim - 4);  // (eight from a multiple of eight, of which this lane takes its four)
-            const u4 x = load8(a.v, from + (d & ~7));
-#pragma unroll
-            for (int j = 0; j < 2; ++j) value[part][t][j] = there ? (d & 4 ? x[2 + j] : x[j]) : 0u;
-          }
+          for (int j = 0; j < kEach / 2; ++j) value[part][t][j] = there ? (kEach == 4 && d & 4 ? x[2 + j] : x[j]) : 0u;
         }
       }
-      u4 p[MT][kTerms];
-      float s[MT][8];
-      int seen[MT];
-      bool whole = true;
+      f4 x[2];
+      scores(x);
+      float s[8];
+      u4 p[kTerms];
+      rows.exponents(x, s);
+      const int seen = rows.seen_new(a, u, n < u.rows, j0 + 8 * g);
+      bool odd = false;
+      if (__ballot(seen != 255)) {
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        if (a.mask) {
-          const uint64_t bits = mt * 16 + n < rows ? a.mask[q.first + token[mt]] : ~0ull;
-          seen[mt] = (int)(bits >> j_value) & 255;  // (j_value < 64: with a mask there are at most two tiles)
-        } else {
-          seen[mt] = mt * 16 + n < rows ? (1 << max(min(token[mt] + 1 - j_value, 8), 0)) - 1 : 255;
-        }
-        seen[mt] &= (1 << max(min(q.fresh - j_value, 8), 0)) - 1;
-        whole &= seen[mt] == 255;
-        scores(mt, s[mt]);
+        for (int part = 0; part < kParts; ++part) odd |= R::has_odd(value[part]);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) s[t] = seen >> t & 1 ? s[t] : -INFINITY;
       }
-      const bool partly = __ballot(!whole) != 0;
-      // A value that is not finite must not reach the rows that do not see it (0 times infinity is NaN): it is left out
-      // of the product and added to the rows that see it by itself.
-      uint32_t odd = 0;
-      if (partly) {
-        constexpr uint32_t kExponent = Half<CT>::kTerms == 2 ? 0x7c00u : 0x7f80u;
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-#pragma unroll
-          for (int part = 0; part < kParts; ++part)
-#pragma unroll
-            for (int j = 0; j < kEach / 2; ++j) {
-              uint32_t& x = value[part][t][j];
-              const bool lo_odd = (x & kExponent) == kExponent, hi_odd = ((x >> 16) & kExponent) == kExponent;
-              odd |= (lo_odd || hi_odd) ? 1u << t : 0u;
-              x &= (lo_odd ? 0xffff0000u : ~0u) & (hi_odd ? 0x0000ffffu : ~0u);
-            }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int t = 0; t < 8; ++t) s[mt][t] = seen[mt] >> t & 1 ? s[mt][t] : -INFINITY;
-      }
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        follow(mt, s[mt]);
-        weights(mt, s[mt]);
-        split<CT, kTerms>(s[mt], p[mt]);
-      }
-      add_values(p);
+      rows.weigh(s, p);
       if (__ballot(odd)) {
-        for (int t = 0; t < kTile; ++t) {
-          const int from_group = t >> 3;
-          if (!(__ballot(odd >> (t & 7) & 1) >> (16 * from_group) & 0xffff)) continue;
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            float w = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w = (t & 7) == j ? s[mt][j] : w;
-            w = __shfl(w, 16 * from_group + n);
-            const bool sees = __shfl(seen[mt], 16 * from_group + n) >> (t & 7) & 1;
-            const int64_t from = (q.first + min(j0 + t, q.fresh - 1)) * a.kv_stride + kv_at;
-#pragma unroll
-            for (int part = 0; part < kParts; ++part)
-#pragma unroll
-              for (int j = 0; j < kEach; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const int d = part * 16 * kEach + kEach * (4 * g + i) + j;
-                  if (sees && d < a.dim) {
-                    float x;
-                    if constexpr (FLOAT) x = (float)(CT)static_cast<const float*>(a.v)[from + d];
-                    else x = (float)static_cast<const CT*>(a.v)[from + d];
-                    if (!(fabsf(x) < INFINITY)) acc[mt][part * kEach + j][i] += w * x;
-                  }
-                }
-          }
-        }
-      }
-    }
-
-    // ---- the four wavefronts of the workgroup
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      l[mt] = over_groups_sum(l[mt]);
-      if (g == 0) row_m[wave][mt * 16 + n] = m[mt], row_l[wave][mt * 16 + n] = l[mt];
-    }
-    __syncthreads();
-    float* const mine_out = a.partial + (int64_t)slot * kRows * stride_of_partial<DP>();
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      if (mt * 16 < rows) {
-        const int row = mt * 16 + n;
-        const float top = fmaxf(fmaxf(row_m[0][row], row_m[1][row]), fmaxf(row_m[2][row], row_m[3][row]));
-        const float mine_scale = m[mt] == -INFINITY ? 0.f : exp2f(m[mt] - top);
-#pragma unroll
-        for (int part = 0; part < kParts; ++part)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < kEach; j += 4) {
-              const f4 x{acc[mt][part * kEach + j][i], acc[mt][part * kEach + j + 1][i], acc[mt][part * kEach + j + 2][i], acc[mt][part * kEach + j + 3][i]};
-              *reinterpret_cast<f4*>(&joined[wave][n][part * 16 * kEach + kEach * (4 * g + i) + j]) = x * mine_scale;
-            }
-      }
-      __syncthreads();
-      for (int e = tid; e < 16 * (DP / 4); e += kThreads) {
-        const int row = e / (DP / 4), d = e % (DP / 4) * 4, of = mt * 16 + row;
-        if (of >= rows || d >= a.dim) continue;
-        const f4 x = (*reinterpret_cast<const f4*>(&joined[0][row][d]) + *reinterpret_cast<const f4*>(&joined[1][row][d])) +
-                     (*reinterpret_cast<const f4*>(&joined[2][row][d]) + *reinterpret_cast<const f4*>(&joined[3][row][d]));
-        const float top = fmaxf(fmaxf(row_m[0][of], row_m[1][of]), fmaxf(row_m[2][of], row_m[3][of]));
-        float total = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) total += row_m[w][of] == -INFINITY ? row_l[w][of] : row_l[w][of] * exp2f(row_m[w][of] - top);
-        if (pieces == 1) {
-          const int id = row0 + of, tok = id / a.group;
-          const int64_t to = (q.first + tok) * a.out_stride + (int64_t)(head * a.group + id - tok * a.group) * a.dim + d;
-          const f4 o = total == 0.f ? f4{0, 0, 0, 0} : x / total;
-          if constexpr (FLOAT) {
-            *reinterpret_cast<f4*>(static_cast<float*>(a.out) + to) = o;
-          } else {
-            const typename Half<CT>::v2 lo2{(CT)o[0], (CT)o[1]}, hi2{(CT)o[2], (CT)o[3]};
-            *reinterpret_cast<u2*>(static_cast<uint16_t*>(a.out) + to) = u2{__builtin_bit_cast(uint32_t, lo2), __builtin_bit_cast(uint32_t, hi2)};
-          }
-        } else {
-          float* to = mine_out + of * stride_of_partial<DP>();
-          *reinterpret_cast<f4*>(to + d) = x;
-          if (d == 0) to[DP] = top, to[DP + 1] = total;
-        }
-      }
-      __syncthreads();
-    }
-    if (pieces == 1) continue;
-
-    // ---- the pieces of these rows: the workgroup that comes last joins them
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) arrived = __hip_atomic_fetch_add(&a.counters[set], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    const bool last = arrived == (uint32_t)pieces - 1;
-    __syncthreads();
-    if (!last) continue;
-    __threadfence();
-    if (tid == 0) __hip_atomic_store(&a.counters[set], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const float* const all = a.partial + (int64_t)(slot - piece) * kRows * stride_of_partial<DP>();
-    constexpr int kPiece = kRows * stride_of_partial<DP>();
-    for (int e = tid; e < kRows * (DP / 4); e += kThreads) {
-      const int of = e / (DP / 4), d = e % (DP / 4) * 4;
-      if (of >= rows || d >= a.dim) continue;
-      const float* from = all + of * stride_of_partial<DP>();
-      float top = -INFINITY, total = 0.f;
-#pragma unroll 4
-      for (int c = 0; c < pieces; ++c) top = fmaxf(top, from[(int64_t)c * kPiece + DP]);
-      f4 x{0, 0, 0, 0};
-#pragma unroll 4
-      for (int c = 0; c < pieces; ++c) {
-        const float* p = from + (int64_t)c * kPiece;
-        const float w = p[DP] == -INFINITY ? 0.f : exp2f(p[DP] - top), lc = p[DP + 1];
-        const f4 xc = *reinterpret_cast<const f4*>(p + d);
-        total += p[DP] == -INFINITY ? lc : lc * w;
-        x += xc * w;
-      }
-      const int id = row0 + of, tok = id / a.group;
-      const int64_t to = (q.first + tok) * a.out_stride + (int64_t)(head * a.group + id - tok * a.group) * a.dim + d;
-      const f4 o = total == 0.f ? f4{0, 0, 0, 0} : x / total;
-      if constexpr (FLOAT) {
-        *reinterpret_cast<f4*>(static_cast<float*>(a.out) + to) = o;
+        for (int part = 0; part < kParts; ++part) rows.add_odd_values(part, value[part], p);
       } else {
-        const typename Half<CT>::v2 lo2{(CT)o[0], (CT)o[1]}, hi2{(CT)o[2], (CT)o[3]};
-        *reinterpret_cast<u2*>(static_cast<uint16_t*>(a.out) + to) = u2{__builtin_bit_cast(uint32_t, lo2), __builtin_bit_cast(uint32_t, hi2)};
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) rows.add_values(part, value[part], p);
       }
     }
+
+    // ---- the four wavefronts
+    if (g == 0) row_m[wave][n] = rows.maximum(), row_l[wave][n] = rows.sum[0];
+    __syncthreads();
+    const float back = behind(rows.maximum(), fmaxf(fmaxf(row_m[0][n], row_m[1][n]), fmaxf(row_m[2][n], row_m[3][n])));
+#pragma unroll
+    for (int part = 0; part < kParts; ++part)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < kEach; j += 4)
+          *reinterpret_cast<f4*>(&joined[wave][n][part * 16 * kEach + kEach * (4 * g + i) + j]) = rows.four(part, i, j) * back;
+    __syncthreads();
+    for (int e = tid; e < u.rows * (DP / 4); e += kThreads) {
+      const int in = e / (DP / 4), d = e % (DP / 4) * 4;
+      if (d >= a.dim) continue;
+      const f4 x = (*reinterpret_cast<const f4*>(&joined[0][in][d]) + *reinterpret_cast<const f4*>(&joined[1][in][d])) +
+                   (*reinterpret_cast<const f4*>(&joined[2][in][d]) + *reinterpret_cast<const f4*>(&joined[3][in][d]));
+      const float top = fmaxf(fmaxf(row_m[0][in], row_m[1][in]), fmaxf(row_m[2][in], row_m[3][in]));
+      float total = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) total += row_m[w][in] == -INFINITY ? row_l[w][in] : row_l[w][in] * exp2f(row_m[w][in] - top);
+      if (u.pieces == 1) {
+        store<CT, FLOAT>(a, u, in, d, x, total);
+      } else {
+        float* to = Partial<DP, kRows>::row(a, u.slot, in);
+        write_through(to + d, x);
+        if (d == 0) write_through(to + DP, top, total);
+      }
+    }
+    if (u.pieces > 1) join<CT, FLOAT, DP, kRows, kThreads>(a, u, tid, arrived);
+    __syncthreads();
+  }
+}
+
+// ---- many rows: the wavefronts share the positions ----------------------------------------------------------
+// A tile is fetched by all wavefronts, a share each, as the 16 bytes that every lane will want of it (keys: fragment (h, k) of
+// the lane; values: one position's eight dimensions), lies in LDS in that order, a kilobyte per fragment without bank conflicts,
+// and is read by all of them.  Tile t is computed from one buffer while t + 1 goes from registers into the other and t + 2
+// is on its way into the registers.
+template <typename CT, bool FLOAT, int DP, int WAVES, bool FULL>
+__global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend_shared(Args a) {
+  typedef Rows<CT, FLOAT, DP> R;
+  constexpr int kSteps = R::kSteps, kEach = R::kEach, kParts = R::kParts, kTerms = R::kTerms;
+  constexpr int kRows = 16 * WAVES;
+  constexpr int kKeys = 2 * kSteps, kValues = DP == 64 ? 4 : 8 * kParts;                          // fragments of a tile
+  constexpr int kFragments = kKeys + kValues, kMine = (kFragments + WAVES - 1) / WAVES;            // that a wavefront fetches
+  static_assert(kFragments % WAVES == 0);
+  __shared__ __align__(16) u4 stage[2][kFragments][64];
+  __shared__ uint32_t arrived;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Plan<kRows> plan(a, threadIdx.x & 63);
+  // The wavefronts of the first half fetch keys, the others values (there are as many of both).
+  constexpr int kHalf = WAVES / 2;
+  const bool keys = wave < kHalf;
+  const int fragment0 = (keys ? wave : wave - kHalf) * kMine;
+  // Fragment f of the keys: step f % kSteps of the 16 keys f / kSteps; of the values: part f % kParts of position f / kParts of the
+  // lane's eight (heads of up to 64: positions 2 f and 2 f + 1, half a row of lanes each).
+
+  for (int64_t unit = first_unit(); unit < plan.units; unit += gridDim.x) {
+    const int tid = hidden(threadIdx.x), lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const Unit u = plan.find(a, unit);
+    const int at = keys ? 8 * (n >> 2) : 8 * g;  // eight positions that lie on one page
+    auto position = [&](int f) { return keys ? (n & 3) + 4 * (f / kSteps) : kEach == 8 ? f / kParts : 2 * f + (n >> 3); };
+    auto dimension = [&](int f) { return within<FULL>(a, keys ? 32 * (f % kSteps) + 8 * g : kEach == 8 ? 128 * (f % kParts) + 8 * n : 8 * (n & 7), 8); };
+    R rows;
+    u4 query[kSteps][kTerms];
+    rows.begin(a, u, 16 * wave, n, g, query);
+    const bool idle = 16 * wave >= u.rows;  // no rows: fetches only
+
+    const int last_page = max(u.q.held - 1, 0) >> a.log2_page, in_page = (1 << a.log2_page) - 1;
+    const int32_t* table = a.table + (int64_t)u.r * a.max_pages;
+    const uint16_t* const cache = (keys ? a.cache_k : a.cache_v) + (int64_t)u.head * a.head_stride;
+    const void* const fresh = keys ? a.k : a.v;
+    const uint32_t lane_part = (at & in_page) * a.token_stride;
+    const int end = u.tile1;
+    auto page = [&](int tile, int at) { return table[min((min(tile, u.cached) * kTile + at) >> a.log2_page, last_page)]; };
+    Eight<CT, FLOAT> mine[kMine];
+    bool is_fresh = false;  // what is in `mine` are activations
+    auto fetch = [&](int tile, int page) {
+      is_fresh = tile >= u.cached;
+      if (!is_fresh) {
+        const uint16_t* p = cache + (int64_t)((tile * kTile) & in_page) * a.token_stride + (uint64_t)((uint32_t)page < (uint32_t)a.pages ? (uint32_t)page : 0u) * a.page_stride + lane_part;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) mine[i].raw[0] = *reinterpret_cast<const u4*>(p + position(fragment0 + i) * a.token_stride + dimension(fragment0 + i));
+      } else {
+        const int j0 = (tile - u.cached) * kTile + at;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+          mine[i].load(fresh, (u.q.first + min(j0 + position(fragment0 + i), u.q.fresh - 1)) * a.kv_stride + (int64_t)u.head * a.dim + dimension(fragment0 + i));
+      }
+    };
+    auto put = [&](int buffer) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) stage[buffer][(keys ? 0 : kKeys) + fragment0 + i][lane] = is_fresh ? mine[i].rounded() : mine[i].raw[0];
+    };
+    // the values of part `part`, as R takes them
+    auto read_values = [&](int buffer, int part, uint32_t (&value)[8][kEach / 2]) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        if constexpr (kEach == 8) {
+          const u4 x = stage[buffer][kKeys + t * kParts + part][lane];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) value[t][j] = x[j];
+        } else {
+          const u2 x = reinterpret_cast<const u2*>(&stage[buffer][kKeys + t / 2][16 * g + (t % 2) * 8 + (n >> 1)])[n & 1];
+          value[t][0] = x[0], value[t][1] = x[1];
+        }
+      }
+    };
+
+    // pages of the tile that is fetched next, and of the value positions of the tiles at hand (which of them are there?)
+    int my_page = page(u.tile0, at), my_next = page(min(u.tile0 + 1, end - 1), at);
+    int there_0 = page(u.tile0, 8 * g), there_1 = page(min(u.tile0 + 1, end - 1), 8 * g), there_2 = page(min(u.tile0 + 2, end - 1), 8 * g);
+    fetch(u.tile0, my_page);
+    put(u.tile0 & 1);
+    my_page = my_next, my_next = page(min(u.tile0 + 2, end - 1), at);
+    fetch(min(u.tile0 + 1, end - 1), my_page);
+    __syncthreads();
+    for (int tile = u.tile0; tile < end; ++tile) {
+      const int buffer = tile & 1;
+      put(buffer ^ 1);
+      my_page = my_next, my_next = page(min(tile + 3, end - 1), at);
+      const int there_3 = page(min(tile + 3, end - 1), 8 * g);
+      fetch(min(tile + 2, end - 1), my_page);
+      if (!idle) {
+        f4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) R::add_score(stage[buffer][k][lane], stage[buffer][kSteps + k][lane], query[k], x);
+        float s[8];
+        u4 p[kTerms];
+        rows.exponents(x, s);
+        const bool is_new = tile >= u.cached;
+        int seen, there;
+        if (!is_new) {
+          seen = there = (uint32_t)there_0 < (uint32_t)a.pages ? eight_bits(u.q.held - tile * kTile - 8 * g) : 0;
+        } else {
+          const int j0 = (tile - u.cached) * kTile + 8 * g;
+          there = eight_bits(u.q.fresh - j0);
+          seen = rows.seen_new(a, u, 16 * wave + n < u.rows, j0);
+        }
+        const bool partly = __ballot(seen != 255) != 0;
+        if (partly) {
+#pragma unroll
+          for (int t = 0; t < 8; ++t) s[t] = seen >> t & 1 ? s[t] : -INFINITY;
+        }
+        rows.weigh(s, p);
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+          bool odd = false;
+          uint32_t value[8][kEach / 2];
+          read_values(buffer, part, value);
+          if (partly) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+#pragma unroll
+              for (int j = 0; j < kEach / 2; ++j) value[t][j] = there >> t & 1 ? value[t][j] : 0u;
+            if (is_new) odd = R::has_odd(value);
+          }
+          if (__ballot(odd)) rows.add_odd_values(part, value, p);
+          else rows.add_values(part, value, p);
+        }
+      }
+      there_0 = there_1, there_1 = there_2, there_2 = there_3;
+      __syncthreads();
+    }
+
+    const int in = 16 * wave + n;
+    if (in < u.rows) {
+      float* const to = Partial<DP, kRows>::row(a, u.slot, in);
+      if (u.pieces > 1 && g == 0) write_through(to + DP, rows.maximum(), rows.sum[0]);
+#pragma unroll
+      for (int part = 0; part < kParts; ++part)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < kEach; j += 4) {
+            const int d = part * 16 * kEach + kEach * (4 * g + i) + j;
+            if (!FULL && d >= a.dim) continue;
+            if (u.pieces == 1) store<CT, FLOAT>(a, u, in, d, rows.four(part, i, j), rows.sum[0]);
+            else write_through(to + d, rows.four(part, i, j));
+          }
+    }
+    if (u.pieces > 1) join<CT, FLOAT, DP, kRows, 64 * WAVES>(a, u, tid, arrived);
   }
 }
 
@@ -635,35 +871,37 @@ const char* fault_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads
 // The kernel for a call, and how it is launched.
 struct Shape {
   int dims;         // head_dim, padded
-  int row_tiles;    // tiles of 16 rows that a wavefront carries
-  int target;       // pieces of work that are aimed at
+  int waves;        // of a workgroup of attend_shared, 0: attend_split
+  int rows;         // of a workgroup
+  int target;       // pieces of work that are aimed at: workgroups that the chip runs at once
   int64_t counters_bytes, bytes;  // of the workspace
 };
 
-// `floats`: the activations are float, whose queries and weights take several operands each
 Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool floats) {
   Shape s;
   s.dims = cache->head_dim <= 64 ? 64 : cache->head_dim <= 128 ? 128 : 256;
   const int64_t rows = (int64_t)step->max_new * (heads / cache->kv_heads);
-  s.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  if (s.dims == 256 && s.row_tiles > 2) s.row_tiles = 2;
-  if (floats && s.dims == 256) s.row_tiles = 1;
-  if (floats && s.dims == 128 && s.row_tiles > 2) s.row_tiles = 2;
-  s.target = 512;
+  // (keys and values of 256 dimensions do not fit in the registers beside a result)
+  s.waves = rows <= 16 && s.dims < 256 ? 0 : rows <= 64 || s.dims == 256 || (floats && s.dims == 128) ? 4 : 8;
+  s.rows = s.waves ? 16 * s.waves : 16;
+  s.target = s.waves == 8 || (s.waves && (floats || s.dims == 256)) ? 256 : 512;
   s.counters_bytes = (int64_t)s.target * 4;
-  s.bytes = s.counters_bytes + (int64_t)2 * s.target * 16 * s.row_tiles * (s.dims + 4) * 4;
+  s.bytes = s.counters_bytes + (int64_t)(2 * s.target + 1) * s.rows * (s.dims + 4) * 4;
   return s;
 }
 
-template <typename CT, bool FLOAT> void (*kernel_of(const Shape& s))(Args) {
-  if (s.dims == 64) return s.row_tiles == 1 ? attend_kernel<CT, FLOAT, 64, 1> : s.row_tiles == 2 ? attend_kernel<CT, FLOAT, 64, 2> : attend_kernel<CT, FLOAT, 64, 4>;
-  if constexpr (FLOAT) {
-    if (s.dims == 128) return s.row_tiles == 1 ? attend_kernel<CT, FLOAT, 128, 1> : attend_kernel<CT, FLOAT, 128, 2>;
-    return attend_kernel<CT, FLOAT, 256, 1>;
-  } else {
-    if (s.dims == 128) return s.row_tiles == 1 ? attend_kernel<CT, FLOAT, 128, 1> : s.row_tiles == 2 ? attend_kernel<CT, FLOAT, 128, 2> : attend_kernel<CT, FLOAT, 128, 4>;
-    return s.row_tiles == 1 ? attend_kernel<CT, FLOAT, 256, 1> : attend_kernel<CT, FLOAT, 256, 2>;
+template <typename CT, bool FLOAT, bool FULL> void (*kernel_of(const Shape& s))(Args) {
+  if (s.dims == 64) return !s.waves ? attend_split<CT, FLOAT, 64, FULL> : s.waves == 4 ? attend_shared<CT, FLOAT, 64, 4, FULL> : attend_shared<CT, FLOAT, 64, 8, FULL>;
+  if (s.dims == 256) return attend_shared<CT, FLOAT, 256, 4, FULL>;
+  if constexpr (!FLOAT) {
+    if (s.waves == 8) return attend_shared<CT, FLOAT, 128, 8, FULL>;
   }
+  return s.waves ? attend_shared<CT, FLOAT, 128, 4, FULL> : attend_split<CT, FLOAT, 128, FULL>;
+}
+
+template <typename CT> void (*kernel_of(const Shape& s, bool floats, bool full))(Args) {
+  if (floats) return full ? kernel_of<CT, true, true>(s) : kernel_of<CT, true, false>(s);
+  return full ? kernel_of<CT, false, true>(s) : kernel_of<CT, false, false>(s);
 }
 
 }  // namespace
@@ -693,17 +931,19 @@ int rsr_tree_attention(const rsr_cache_t* cache, const rsr_step_t* step, const v
   if (!fault && (!workspace || !rsr_internal::aligned(workspace, 256) || workspace_bytes < s.bytes))
     fault = "the workspace is missing, too small or not 256-byte aligned";
   if (fault) return set_error(RSR_ERR_INVALID_ARGUMENT, fault);
+  const int group = heads / cache->kv_heads;
   const Args a{q, k, v, out, static_cast<const uint16_t*>(cache->k), static_cast<const uint16_t*>(cache->v), step->table, step->held, step->start, step->mask,
                static_cast<uint32_t*>(workspace), reinterpret_cast<float*>(static_cast<char*>(workspace) + s.counters_bytes),
-               q_stride, kv_stride, out_stride, cache->page_stride, cache->head_stride, cache->token_stride, step->requests, step->tokens, step->max_new,
-               step->max_pages, rsr_internal::log2_of(cache->page_size), cache->pages, cache->kv_heads, cache->head_dim, heads / cache->kv_heads, s.target, scale};
-  auto kern = cache->dtype == RSR_F16 ? (floats ? kernel_of<_Float16, true>(s) : kernel_of<_Float16, false>(s))
-                                      : (floats ? kernel_of<__bf16, true>(s) : kernel_of<__bf16, false>(s));
+               q_stride, kv_stride, out_stride, cache->head_stride, (uint32_t)cache->page_stride, (uint32_t)cache->token_stride, step->requests, step->tokens,
+               step->max_new, step->max_pages, rsr_internal::log2_of(cache->page_size), cache->pages, cache->kv_heads, cache->head_dim, group,
+               group == 1 ? 0u : (uint32_t)(((uint64_t(1) << 32) + group - 1) / group), 1.0 / s.target, scale};
+  const bool full = cache->head_dim == s.dims;
+  auto kern = cache->dtype == RSR_F16 ? kernel_of<_Float16>(s, floats, full) : kernel_of<__bf16>(s, floats, full);
   // no more workgroups than there can be pieces
-  const int64_t blocks = ((int64_t)step->max_new * (heads / cache->kv_heads) + 16 * s.row_tiles - 1) / (16 * s.row_tiles);
+  const int64_t blocks = ((int64_t)step->max_new * group + s.rows - 1) / s.rows;
   const int64_t tiles = (((int64_t)step->max_pages * cache->page_size) + kTile - 1) / kTile + (step->max_new + kTile - 1) / kTile;
   const int64_t units = step->requests * (int64_t)cache->kv_heads * blocks * ((tiles + kLeastTiles - 1) / kLeastTiles);
-  hipLaunchKernelGGL(kern, dim3((unsigned)std::min(units, (int64_t)s.target)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)std::min(units, (int64_t)s.target)), dim3(s.waves ? 64 * s.waves : kThreads), 0, static_cast<hipStream_t>(stream), a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(RSR_ERR_HIP, std::string("rsr_tree_attention: ") + hipGetErrorString(e));
   return RSR_OK;

@@ -25,6 +25,7 @@ inline const char* fault_of(const rsr_cache_t* c) {
   if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8) return "head_dim must be a multiple of 8 in 8..256";
   if ((c->page_stride | c->head_stride | c->token_stride) & 7) return "the cache's strides must be multiples of 8";
   if (c->page_stride < 0 || c->head_stride < 0 || c->token_stride < 0) return "the cache's strides must not be negative";
+  if (c->page_stride >> 31 || c->token_stride >> 24) return "the cache's page_stride must be below 2^31, its token_stride below 2^24";
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) return "the cache must be 16-byte aligned";
   return nullptr;
 }
