@@ -177,6 +177,8 @@ def _host_matrix(A) -> np.ndarray:
 
 
 def _addr(x) -> int:
+    if type(x) is int:
+        return x
     if x is None:
         return 0
     if hasattr(x, "data_ptr"):
@@ -327,33 +329,42 @@ class RsrStep(ctypes.Structure):
     ]
 
 
+_dtypes: dict = {}  # torch's types to the header's (torch is imported by load(), not here)
+
+
 def _dtype(x) -> int:
-    name = str(x.dtype)
-    if name not in _DTYPES:
-        raise TypeError(f"float32, float16 or bfloat16 wanted, not {name}")
-    return _DTYPES[name]
+    code = _dtypes.get(x.dtype)
+    if code is None:
+        import torch
+
+        _dtypes.update({torch.float32: RSR_F32, torch.float16: RSR_F16, torch.bfloat16: RSR_BF16})
+        code = _dtypes.get(x.dtype)
+        if code is None:
+            raise TypeError(f"float32, float16 or bfloat16 wanted, not {x.dtype}")
+    return code
 
 
-_DTYPES = {"torch.float32": RSR_F32, "torch.float16": RSR_F16, "torch.bfloat16": RSR_BF16}
+def _rows(x, rows: int, width: int) -> int:
+    """Stride of a 2-D tensor of `rows` rows of `width` elements that lie side by side."""
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 2 or shape[0] != rows or shape[1] != width or (stride[1] != 1 and width > 1):
+        raise ValueError(f"a 2-D tensor with {rows} contiguous rows of {width} elements is wanted")
+    return stride[0] if rows > 1 else max(stride[0], width)
 
 
-def _rows(x, like=None) -> int:
-    """Stride of a 2-D tensor of rows whose elements lie side by side."""
-    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
-        raise ValueError("a 2-D tensor with contiguous rows is wanted")
-    if like is not None and (x.dtype != like.dtype or x.shape != like.shape or (x.stride(0) != like.stride(0) and x.shape[0] > 1)):
-        raise ValueError("keys and values must have the same type, shape and stride")
-    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1])
+_WHOLE: dict = {32: {"torch.int32"}, 64: {"torch.int64", "torch.uint64"}}  # names, and then the types themselves
 
 
-def _whole(x, dtypes, count=None):
-    """A contiguous tensor of one of the given types, with at least `count` elements."""
-    if str(x.dtype) not in dtypes or not x.is_contiguous() or (count is not None and x.numel() < count):
-        raise ValueError(f"a contiguous tensor of {dtypes[0]}" + (f" with {count} elements" if count is not None else "") + " is wanted")
-    return x
-
-
-_I32, _U64 = ("torch.int32",), ("torch.uint64", "torch.int64")
+def _whole(x, bits: int, count: int) -> int:
+    """Address of a contiguous tensor of whole numbers of so many bits, with at least `count` elements."""
+    dtype, known = x.dtype, _WHOLE[bits]
+    if dtype not in known:
+        if str(dtype) not in known:
+            raise ValueError(f"a tensor of {bits}-bit integers is wanted, not {dtype}")
+        known.add(dtype)
+    if x.numel() < count or not x.is_contiguous():
+        raise ValueError(f"a contiguous tensor of {count} integers is wanted")
+    return x.data_ptr()
 
 
 def make_cache(k, v) -> RsrCache:
@@ -368,12 +379,10 @@ def make_step(table, held, start, tokens: int, max_new: int, mask=None) -> RsrSt
     """rsr_step_t of device tensors: ``table [requests][max_pages]``, ``held [requests]``, ``start [requests+1]`` (int32) and
     ``mask [tokens]`` (64 bits) or None.  Keep the tensors alive; what they hold may change between calls."""
     requests = held.numel()
-    _whole(table, _I32), _whole(held, _I32), _whole(start, _I32, requests + 1)
     if table.dim() != 2 or table.shape[0] != requests:
         raise ValueError("the table has a row for each request")
-    if mask is not None:
-        _whole(mask, _U64, tokens)
-    return RsrStep(table.data_ptr(), held.data_ptr(), start.data_ptr(), _addr(mask), requests, int(tokens), int(max_new), table.shape[1])
+    return RsrStep(_whole(table, 32, 0), _whole(held, 32, 0), _whole(start, 32, requests + 1), None if mask is None else _whole(mask, 64, tokens),
+                   requests, int(tokens), int(max_new), table.shape[1])
 
 
 def rsr_tree_attention_workspace(cache: RsrCache, step: RsrStep, heads: int) -> int:
@@ -387,42 +396,50 @@ def rsr_tree_attention_workspace(cache: RsrCache, step: RsrStep, heads: int) -> 
 def rsr_tree_attention(cache: RsrCache, step: RsrStep, q, k, v, out, heads: int, scale: float, workspace, stream=None) -> None:
     """``q``, ``out``: device ``[tokens][heads * head_dim]``; ``k``, ``v``: ``[tokens][kv_heads * head_dim]`` (slices of wider rows
     will do), all float32 or of the cache's type; ``workspace``: device bytes that were zero at first."""
-    width, kv_width = heads * cache.head_dim, cache.kv_heads * cache.head_dim
-    if q.shape != (step.tokens, width) or out.shape != q.shape or out.dtype != q.dtype or k.shape != (step.tokens, kv_width) or k.dtype != q.dtype:
-        raise ValueError("q and out are [tokens][heads * head_dim], k and v [tokens][kv_heads * head_dim], all of one type")
-    _check(load().rsr_tree_attention(ctypes.addressof(cache), ctypes.addressof(step), q.data_ptr(), _rows(q), k.data_ptr(), v.data_ptr(), _rows(k, v),
-                                     out.data_ptr(), _rows(out), _dtype(q), heads, scale, workspace.data_ptr(),
-                                     workspace.numel() * workspace.element_size(), _addr(stream)))
+    dtype, tokens, width, kv_width = q.dtype, step.tokens, heads * cache.head_dim, cache.kv_heads * cache.head_dim
+    kv_stride = _rows(k, tokens, kv_width)
+    if out.dtype != dtype or k.dtype != dtype or v.dtype != dtype or _rows(v, tokens, kv_width) != kv_stride:
+        raise ValueError("q, k, v and out must have one type, k and v one stride")
+    code = (_lib or load()).rsr_tree_attention(
+        ctypes.addressof(cache), ctypes.addressof(step), q.data_ptr(), _rows(q, tokens, width), k.data_ptr(), v.data_ptr(), kv_stride,
+        out.data_ptr(), _rows(out, tokens, width), _dtypes.get(dtype) or _dtype(q), heads, scale, workspace.data_ptr(), workspace.nbytes, _addr(stream))
+    if code:
+        _check(code)
 
 
 def rsr_cache_slots(held, add, table, page_size: int, free_pages, free_count, slots, start, now, free_left, stream=None) -> None:
     """Pages and slots for the next ``add[r]`` tokens of every request; all device int32, see the header."""
     requests = held.numel()
-    for x, count in ((held, None), (add, requests), (table, None), (free_pages, None), (free_count, 1), (slots, None), (start, requests + 1), (now, requests), (free_left, 1)):
-        _whole(x, _I32, count)
     if table.dim() != 2 or table.shape[0] != requests:
         raise ValueError("the table has a row for each request")
-    _check(load().rsr_cache_slots(held.data_ptr(), add.data_ptr(), requests, table.data_ptr(), table.shape[1], int(page_size), free_pages.data_ptr(),
-                                  free_count.data_ptr(), free_left.data_ptr(), slots.data_ptr(), slots.numel(), start.data_ptr(), now.data_ptr(),
-                                  _addr(stream)))
+    code = (_lib or load()).rsr_cache_slots(
+        _whole(held, 32, 0), _whole(add, 32, requests), requests, _whole(table, 32, 0), table.shape[1], int(page_size), _whole(free_pages, 32, 0),
+        _whole(free_count, 32, 1), _whole(free_left, 32, 1), _whole(slots, 32, 0), slots.numel(), _whole(start, 32, requests + 1),
+        _whole(now, 32, requests), _addr(stream))
+    if code:
+        _check(code)
 
 
 def rsr_cache_append(cache: RsrCache, k, v, slots, rows=None, stream=None) -> None:
     """Row ``rows[i]`` (None: row ``i``) of ``k`` and ``v`` (``[nrows][kv_heads * head_dim]``) goes to ``slots[i]``."""
-    if k.dim() != 2 or k.shape[1] != cache.kv_heads * cache.head_dim:
-        raise ValueError("k and v are [rows][kv_heads * head_dim]")
-    _whole(slots, _I32)
-    if rows is not None:
-        _whole(rows, _I32, slots.numel())
-    _check(load().rsr_cache_append(ctypes.addressof(cache), k.data_ptr(), v.data_ptr(), _rows(k, v), k.shape[0], _dtype(k), _addr(rows),
-                                   slots.data_ptr(), slots.numel(), _addr(stream)))
+    count, nrows, width = slots.numel(), k.shape[0], cache.kv_heads * cache.head_dim
+    stride = _rows(k, nrows, width)
+    if k.dtype != v.dtype or _rows(v, nrows, width) != stride:
+        raise ValueError("keys and values must have one type and stride")
+    code = (_lib or load()).rsr_cache_append(
+        ctypes.addressof(cache), k.data_ptr(), v.data_ptr(), stride, nrows, _dtypes.get(k.dtype) or _dtype(k),
+        None if rows is None else _whole(rows, 32, count), _whole(slots, 32, 0), count, _addr(stream))
+    if code:
+        _check(code)
 
 
 def rsr_tree_masks(parent, start, mask, depth, stream=None) -> None:
     """``mask`` (64 bits) and ``depth`` (int32) of the drafted tokens from their ``parent`` (int32, -1: hangs on the cache)."""
     tokens, requests = parent.numel(), start.numel() - 1
-    _whole(parent, _I32), _whole(start, _I32), _whole(mask, _U64, tokens), _whole(depth, _I32, tokens)
-    _check(load().rsr_tree_masks(parent.data_ptr(), start.data_ptr(), requests, tokens, mask.data_ptr(), depth.data_ptr(), _addr(stream)))
+    code = (_lib or load()).rsr_tree_masks(_whole(parent, 32, 0), _whole(start, 32, 1), requests, tokens, _whole(mask, 64, tokens),
+                                           _whole(depth, 32, tokens), _addr(stream))
+    if code:
+        _check(code)
 
 
 class RsrJob(ctypes.Structure):

@@ -37,6 +37,7 @@ constexpr int kLeastTiles = 4;   // of a piece
 constexpr float kBias = 7.f;     // weights are 2^(s - m + 7): as float16 they keep their bits down to 2^-21 of the largest
 constexpr float kLimit = 15.f;   // m follows the maximum when a weight would pass 2^15, so that it seldom does
 
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
@@ -473,34 +474,68 @@ __device__ inline float behind(float m, float top) { return m == -INFINITY ? 0.f
 
 // The workgroup that comes last joins the pieces of its rows, in their order.  What the others wrote is there: every wavefront
 // waits until its writes, which go through all caches, are done, then the workgroup counts itself; the last one drops what its own
-// caches may hold before it reads.
-template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inline void join(const Args& a, const Unit& u, int tid, uint32_t& arrived) {
+// caches may hold before it reads.  Bound by the latency of these reads: the lanes share out the pieces of a row for its maximum and
+// sum, then the pieces of its values as far as the values do not fill the lanes, and many reads are under way at once.
+template <int ROWS, int THREADS> struct Joint {
+  static constexpr int kShares = THREADS / ROWS;
+  float m[kShares][ROWS], l[kShares][ROWS];
+  f4 part[THREADS];
+  uint32_t arrived;
+};
+
+template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inline void join(const Args& a, const Unit& u, Joint<ROWS, THREADS>& lds) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (tid == 0) arrived = __hip_atomic_fetch_add(&a.counters[u.set], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const int tid = hidden(threadIdx.x);
+  if (tid == 0) lds.arrived = __hip_atomic_fetch_add(&a.counters[u.set], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
-  const bool last = arrived == (uint32_t)u.pieces - 1;
-  __syncthreads();
-  if (!last) return;
+  if (lds.arrived != (uint32_t)u.pieces - 1) return;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   if (tid == 0) __hip_atomic_store(&a.counters[u.set], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   typedef Partial<DP, ROWS> P;
-  for (int e = tid; e < u.rows * (DP / 4); e += THREADS) {
-    const int in = e / (DP / 4), d = e % (DP / 4) * 4;
-    if (d >= a.dim) continue;
-    const float* from = P::row(a, u.slot - u.piece, in);
-    float top = -INFINITY, total = 0.f;
-#pragma unroll 8
-    for (int c = 0; c < u.pieces; ++c) top = fmaxf(top, from[c * P::kPiece + DP]);
-    f4 x{0, 0, 0, 0};
-#pragma unroll 8
-    for (int c = 0; c < u.pieces; ++c) {
-      const float* p = from + c * P::kPiece;
-      const float w = behind(p[DP], top);
-      total += p[DP] == -INFINITY ? p[DP + 1] : p[DP + 1] * w;  // (without a maximum: 0, or NaN)
-      x += *reinterpret_cast<const f4*>(p + d) * w;
+  const float* const first = P::row(a, u.slot - u.piece, 0);
+  {
+    const int in = tid % ROWS, share = tid / ROWS;
+    float m = -INFINITY, l = 0.f;
+    if (in < u.rows) {
+#pragma unroll 4
+      for (int c = share; c < u.pieces; c += Joint<ROWS, THREADS>::kShares) {
+        const f2 ml = *reinterpret_cast<const f2*>(first + (int64_t)c * P::kPiece + in * P::kRow + DP);
+        const float mc = ml[0], lc = ml[1], top = fmaxf(m, mc);
+        // (without a maximum: 0, or NaN)
+        l = (m == -INFINITY ? l : l * exp2f(m - top)) + (mc == -INFINITY ? lc : lc * exp2f(mc - top));
+        m = top;
+      }
     }
-    store<CT, FLOAT>(a, u, in, d, x, total);
+    lds.m[share][in] = m, lds.l[share][in] = l;
+  }
+  __syncthreads();
+  const int items = u.rows * (DP / 4), shares = items < THREADS ? THREADS / items : 1;
+  for (int e0 = 0; e0 < items; e0 += THREADS) {
+    const int e = e0 + tid % (shares > 1 ? items : THREADS), share = shares > 1 ? tid / items : 0;
+    const int in = e / (DP / 4), d = e % (DP / 4) * 4;
+    const bool there = e < items && d < a.dim && share < shares;
+    f4 x{0, 0, 0, 0};
+    float top = -INFINITY, total = 0.f;
+    if (there) {
+#pragma unroll
+      for (int w = 0; w < Joint<ROWS, THREADS>::kShares; ++w) top = fmaxf(top, lds.m[w][in]);
+#pragma unroll
+      for (int w = 0; w < Joint<ROWS, THREADS>::kShares; ++w) total += lds.m[w][in] == -INFINITY ? lds.l[w][in] : lds.l[w][in] * exp2f(lds.m[w][in] - top);
+      const float* const from = first + in * P::kRow;
+#pragma unroll 8
+      for (int c = share; c < u.pieces; c += shares) {
+        const float* const p = from + (int64_t)c * P::kPiece;
+        x += *reinterpret_cast<const f4*>(p + d) * behind(p[DP], top);
+      }
+    }
+    if (shares > 1) {
+      lds.part[tid] = x;
+      __syncthreads();
+      if (tid >= items) continue;
+      for (int w = 1; w < shares; ++w) x += lds.part[w * items + tid];
+    }
+    if (there) store<CT, FLOAT>(a, u, in, d, x, total);
   }
 }
 
@@ -513,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
   __shared__ float row_m[kWaves][kRows], row_l[kWaves][kRows];
   __shared__ __align__(16) float joined[kWaves][16][kLine];
   __shared__ __align__(16) u4 queries[FLOAT ? kSteps : 1][FLOAT ? kTerms : 1][64];  // the operands of floats fill too many registers
-  __shared__ uint32_t arrived;
+  __shared__ Joint<kRows, kThreads> joint;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Plan<kRows> plan(a, threadIdx.x & 63);
 
@@ -698,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
         if (d == 0) write_through(to + DP, top, total);
       }
     }
-    if (u.pieces > 1) join<CT, FLOAT, DP, kRows, kThreads>(a, u, tid, arrived);
+    if (u.pieces > 1) join<CT, FLOAT, DP, kRows, kThreads>(a, u, joint);
     __syncthreads();
   }
 }
@@ -717,7 +752,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
   constexpr int kFragments = kKeys + kValues, kMine = (kFragments + WAVES - 1) / WAVES;            // that a wavefront fetches
   static_assert(kFragments % WAVES == 0);
   __shared__ __align__(16) u4 stage[2][kFragments][64];
-  __shared__ uint32_t arrived;
+  __shared__ Joint<kRows, 64 * WAVES> joint;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Plan<kRows> plan(a, threadIdx.x & 63);
   // The wavefronts of the first half fetch keys, the others values (there are as many of both).
@@ -851,7 +886,8 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
             else write_through(to + d, rows.four(part, i, j));
           }
     }
-    if (u.pieces > 1) join<CT, FLOAT, DP, kRows, 64 * WAVES>(a, u, tid, arrived);
+    if (u.pieces > 1) join<CT, FLOAT, DP, kRows, 64 * WAVES>(a, u, joint);
+    __syncthreads();
   }
 }
 
