@@ -205,7 +205,7 @@ template <int ROWS> struct Plan {
     } else {
       work = from_lane(work, 0);
     }
-    most = max((int)((double)work * a.per_target) + 1, kLeastTiles);
+    most = __builtin_amdgcn_readfirstlane(max((int)((double)work * a.per_target) + 1, kLeastTiles));
     int64_t mine = 0;
     uint64_t mine_cut = 0;
     if (run == 1) {
@@ -285,6 +285,7 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
   float base;    // taken off the exponents: m - kBias
   float limit;   // of an exponent: kLimit, and -infinity before the row has seen anything
   int token;
+  uint64_t mask;  // new tokens that the row sees
 
   // Queries of the 16 rows from `first` on: operand B of the scores, zeros behind the last dimension and the last row.
   __device__ void begin(const Args& a, const Unit& u, int first, int n, int g, u4 (&query)[kSteps][kTerms]) {
@@ -292,6 +293,8 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
     const bool there = in < u.rows;
     token = there ? token_of(a, row) : 0;
     const int64_t from = (u.q.first + token) * a.q_stride + (int64_t)(u.head * a.group + (there ? row - token * a.group : 0)) * a.dim;
+    mask = there && a.mask ? a.mask[u.q.first + token] : ~0ull;
+    if (!there) token = a.max_new;  // (a row that is not there sees all: it must not make a tile one that has to be masked)
     factor = a.scale * 1.44269504088896341f;
     base = 0.f, limit = -INFINITY;
     sum = f4{0, 0, 0, 0};
@@ -394,10 +397,8 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
   }
 
   // Which of eight new tokens from number j0 on the row sees, a bit each.
-  __device__ int seen_new(const Args& a, const Unit& u, bool row, int j0) const {
-    int bits = 255;
-    if (row) bits = a.mask ? (int)(a.mask[u.q.first + token] >> min(j0, 63)) & 255 : eight_bits(token + 1 - j0);
-    return bits & eight_bits(u.q.fresh - j0);
+  __device__ int seen_new(const Args& a, const Unit& u, int j0) const {
+    return (a.mask ? (int)(mask >> min(j0, 63)) & 255 : eight_bits(token + 1 - j0)) & eight_bits(u.q.fresh - j0);
   }
 
   // A value that is not finite must not reach the rows that do not see it (0 times infinity is NaN).  Does the lane hold one?
@@ -686,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
       float s[8];
       u4 p[kTerms];
       rows.exponents(x, s);
-      const int seen = rows.seen_new(a, u, n < u.rows, j0 + 8 * g);
+      const int seen = rows.seen_new(a, u, j0 + 8 * g);
       bool odd = false;
       if (__ballot(seen != 255)) {
 #pragma unroll
@@ -740,110 +741,142 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
 
 // ---- many rows: the wavefronts share the positions ----------------------------------------------------------
 // A tile is fetched by all wavefronts, a share each, as the 16 bytes that every lane will want of it (keys: fragment (h, k) of
-// the lane; values: one position's eight dimensions), lies in LDS in that order, a kilobyte per fragment without bank conflicts,
-// and is read by all of them.  Tile t is computed from one buffer while t + 1 goes from registers into the other and t + 2
-// is on its way into the registers.
+// the lane; values: one position's eight dimensions), straight into LDS, where it lies in that order, a kilobyte per fragment
+// without bank conflicts, and is read by all of them.  kAhead tiles are on their way while one is computed: the cache answers
+// after one to two microseconds, a tile's products take a third of that.
+constexpr int kWindow = 512;  // entries of a request's table in LDS
+
+// 16 bytes per lane from memory to the kilobyte of LDS at `to`.  The compiler does not know that LDS changes: wait_for_all_but waits
+// for it.  (Known to the compiler, every read of LDS would wait for all such loads.)
+__device__ inline void to_lds(const void* from, uint32_t to) {
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0" : "=&s"(m0) : "v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "memory");
+}
+// Until all but the last LOADS loads of the wavefront are done, and what it reads from and writes to LDS; then all wavefronts.
+template <int LOADS> __device__ inline void wait_for_all_but() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 template <typename CT, bool FLOAT, int DP, int WAVES, bool FULL>
 __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend_shared(Args a) {
   typedef Rows<CT, FLOAT, DP> R;
   constexpr int kSteps = R::kSteps, kEach = R::kEach, kParts = R::kParts, kTerms = R::kTerms;
   constexpr int kRows = 16 * WAVES;
-  constexpr int kKeys = 2 * kSteps, kValues = DP == 64 ? 4 : 8 * kParts;                          // fragments of a tile
-  constexpr int kFragments = kKeys + kValues, kMine = (kFragments + WAVES - 1) / WAVES;            // that a wavefront fetches
+  constexpr int kKeys = 2 * kSteps, kValues = DP == 64 ? 4 : 8 * kParts;   // fragments of a tile
+  constexpr int kFragments = kKeys + kValues, kMine = kFragments / WAVES;  // that a wavefront fetches
+  constexpr int kAhead = 3, kBuffers = kAhead + 1;
   static_assert(kFragments % WAVES == 0);
-  __shared__ __align__(16) u4 stage[2][kFragments][64];
-  __shared__ Joint<kRows, 64 * WAVES> joint;
+  struct Lds {
+    u4 stage[kBuffers][kFragments][64];
+    int32_t seen[kBuffers][4];  // which of eight positions there are
+    int32_t pages[kWindow];
+    Joint<kRows, 64 * WAVES> joint;
+  };
+  __shared__ __align__(1024) Lds lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Plan<kRows> plan(a, threadIdx.x & 63);
   // The wavefronts of the first half fetch keys, the others values (there are as many of both).
   constexpr int kHalf = WAVES / 2;
   const bool keys = wave < kHalf;
   const int fragment0 = (keys ? wave : wave - kHalf) * kMine;
-  // Fragment f of the keys: step f % kSteps of the 16 keys f / kSteps; of the values: part f % kParts of position f / kParts of the
-  // lane's eight (heads of up to 64: positions 2 f and 2 f + 1, half a row of lanes each).
 
   for (int64_t unit = first_unit(); unit < plan.units; unit += gridDim.x) {
     const int tid = hidden(threadIdx.x), lane = tid & 63, n = lane & 15, g = lane >> 4;
     const Unit u = plan.find(a, unit);
+    // Fragment f of the keys: step f % kSteps of the 16 keys f / kSteps; of the values: part f % kParts of position f / kParts of the
+    // lane's eight (heads of up to 64: positions 2 f and 2 f + 1, half a row of lanes each).
     const int at = keys ? 8 * (n >> 2) : 8 * g;  // eight positions that lie on one page
     auto position = [&](int f) { return keys ? (n & 3) + 4 * (f / kSteps) : kEach == 8 ? f / kParts : 2 * f + (n >> 3); };
     auto dimension = [&](int f) { return within<FULL>(a, keys ? 32 * (f % kSteps) + 8 * g : kEach == 8 ? 128 * (f % kParts) + 8 * n : 8 * (n & 7), 8); };
     R rows;
     u4 query[kSteps][kTerms];
     rows.begin(a, u, 16 * wave, n, g, query);
+    // (in registers now: a wait for these loads inside the loop would be one for all tiles that are on their way)
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+      for (int t = 0; t < kTerms; ++t) asm volatile("" : "+v"(query[k][t]));
+    asm volatile("" : "+v"(rows.mask));
     const bool idle = 16 * wave >= u.rows;  // no rows: fetches only
 
-    const int last_page = max(u.q.held - 1, 0) >> a.log2_page, in_page = (1 << a.log2_page) - 1;
+    const int last_page = max(u.q.held - 1, 0) >> a.log2_page, in_page = (1 << a.log2_page) - 1, end = u.tile1;
     const int32_t* table = a.table + (int64_t)u.r * a.max_pages;
     const uint16_t* const cache = (keys ? a.cache_k : a.cache_v) + (int64_t)u.head * a.head_stride;
     const void* const fresh = keys ? a.k : a.v;
     const uint32_t lane_part = (at & in_page) * a.token_stride;
-    const int end = u.tile1;
-    auto page = [&](int tile, int at) { return table[min((min(tile, u.cached) * kTile + at) >> a.log2_page, last_page)]; };
-    Eight<CT, FLOAT> mine[kMine];
-    bool is_fresh = false;  // what is in `mine` are activations
-    auto fetch = [&](int tile, int page) {
-      is_fresh = tile >= u.cached;
-      if (!is_fresh) {
-        const uint16_t* p = cache + (int64_t)((tile * kTile) & in_page) * a.token_stride + (uint64_t)((uint32_t)page < (uint32_t)a.pages ? (uint32_t)page : 0u) * a.page_stride + lane_part;
+    int window = (u.tile0 * kTile) >> a.log2_page;  // the entry that pages[0] holds
+    auto fill_window = [&] {
+      for (int i = tid; i < kWindow; i += 64 * WAVES) lds.pages[i] = table[min(window + i, last_page)];
+    };
+    const uint32_t stage_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) u4*)&lds.stage[0][keys ? fragment0 : kKeys + fragment0][0];
+    auto fetch = [&](int tile, int buffer) {
+      const uint32_t to = stage_at + buffer * (kFragments * 1024);
+      if (tile < u.cached) {
+        const int page = lds.pages[min((tile * kTile + at) >> a.log2_page, last_page) - window];
+        const bool there = (uint32_t)page < (uint32_t)a.pages;
+        const uint16_t* p = cache + (int64_t)((tile * kTile) & in_page) * a.token_stride + (uint64_t)(there ? (uint32_t)page : 0u) * a.page_stride + lane_part;
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) mine[i].raw[0] = *reinterpret_cast<const u4*>(p + position(fragment0 + i) * a.token_stride + dimension(fragment0 + i));
+        for (int i = 0; i < kMine; ++i) to_lds(p + position(fragment0 + i) * a.token_stride + dimension(fragment0 + i), to + i * 1024);
+        if (wave == WAVES - 1 && n == 0) lds.seen[buffer][g] = there ? eight_bits(u.q.held - tile * kTile - at) : 0;
       } else {
         const int j0 = (tile - u.cached) * kTile + at;
 #pragma unroll
-        for (int i = 0; i < kMine; ++i)
-          mine[i].load(fresh, (u.q.first + min(j0 + position(fragment0 + i), u.q.fresh - 1)) * a.kv_stride + (int64_t)u.head * a.dim + dimension(fragment0 + i));
+        for (int i = 0; i < kMine; ++i) {
+          const int64_t from = (u.q.first + min(j0 + position(fragment0 + i), u.q.fresh - 1)) * a.kv_stride + (int64_t)u.head * a.dim + dimension(fragment0 + i);
+          if constexpr (FLOAT) {
+            // (these loads the compiler waits for, and with them for all that were made before)
+            Eight<CT, FLOAT> e;
+            e.load(fresh, from);
+            lds.stage[buffer][(keys ? 0 : kKeys) + fragment0 + i][lane] = e.rounded();
+          } else {
+            to_lds(static_cast<const uint16_t*>(fresh) + from, to + i * 1024);
+          }
+        }
+        if (wave == WAVES - 1 && n == 0) lds.seen[buffer][g] = eight_bits(u.q.fresh - j0);
       }
-    };
-    auto put = [&](int buffer) {
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) stage[buffer][(keys ? 0 : kKeys) + fragment0 + i][lane] = is_fresh ? mine[i].rounded() : mine[i].raw[0];
     };
     // the values of part `part`, as R takes them
     auto read_values = [&](int buffer, int part, uint32_t (&value)[8][kEach / 2]) {
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
         if constexpr (kEach == 8) {
-          const u4 x = stage[buffer][kKeys + t * kParts + part][lane];
+          const u4 x = lds.stage[buffer][kKeys + t * kParts + part][lane];
 #pragma unroll
           for (int j = 0; j < 4; ++j) value[t][j] = x[j];
         } else {
-          const u2 x = reinterpret_cast<const u2*>(&stage[buffer][kKeys + t / 2][16 * g + (t % 2) * 8 + (n >> 1)])[n & 1];
+          const u2 x = reinterpret_cast<const u2*>(&lds.stage[buffer][kKeys + t / 2][16 * g + (t % 2) * 8 + (n >> 1)])[n & 1];
           value[t][0] = x[0], value[t][1] = x[1];
         }
       }
     };
 
-    // pages of the tile that is fetched next, and of the value positions of the tiles at hand (which of them are there?)
-    int my_page = page(u.tile0, at), my_next = page(min(u.tile0 + 1, end - 1), at);
-    int there_0 = page(u.tile0, 8 * g), there_1 = page(min(u.tile0 + 1, end - 1), 8 * g), there_2 = page(min(u.tile0 + 2, end - 1), 8 * g);
-    fetch(u.tile0, my_page);
-    put(u.tile0 & 1);
-    my_page = my_next, my_next = page(min(u.tile0 + 2, end - 1), at);
-    fetch(min(u.tile0 + 1, end - 1), my_page);
+    fill_window();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // from here on only tiles are on their way
     __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) fetch(min(u.tile0 + i, end - 1), i);  // (the last tile again instead of none: the count of loads stays)
+    int buffer = 0;
     for (int tile = u.tile0; tile < end; ++tile) {
-      const int buffer = tile & 1;
-      put(buffer ^ 1);
-      my_page = my_next, my_next = page(min(tile + 3, end - 1), at);
-      const int there_3 = page(min(tile + 3, end - 1), 8 * g);
-      fetch(min(tile + 2, end - 1), my_page);
+      wait_for_all_but<(kAhead - 1) * kMine>();  // the tile is there, and all are done with the one before
+      const int next = min(tile + kAhead, end - 1), into = buffer ? buffer - 1 : kBuffers - 1;
+      if (next < u.cached && ((next * kTile + kTile - 1) >> a.log2_page) - window >= kWindow) {
+        window = (next * kTile) >> a.log2_page;
+        fill_window();
+        __syncthreads();
+      }
+      fetch(next, into);
       if (!idle) {
         f4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) R::add_score(stage[buffer][k][lane], stage[buffer][kSteps + k][lane], query[k], x);
+        for (int k = 0; k < kSteps; ++k) R::add_score(lds.stage[buffer][k][lane], lds.stage[buffer][kSteps + k][lane], query[k], x);
         float s[8];
         u4 p[kTerms];
         rows.exponents(x, s);
         const bool is_new = tile >= u.cached;
-        int seen, there;
-        if (!is_new) {
-          seen = there = (uint32_t)there_0 < (uint32_t)a.pages ? eight_bits(u.q.held - tile * kTile - 8 * g) : 0;
-        } else {
-          const int j0 = (tile - u.cached) * kTile + 8 * g;
-          there = eight_bits(u.q.fresh - j0);
-          seen = rows.seen_new(a, u, 16 * wave + n < u.rows, j0);
-        }
+        const int there = lds.seen[buffer][g];
+        const int seen = is_new ? rows.seen_new(a, u, (tile - u.cached) * kTile + 8 * g) : there;
         const bool partly = __ballot(seen != 255) != 0;
         if (partly) {
 #pragma unroll
@@ -866,9 +899,9 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
           else rows.add_values(part, value, p);
         }
       }
-      there_0 = there_1, there_1 = there_2, there_2 = there_3;
-      __syncthreads();
+      buffer = buffer + 1 == kBuffers ? 0 : buffer + 1;
     }
+    wait_for_all_but<0>();
 
     const int in = 16 * wave + n;
     if (in < u.rows) {
@@ -886,7 +919,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
             else write_through(to + d, rows.four(part, i, j));
           }
     }
-    if (u.pieces > 1) join<CT, FLOAT, DP, kRows, 64 * WAVES>(a, u, joint);
+    if (u.pieces > 1) join<CT, FLOAT, DP, kRows, 64 * WAVES>(a, u, lds.joint);
     __syncthreads();
   }
 }
