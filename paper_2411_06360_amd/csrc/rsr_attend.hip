@@ -12,12 +12,12 @@
 // of dwords with v_perm_b32, eight positions of each dimension, the other operand.
 //
 // Two kernels, by the rows that a key head has (new tokens times query heads of the group):
-//   attend_split  up to 16: the four wavefronts of a workgroup take the same rows and different positions, keys and values go
+//   attend_split  up to 16: the eight wavefronts of a workgroup take the same rows and different positions, keys and values go
 //                 from the cache straight into registers, LDS serves to join the wavefronts at the end
 //   attend_shared more: the wavefronts take different rows and the same positions, which come through LDS
-// The positions of a request (tiles of 32: first the cached ones, then the new ones) are cut into as many pieces as keep the chip
-// busy, a workgroup per piece.  The pieces of a row meet in the workspace, where the workgroup that comes last joins them in
-// their order.
+// The positions of all requests (tiles of 32: first a request's cached ones, then its new ones) are dealt out evenly to as many
+// workgroups as the chip runs at once.  The pieces of a row meet in the workspace, where the workgroup that comes last joins them
+// in their order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -31,9 +31,9 @@ namespace {
 
 using rsr_internal::set_error;
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 512, kWaves = kThreads / 64;  // of attend_split
 constexpr int kTile = 32;        // positions of a tile
-constexpr int kLeastTiles = 4;   // of a piece
+constexpr int kLeastTiles = 16;  // of a workgroup, unless a set has fewer
 constexpr float kBias = 7.f;     // weights are 2^(s - m + 7): as float16 they keep their bits down to 2^-21 of the largest
 constexpr float kLimit = 15.f;   // m follows the maximum when a weight would pass 2^15, so that it seldom does
 
@@ -54,7 +54,6 @@ struct Args {
   uint32_t page_stride, token_stride;
   int32_t requests, tokens, max_new, max_pages, log2_page, pages, kv_heads, dim, group;
   uint32_t group_inverse;  // ceil(2^32 / group), 0 for 1
-  double per_target;       // 1 / pieces that are aimed at
   float scale;
 };
 
@@ -162,77 +161,77 @@ template <typename T> __device__ inline T from_lane(T x, int lane) {
   }
 }
 
+__device__ inline int token_of(const Args& a, int row) { return a.group_inverse ? (int)__umulhi((uint32_t)row, a.group_inverse) : row; }
+
+// A set: the rows of a key head that a workgroup takes together.  The tiles of all sets, one set behind the other, are dealt
+// out to the workgroups in equal runs, so that a workgroup has the end of one set, whole sets, and the beginning of another.
 struct Unit {
   Request q;
-  int32_t r, head, row0, rows;  // request, key head, first row and rows
-  int32_t piece, pieces;
-  int32_t slot, set;            // of the piece in the workspace; of its rows among those that are cut
-  int32_t tile0, tile1, cached; // its tiles; tiles of cached tokens (those behind hold new ones)
+  int32_t r, head, row0, rows;   // request, key head, first row and rows
+  int32_t piece, pieces;         // of the set
+  int32_t slot0, counter;        // where its pieces lie in the workspace, and where they are counted
+  int32_t tile0, tile1, cached;  // its tiles; tiles of cached tokens (those behind hold new ones)
+  __device__ int slot(int c) const { return slot0 + 2 * c - (c > 0); }
 };
 
-// Every wavefront counts the pieces of all requests by itself, a run of requests per lane, without a barrier.
+// x / y for x below 2^51 (rsr_tree_attention sees to that): a quotient in floating point that is off by one at most.  (A workgroup
+// waits for some of these before its first load.)
+__device__ inline int64_t divided(int64_t x, int64_t y) {
+  if (x < (1 << 22)) {
+    const int n = (int)x, d = (int)min(y, (int64_t)1 << 22);
+    int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d));
+    const int left = n - q * d;
+    return q + (left >= d) - (left < 0);
+  }
+  int64_t q = (int64_t)((double)x / (double)y);
+  const int64_t left = x - q * y;
+  return q + (left >= y) - (left < 0);
+}
+
+// Every wavefront adds up the tiles of all requests by itself, a run of requests per lane, without a barrier.
 template <int ROWS> struct Plan {
-  int64_t end, units;  // pieces up to the lane's last request; of all
-  uint64_t cut;        // before the lane's first request: pieces of rows that are cut << 32 | sets of such rows
-  Request q;           // the lane's first request
-  int32_t run, most;   // requests per lane, tiles of a piece
+  int64_t end, work;    // tiles up to the lane's last request; of all
+  Request q;            // the lane's first request
+  int32_t run, groups;  // requests per lane; workgroups with work
 
   static __device__ int blocks_of(const Args& a, const Request& q) { return (q.fresh * a.group + ROWS - 1) / ROWS; }
   static __device__ int tiles_in(const Request& q) { return tiles_of(q.held) + tiles_of(q.fresh); }
-  __device__ int pieces_of(const Request& q) const {
-    const uint32_t tiles = tiles_in(q);
-    return tiles <= (uint32_t)most ? 1 : (tiles + most - 1) / (uint32_t)most;
-  }
-  __device__ void count(const Args& a, const Request& q, int64_t& units, uint64_t& cut) const {
-    const int pieces = pieces_of(q);
-    const int64_t sets = (int64_t)blocks_of(a, q) * a.kv_heads;
-    units += sets * pieces;
-    if (pieces > 1) cut += (uint64_t)(sets * pieces) << 32 | (uint64_t)sets;
-  }
+  static __device__ int64_t work_of(const Args& a, const Request& q) { return (int64_t)blocks_of(a, q) * a.kv_heads * tiles_in(q); }
 
   __device__ explicit Plan(const Args& a, int lane) {
     run = (a.requests + 63) / 64;
     const int r0 = min(lane * run, a.requests), r1 = min(r0 + run, a.requests);
-    int64_t work = 0;
+    int64_t sets = 0;
+    end = 0;
     q = {0, 0, 0};
     for (int r = r1 - 1; r >= r0; --r) {
       q = request_of(a, r);
-      work += (int64_t)blocks_of(a, q) * a.kv_heads * tiles_in(q);
+      end += work_of(a, q);
+      sets += (int64_t)blocks_of(a, q) * a.kv_heads;
     }
-    if (a.requests > 1) {
-#pragma unroll
-      for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d);
-    } else {
-      work = from_lane(work, 0);
-    }
-    most = __builtin_amdgcn_readfirstlane(max((int)((double)work * a.per_target) + 1, kLeastTiles));
-    int64_t mine = 0;
-    uint64_t mine_cut = 0;
-    if (run == 1) {
-      if (r0 < r1) count(a, q, mine, mine_cut);
-    } else {
-      for (int r = r0; r < r1; ++r) count(a, request_of(a, r), mine, mine_cut);
-    }
-    end = mine, cut = mine_cut;
     if (a.requests > 1) {
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
-        const int64_t u = __shfl_up(end, d);
-        const uint64_t c = __shfl_up(cut, d);
-        if (lane >= d) end += u, cut += c;
+        const int64_t u = __shfl_up(end, d), v = __shfl_up(sets, d);
+        if (lane >= d) end += u, sets += v;
       }
+      work = from_lane(end, 63), sets = from_lane(sets, 63);
     } else {
-      end = from_lane(end, 0);
+      work = end = from_lane(end, 0), sets = from_lane(sets, 0);
     }
-    cut -= mine_cut;
-    units = from_lane(end, 63);
+    groups = (int)min((int64_t)gridDim.x, max((work + kLeastTiles - 1) / kLeastTiles, sets));
+    // as many for each set, if there are enough: sets of one length are then cut alike and no workgroup has parts of two
+    if (sets && sets <= groups) groups -= groups % (int)sets;
   }
 
-  __device__ Unit find(const Args& a, int64_t unit) const {
+  __device__ int64_t begin_of(int group) const { return divided(work * group, groups); }
+  __device__ int group_of(int64_t tile) const { return (int)divided((tile + 1) * groups - 1, work); }  // whose run it is in
+
+  // The piece that begins at tile `at` of all and ends at `stop` at the latest; the tiles that it takes are added to `at`.
+  __device__ Unit next(const Args& a, int64_t& at, int64_t stop) const {
     Unit u;
-    const int lane = __builtin_amdgcn_readfirstlane(__builtin_ctzll(__ballot(end > unit)));
-    int64_t at = unit - (lane ? from_lane(end, lane - 1) : 0);
-    uint64_t before = from_lane(cut, lane);
+    const int lane = __builtin_amdgcn_readfirstlane(__builtin_ctzll(__ballot(end > at)));
+    int64_t before = lane ? from_lane(end, lane - 1) : 0;
     u.r = lane * run;
     if (run == 1) {
       u.q = {from_lane(q.first, lane), from_lane(q.fresh, lane), from_lane(q.held, lane)};
@@ -240,34 +239,38 @@ template <int ROWS> struct Plan {
       for (;; ++u.r) {
         const Request q = request_of(a, u.r);
         u.q = {from_lane(q.first, 0), from_lane(q.fresh, 0), from_lane(q.held, 0)};
-        int64_t n = 0;
-        uint64_t c = 0;
-        count(a, u.q, n, c);
-        if (at < n) break;
-        at -= n, before += c;
+        const int64_t work = work_of(a, u.q);
+        if (at < before + work) break;
+        before += work;
       }
     }
-    const uint32_t blocks = blocks_of(a, u.q), in = (uint32_t)at, block = in % blocks, rest = in / blocks;
-    u.pieces = pieces_of(u.q);
-    u.piece = rest % (uint32_t)u.pieces, u.head = rest / (uint32_t)u.pieces;
-    u.set = (int)(uint32_t)before + u.head * blocks + block;
-    u.slot = (int)(before >> 32) + (u.head * blocks + block) * u.pieces + u.piece;
+    const int all = tiles_in(u.q), blocks = blocks_of(a, u.q), set = (int)divided(at - before, all);
+    const int64_t from = before + (int64_t)set * all, last = min(from + all, stop);
+    u.head = blocks == 1 ? set : (int)divided(set, blocks);
+    // (long and short blocks of a chain in turn: a run of tiles has some of both)
+    const int in = set - u.head * blocks, block = in & 1 ? blocks - 1 - (in >> 1) : in >> 1;
     u.row0 = block * ROWS, u.rows = min(ROWS, u.q.fresh * a.group - u.row0);
     u.cached = tiles_of(u.q.held);
-    const int tiles = u.cached + tiles_of(a.mask ? u.q.fresh : (u.row0 + u.rows - 1) / a.group + 1);  // (a chain's rows see no further)
-    // pieces as even as can be
-    const int each = tiles / u.pieces, more = tiles - each * u.pieces;
-    u.tile0 = each * u.piece + min(u.piece, more), u.tile1 = u.tile0 + each + (u.piece < more);
+    u.tile0 = (int)(at - from), u.tile1 = (int)(last - from);
+    if (!a.mask) {  // a chain's rows see no further than themselves: a share of fewer tiles
+      const int tiles = u.cached + tiles_of(token_of(a, u.row0 + u.rows - 1) + 1);
+      if (tiles < all) u.tile0 = (int)divided((int64_t)u.tile0 * tiles, all), u.tile1 = (int)divided((int64_t)u.tile1 * tiles, all);
+    }
+    u.pieces = 1, u.piece = 0;
+    int first = 0;
+    if (at > from || last < from + all) {
+      first = group_of(from);
+      u.pieces = group_of(from + all - 1) - first + 1, u.piece = group_of(at) - first;
+    }
+    u.counter = first;
+    u.slot0 = 2 * first + 1;  // the first workgroup's last run; of the others their first: 2 (first + c)
+    at = last;
     return u;
   }
 };
 
-// Consecutive pieces (the same cached tokens for other rows) go to workgroups of one XCD (blockIdx % 8).
-__device__ inline int64_t first_unit() {
-  return gridDim.x % 8 ? blockIdx.x : (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
-}
-
-__device__ inline int token_of(const Args& a, int row) { return a.group_inverse ? (int)__umulhi((uint32_t)row, a.group_inverse) : row; }
+// Runs that follow each other (the same cached tokens for other rows) go to workgroups of one XCD (blockIdx % 8).
+__device__ inline int group_index() { return gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8; }
 
 // The first of `count` dimensions: where the head ends before them the last ones it has (they meet zeros of the query, or a
 // result that nobody wants).  FULL: the head has as many dimensions as the kernel.
@@ -452,7 +455,7 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
 template <typename CT, bool FLOAT> __device__ inline void store(const Args& a, const Unit& u, int in, int d, f4 x, float total) {
   const int row = u.row0 + in, token = token_of(a, row);
   const int64_t to = (u.q.first + token) * a.out_stride + (int64_t)(u.head * a.group + row - token * a.group) * a.dim + d;
-  const f4 o = total == 0.f ? f4{0, 0, 0, 0} : x / total;
+  const f4 o = total == 0.f ? f4{0, 0, 0, 0} : x * (1.f / total);
   if constexpr (FLOAT) *reinterpret_cast<f4*>(static_cast<float*>(a.out) + to) = o;
   else *reinterpret_cast<u2*>(static_cast<uint16_t*>(a.out) + to) = u2{pair_of<CT>(o[0], o[1]), pair_of<CT>(o[2], o[3])};
 }
@@ -475,68 +478,72 @@ __device__ inline float behind(float m, float top) { return m == -INFINITY ? 0.f
 
 // The workgroup that comes last joins the pieces of its rows, in their order.  What the others wrote is there: every wavefront
 // waits until its writes, which go through all caches, are done, then the workgroup counts itself; the last one drops what its own
-// caches may hold before it reads.  Bound by the latency of these reads: the lanes share out the pieces of a row for its maximum and
-// sum, then the pieces of its values as far as the values do not fill the lanes, and many reads are under way at once.
-template <int ROWS, int THREADS> struct Joint {
-  static constexpr int kShares = THREADS / ROWS;
-  float m[kShares][ROWS], l[kShares][ROWS];
+// caches may hold before it reads.  Bound by the latency of these reads: a lane has eight pieces of its four values under way at once,
+// and lanes that are left over take a share of the pieces.
+template <int THREADS> struct Joint {
   f4 part[THREADS];
+  float m[THREADS], l[THREADS];
   uint32_t arrived;
 };
 
-template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inline void join(const Args& a, const Unit& u, Joint<ROWS, THREADS>& lds) {
+template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inline void join(const Args& a, const Unit& u, Joint<THREADS>& lds) {
+  constexpr int kAtOnce = 8;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   const int tid = hidden(threadIdx.x);
-  if (tid == 0) lds.arrived = __hip_atomic_fetch_add(&a.counters[u.set], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (tid == 0) lds.arrived = __hip_atomic_fetch_add(&a.counters[u.counter], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   if (lds.arrived != (uint32_t)u.pieces - 1) return;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  if (tid == 0) __hip_atomic_store(&a.counters[u.set], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (tid == 0) __hip_atomic_store(&a.counters[u.counter], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   typedef Partial<DP, ROWS> P;
-  const float* const first = P::row(a, u.slot - u.piece, 0);
-  {
-    const int in = tid % ROWS, share = tid / ROWS;
+  const int items = u.rows * (DP / 4), shares = items < THREADS ? THREADS / items : 1;
+  for (int e0 = 0; e0 < items; e0 += THREADS) {
+    const int share = shares > 1 ? tid / items : 0, e = e0 + tid - share * items, in = e / (DP / 4), d = e % (DP / 4) * 4;
+    const bool there = e < items && d < a.dim && share < shares;
+    f4 x{0, 0, 0, 0};
     float m = -INFINITY, l = 0.f;
-    if (in < u.rows) {
-#pragma unroll 4
-      for (int c = share; c < u.pieces; c += Joint<ROWS, THREADS>::kShares) {
-        const f2 ml = *reinterpret_cast<const f2*>(first + (int64_t)c * P::kPiece + in * P::kRow + DP);
-        const float mc = ml[0], lc = ml[1], top = fmaxf(m, mc);
-        // (without a maximum: 0, or NaN)
-        l = (m == -INFINITY ? l : l * exp2f(m - top)) + (mc == -INFINITY ? lc : lc * exp2f(mc - top));
+    if (there) {
+      const float* const from = P::row(a, 0, in);
+      for (int c0 = share; c0 < u.pieces; c0 += kAtOnce * shares) {
+        f4 xc[kAtOnce];
+        f2 mlc[kAtOnce];
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          const float* const p = from + (int64_t)u.slot(min(c0 + k * shares, u.pieces - 1)) * P::kPiece;
+          xc[k] = *reinterpret_cast<const f4*>(p + d), mlc[k] = *reinterpret_cast<const f2*>(p + DP);
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          if (c0 + k * shares >= u.pieces) mlc[k] = f2{-INFINITY, 0.f};
+          top = fmaxf(top, mlc[k][0]);
+        }
+        const float back = behind(m, top);
+        x *= back, l = m == -INFINITY ? l : l * back;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          const float w = behind(mlc[k][0], top);
+          x += xc[k] * w, l += mlc[k][0] == -INFINITY ? mlc[k][1] : mlc[k][1] * w;  // (without a maximum: 0, or NaN)
+        }
         m = top;
       }
     }
-    lds.m[share][in] = m, lds.l[share][in] = l;
-  }
-  __syncthreads();
-  const int items = u.rows * (DP / 4), shares = items < THREADS ? THREADS / items : 1;
-  for (int e0 = 0; e0 < items; e0 += THREADS) {
-    const int e = e0 + tid % (shares > 1 ? items : THREADS), share = shares > 1 ? tid / items : 0;
-    const int in = e / (DP / 4), d = e % (DP / 4) * 4;
-    const bool there = e < items && d < a.dim && share < shares;
-    f4 x{0, 0, 0, 0};
-    float top = -INFINITY, total = 0.f;
-    if (there) {
-#pragma unroll
-      for (int w = 0; w < Joint<ROWS, THREADS>::kShares; ++w) top = fmaxf(top, lds.m[w][in]);
-#pragma unroll
-      for (int w = 0; w < Joint<ROWS, THREADS>::kShares; ++w) total += lds.m[w][in] == -INFINITY ? lds.l[w][in] : lds.l[w][in] * exp2f(lds.m[w][in] - top);
-      const float* const from = first + in * P::kRow;
-#pragma unroll 8
-      for (int c = share; c < u.pieces; c += shares) {
-        const float* const p = from + (int64_t)c * P::kPiece;
-        x += *reinterpret_cast<const f4*>(p + d) * behind(p[DP], top);
-      }
-    }
     if (shares > 1) {
-      lds.part[tid] = x;
+      lds.part[tid] = x, lds.m[tid] = m, lds.l[tid] = l;
       __syncthreads();
       if (tid >= items) continue;
-      for (int w = 1; w < shares; ++w) x += lds.part[w * items + tid];
+      float top = m;
+      for (int w = 1; w < shares; ++w) top = fmaxf(top, lds.m[w * items + tid]);
+      const float back = behind(m, top);
+      x *= back, l = m == -INFINITY ? l : l * back;
+      for (int w = 1; w < shares; ++w) {
+        const int at = w * items + tid;
+        const float mw = lds.m[at], lw = lds.l[at], by = behind(mw, top);
+        x += lds.part[at] * by, l += mw == -INFINITY ? lw : lw * by;
+      }
     }
-    if (there) store<CT, FLOAT>(a, u, in, d, x, total);
+    if (there) store<CT, FLOAT>(a, u, in, d, x, l);
   }
 }
 
@@ -546,16 +553,20 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
   typedef Rows<CT, FLOAT, DP> R;
   constexpr int kRows = 16, kSteps = R::kSteps, kEach = R::kEach, kParts = R::kParts, kTerms = R::kTerms;
   constexpr int kLine = DP + 4;  // floats between rows in LDS
-  __shared__ float row_m[kWaves][kRows], row_l[kWaves][kRows];
+  __shared__ float row_m[kWaves][kRows], row_l[kWaves][kRows], all_m[kRows], all_l[kRows];
   __shared__ __align__(16) float joined[kWaves][16][kLine];
   __shared__ __align__(16) u4 queries[FLOAT ? kSteps : 1][FLOAT ? kTerms : 1][64];  // the operands of floats fill too many registers
-  __shared__ Joint<kRows, kThreads> joint;
+  __shared__ Joint<kThreads> joint;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Plan<kRows> plan(a, threadIdx.x & 63);
 
-  for (int64_t unit = first_unit(); unit < plan.units; unit += gridDim.x) {
+  const int group = group_index();
+  if (group >= plan.groups) return;
+  int64_t at_tile = plan.begin_of(group);
+  const int64_t stop = plan.begin_of(group + 1);
+  while (at_tile < stop) {
     const int tid = hidden(threadIdx.x), lane = tid & 63, n = lane & 15, g = lane >> 4;
-    const Unit u = plan.find(a, unit);
+    const Unit u = plan.next(a, at_tile, stop);
     const int t0 = u.tile0 + (u.tile1 - u.tile0) * wave / kWaves, t1 = u.tile0 + (u.tile1 - u.tile0) * (wave + 1) / kWaves;
     R rows;
     u4 query[kSteps][kTerms];
@@ -705,10 +716,13 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
       }
     }
 
-    // ---- the four wavefronts
+    // ---- the wavefronts
     if (g == 0) row_m[wave][n] = rows.maximum(), row_l[wave][n] = rows.sum[0];
     __syncthreads();
-    const float back = behind(rows.maximum(), fmaxf(fmaxf(row_m[0][n], row_m[1][n]), fmaxf(row_m[2][n], row_m[3][n])));
+    float top = row_m[0][n];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, row_m[w][n]);
+    const float back = behind(rows.maximum(), top);
 #pragma unroll
     for (int part = 0; part < kParts; ++part)
 #pragma unroll
@@ -716,22 +730,25 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
 #pragma unroll
         for (int j = 0; j < kEach; j += 4)
           *reinterpret_cast<f4*>(&joined[wave][n][part * 16 * kEach + kEach * (4 * g + i) + j]) = rows.four(part, i, j) * back;
+    if (wave == 0 && g == 0) {
+      float total = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) total += row_m[w][n] == -INFINITY ? row_l[w][n] : row_l[w][n] * exp2f(row_m[w][n] - top);
+      all_m[n] = top, all_l[n] = total;
+    }
     __syncthreads();
     for (int e = tid; e < u.rows * (DP / 4); e += kThreads) {
       const int in = e / (DP / 4), d = e % (DP / 4) * 4;
-      if (d >= a.dim) continue;
-      const f4 x = (*reinterpret_cast<const f4*>(&joined[0][in][d]) + *reinterpret_cast<const f4*>(&joined[1][in][d])) +
-                   (*reinterpret_cast<const f4*>(&joined[2][in][d]) + *reinterpret_cast<const f4*>(&joined[3][in][d]));
-      const float top = fmaxf(fmaxf(row_m[0][in], row_m[1][in]), fmaxf(row_m[2][in], row_m[3][in]));
-      float total = 0.f;
+      if (!FULL && d >= a.dim) continue;
+      f4 x = *reinterpret_cast<const f4*>(&joined[0][in][d]);
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) total += row_m[w][in] == -INFINITY ? row_l[w][in] : row_l[w][in] * exp2f(row_m[w][in] - top);
+      for (int w = 1; w < kWaves; ++w) x += *reinterpret_cast<const f4*>(&joined[w][in][d]);
       if (u.pieces == 1) {
-        store<CT, FLOAT>(a, u, in, d, x, total);
+        store<CT, FLOAT>(a, u, in, d, x, all_l[in]);
       } else {
-        float* to = Partial<DP, kRows>::row(a, u.slot, in);
+        float* to = Partial<DP, kRows>::row(a, u.slot(u.piece), in);
         write_through(to + d, x);
-        if (d == 0) write_through(to + DP, top, total);
+        if (d == 0) write_through(to + DP, all_m[in], all_l[in]);
       }
     }
     if (u.pieces > 1) join<CT, FLOAT, DP, kRows, kThreads>(a, u, joint);
@@ -772,7 +789,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
     u4 stage[kBuffers][kFragments][64];
     int32_t seen[kBuffers][4];  // which of eight positions there are
     int32_t pages[kWindow];
-    Joint<kRows, 64 * WAVES> joint;
+    Joint<64 * WAVES> joint;
   };
   __shared__ __align__(1024) Lds lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -782,9 +799,13 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
   const bool keys = wave < kHalf;
   const int fragment0 = (keys ? wave : wave - kHalf) * kMine;
 
-  for (int64_t unit = first_unit(); unit < plan.units; unit += gridDim.x) {
+  const int group = group_index();
+  if (group >= plan.groups) return;
+  int64_t at_tile = plan.begin_of(group);
+  const int64_t stop = plan.begin_of(group + 1);
+  while (at_tile < stop) {
     const int tid = hidden(threadIdx.x), lane = tid & 63, n = lane & 15, g = lane >> 4;
-    const Unit u = plan.find(a, unit);
+    const Unit u = plan.next(a, at_tile, stop);
     // Fragment f of the keys: step f % kSteps of the 16 keys f / kSteps; of the values: part f % kParts of position f / kParts of the
     // lane's eight (heads of up to 64: positions 2 f and 2 f + 1, half a row of lanes each).
     const int at = keys ? 8 * (n >> 2) : 8 * g;  // eight positions that lie on one page
@@ -905,7 +926,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
 
     const int in = 16 * wave + n;
     if (in < u.rows) {
-      float* const to = Partial<DP, kRows>::row(a, u.slot, in);
+      float* const to = Partial<DP, kRows>::row(a, u.slot(u.piece), in);
       if (u.pieces > 1 && g == 0) write_through(to + DP, rows.maximum(), rows.sum[0]);
 #pragma unroll
       for (int part = 0; part < kParts; ++part)
@@ -942,7 +963,7 @@ struct Shape {
   int dims;         // head_dim, padded
   int waves;        // of a workgroup of attend_shared, 0: attend_split
   int rows;         // of a workgroup
-  int target;       // pieces of work that are aimed at: workgroups that the chip runs at once
+  int target;       // workgroups at most: those that the chip runs at once
   int64_t counters_bytes, bytes;  // of the workspace
 };
 
@@ -953,9 +974,9 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   // (keys and values of 256 dimensions do not fit in the registers beside a result)
   s.waves = rows <= 16 && s.dims < 256 ? 0 : rows <= 64 || s.dims == 256 || (floats && s.dims == 128) ? 4 : 8;
   s.rows = s.waves ? 16 * s.waves : 16;
-  s.target = s.waves == 8 || (s.waves && (floats || s.dims == 256)) ? 256 : 512;
+  s.target = s.waves == 4 && !floats && s.dims < 256 ? 512 : 256;
   s.counters_bytes = (int64_t)s.target * 4;
-  s.bytes = s.counters_bytes + (int64_t)(2 * s.target + 1) * s.rows * (s.dims + 4) * 4;
+  s.bytes = s.counters_bytes + (int64_t)2 * s.target * s.rows * (s.dims + 4) * 4;
   return s;
 }
 
@@ -1005,14 +1026,16 @@ int rsr_tree_attention(const rsr_cache_t* cache, const rsr_step_t* step, const v
                static_cast<uint32_t*>(workspace), reinterpret_cast<float*>(static_cast<char*>(workspace) + s.counters_bytes),
                q_stride, kv_stride, out_stride, cache->head_stride, (uint32_t)cache->page_stride, (uint32_t)cache->token_stride, step->requests, step->tokens,
                step->max_new, step->max_pages, rsr_internal::log2_of(cache->page_size), cache->pages, cache->kv_heads, cache->head_dim, group,
-               group == 1 ? 0u : (uint32_t)(((uint64_t(1) << 32) + group - 1) / group), 1.0 / s.target, scale};
+               group == 1 ? 0u : (uint32_t)(((uint64_t(1) << 32) + group - 1) / group), scale};
   const bool full = cache->head_dim == s.dims;
   auto kern = cache->dtype == RSR_F16 ? kernel_of<_Float16>(s, floats, full) : kernel_of<__bf16>(s, floats, full);
   // no more workgroups than there can be pieces
   const int64_t blocks = ((int64_t)step->max_new * group + s.rows - 1) / s.rows;
   const int64_t tiles = (((int64_t)step->max_pages * cache->page_size) + kTile - 1) / kTile + (step->max_new + kTile - 1) / kTile;
-  const int64_t units = step->requests * (int64_t)cache->kv_heads * blocks * ((tiles + kLeastTiles - 1) / kLeastTiles);
-  hipLaunchKernelGGL(kern, dim3((unsigned)std::min(units, (int64_t)s.target)), dim3(s.waves ? 64 * s.waves : kThreads), 0, static_cast<hipStream_t>(stream), a);
+  const int64_t most = std::min((int64_t)s.target, (int64_t)step->requests * cache->kv_heads * blocks * ((tiles + kLeastTiles - 1) / kLeastTiles));
+  if ((double)step->requests * cache->kv_heads * blocks * tiles >= 0x1p42)
+    return set_error(RSR_ERR_UNSUPPORTED, "the tables could name more tokens than the kernels count");
+  hipLaunchKernelGGL(kern, dim3((unsigned)most), dim3(s.waves ? 64 * s.waves : kThreads), 0, static_cast<hipStream_t>(stream), a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(RSR_ERR_HIP, std::string("rsr_tree_attention: ") + hipGetErrorString(e));
   return RSR_OK;
