@@ -220,8 +220,8 @@ template <int ROWS> struct Plan {
       work = end = from_lane(end, 0), sets = from_lane(sets, 0);
     }
     groups = (int)min((int64_t)gridDim.x, max((work + kLeastTiles - 1) / kLeastTiles, sets));
-    // as many for each set, if there are enough: sets of one length are then cut alike and no workgroup has parts of two
-    if (sets && sets <= groups) groups -= groups % (int)sets;
+    // as many for each set, if few are lost by it: sets of one length are then cut alike and no workgroup has parts of two
+    if (sets && sets <= groups && groups % (int)sets <= groups / 8) groups -= groups % (int)sets;
   }
 
   __device__ int64_t begin_of(int group) const { return divided(work * group, groups); }
@@ -473,12 +473,18 @@ __device__ inline void write_through(float* to, float x, float y) {
 }
 __device__ inline void write_through(float* to, f4 x) { write_through(to, x[0], x[1]), write_through(to + 2, x[2], x[3]); }
 
+// And they are read past the caches, which may hold what was there before.
+__device__ inline f2 read_through(const float* from) {
+  const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return __builtin_bit_cast(f2, x);
+}
+
 // 2^(m - top) for a maximum that may be that of nothing
 __device__ inline float behind(float m, float top) { return m == -INFINITY ? 0.f : exp2f(m - top); }
 
 // The workgroup that comes last joins the pieces of its rows, in their order.  What the others wrote is there: every wavefront
-// waits until its writes, which go through all caches, are done, then the workgroup counts itself; the last one drops what its own
-// caches may hold before it reads.  Bound by the latency of these reads: a lane has eight pieces of its four values under way at once,
+// waits until its writes, which go through all caches, are done, then the workgroup counts itself.  (A release and an acquire
+// instead would write back and drop a whole L2 each, 0.1 and 0.3 us for every workgroup, one after the other.)  Bound by the latency of these reads: a lane has eight pieces of its four values under way at once,
 // and lanes that are left over take a share of the pieces.
 template <int THREADS> struct Joint {
   f4 part[THREADS];
@@ -494,7 +500,6 @@ template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inl
   if (tid == 0) lds.arrived = __hip_atomic_fetch_add(&a.counters[u.counter], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   if (lds.arrived != (uint32_t)u.pieces - 1) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   if (tid == 0) __hip_atomic_store(&a.counters[u.counter], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   typedef Partial<DP, ROWS> P;
   const int items = u.rows * (DP / 4), shares = items < THREADS ? THREADS / items : 1;
@@ -512,7 +517,8 @@ template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inl
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
           const float* const p = from + (int64_t)u.slot(min(c0 + k * shares, u.pieces - 1)) * P::kPiece;
-          xc[k] = *reinterpret_cast<const f4*>(p + d), mlc[k] = *reinterpret_cast<const f2*>(p + DP);
+          const f2 lo = read_through(p + d), hi = read_through(p + d + 2);
+          xc[k] = f4{lo[0], lo[1], hi[0], hi[1]}, mlc[k] = read_through(p + DP);
         }
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
@@ -596,6 +602,19 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
       }
     };
 
+    // The new tokens of the wavefront's first such tile are asked for now, a line per lane, and come from L2 when it is their turn.
+    constexpr int kAsked = FLOAT ? 4 : 2;  // loads: keys and values, 64 dimensions of 16 bits or 32 floats in a line
+    uint32_t asked[kAsked];
+    if (t1 > u.cached) {
+      const int j = min((max(t0, u.cached) - u.cached) * kTile + (lane >> 1), u.q.fresh - 1);
+      const int64_t from = (u.q.first + j) * a.kv_stride + (int64_t)u.head * a.dim;
+#pragma unroll
+      for (int i = 0; i < kAsked; ++i) {
+        const int64_t at = from + min((lane & 1) * (FLOAT ? 32 : 64) + i / 2 * 64, a.dim - 2);
+        asked[i] = *reinterpret_cast<const uint32_t*>(static_cast<const char*>(i & 1 ? a.v : a.k) + at * (FLOAT ? 4 : 2));
+      }
+    }
+
     // ---- cached tokens.  Loads run ahead by a tile, their pages by two; the last ones are loaded again instead of none,
     // so that the order of loads is the same in every turn and none waits for a later one.
     const int c1 = min(t1, u.cached);
@@ -667,6 +686,10 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
     }
 
     // ---- new tokens
+    if (t1 > u.cached) {
+#pragma unroll
+      for (int i = 0; i < kAsked; ++i) asm volatile("" ::"v"(asked[i]));
+    }
     for (int tile = max(t0, u.cached); tile < t1; ++tile) {
       const int j0 = (tile - u.cached) * kTile;
       const int64_t in_row = (int64_t)u.head * a.dim;
