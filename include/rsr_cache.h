@@ -90,7 +90,7 @@ typedef struct rsr_step_t {
  *   dtype    of q, k, v and out: RSR_F32 or the type of the cache
  *   heads    a multiple of kv_heads, at most 64 * kv_heads
  *   scale    finite
- *   strides  at least a row's elements; rows and pointers 16-byte aligned
+ *   strides  at least a row's elements, below 2^31; rows and pointers 16-byte aligned
  *   workspace  DEVICE, rsr_tree_attention_workspace bytes, 256-byte aligned, zero before its first use; calls leave it
  *            ready for the next one.  Calls that share it must not overlap.
  *
@@ -98,7 +98,8 @@ typedef struct rsr_step_t {
  * through the matrix cores as sums of two float16 or three bfloat16.  With 16-bit activations the weights
  * are rounded to that type before they meet the values.  The order of additions is fixed for given lengths:
  * results are reproducible.
- * Errors: RSR_ERR_INVALID_ARGUMENT, RSR_ERR_HIP (launch failure).
+ * Errors: RSR_ERR_INVALID_ARGUMENT, RSR_ERR_UNSUPPORTED (tables that could name more than some 2^47 tokens of all key heads),
+ * RSR_ERR_HIP (launch failure).
  */
 int64_t rsr_tree_attention_workspace(const rsr_cache_t *cache, const rsr_step_t *step, int heads); /* bytes, or a negative status; HOST only */
 int rsr_tree_attention(const rsr_cache_t *cache, const rsr_step_t *step, const void *q, int64_t q_stride, const void *k,

@@ -50,8 +50,8 @@ struct Args {
   const uint64_t* mask;
   uint32_t* counters;
   float* partial;
-  int64_t q_stride, kv_stride, out_stride, head_stride;
-  uint32_t page_stride, token_stride;
+  int64_t head_stride;
+  uint32_t q_stride, kv_stride, out_stride, page_stride, token_stride;
   int32_t requests, tokens, max_new, max_pages, log2_page, pages, kv_heads, dim, group;
   uint32_t group_inverse;  // ceil(2^32 / group), 0 for 1
   float scale;
@@ -133,13 +133,16 @@ __device__ inline float max3(float x, float y, float z) {
   return r;
 }
 
+// Where the elements of row `row` of activations begin.
+__device__ inline int64_t row_at(int row, uint32_t stride) { return (int64_t)((uint64_t)(uint32_t)row * stride); }
+
 __device__ inline int eight_bits(int count) { return (1 << max(min(count, 8), 0)) - 1; }  // the lowest `count`
 
 // ---- which piece of work ------------------------------------------------------------------------------------
 __device__ inline int tiles_of(int n) { return (n + kTile - 1) / kTile; }
 
 struct Request {
-  int64_t first;  // row of its first new token
+  int32_t first;  // row of its first new token
   int32_t fresh;  // new tokens
   int32_t held;   // cached tokens
 };
@@ -148,7 +151,7 @@ __device__ inline Request request_of(const Args& a, int r) {
   const int64_t first = a.start[r], end = min((int64_t)a.start[r + 1], (int64_t)a.tokens);
   const int64_t fresh = first < 0 ? 0 : max(min(end - first, (int64_t)a.max_new), (int64_t)0);
   const int64_t held = min((int64_t)max(a.held[r], 0), (int64_t)a.max_pages << a.log2_page);
-  return {first, (int32_t)fresh, (int32_t)min(held, (int64_t)INT32_MAX - 65536 - 1024)};
+  return {(int32_t)first, (int32_t)fresh, (int32_t)min(held, (int64_t)INT32_MAX - 65536 - 1024)};
 }
 
 template <typename T> __device__ inline T from_lane(T x, int lane) {
@@ -295,7 +298,7 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
     const int in = first + n, row = u.row0 + in;
     const bool there = in < u.rows;
     token = there ? token_of(a, row) : 0;
-    const int64_t from = (u.q.first + token) * a.q_stride + (int64_t)(u.head * a.group + (there ? row - token * a.group : 0)) * a.dim;
+    const int64_t from = row_at(u.q.first + token, a.q_stride) + (u.head * a.group + (there ? row - token * a.group : 0)) * a.dim;
     mask = there && a.mask ? a.mask[u.q.first + token] : ~0ull;
     if (!there) token = a.max_new;  // (a row that is not there sees all: it must not make a tile one that has to be masked)
     factor = a.scale * 1.44269504088896341f;
@@ -383,20 +386,20 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
   }
 
   // Of eight positions the dimension that is number j of the lane's piece.
-  static __device__ u4 column(const uint32_t (&value)[8][kEach / 2], int j) {
+  static __device__ u4 column(const uint32_t (&value)[8][kEach / 2], int j, uint32_t even = 0x05040100, uint32_t odd = 0x07060302) {
     u4 x;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) x[t] = __builtin_amdgcn_perm(value[2 * t + 1][j >> 1], value[2 * t][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+    for (int t = 0; t < 4; ++t) x[t] = __builtin_amdgcn_perm(value[2 * t + 1][j >> 1], value[2 * t][j >> 1], j & 1 ? odd : even);
     return x;
+  }
+  __device__ void add_column(int at, u4 x, const u4 (&p)[kTerms]) {
+#pragma unroll
+    for (int t = kTerms - 1; t >= 0; --t) acc[at] = Half<CT>::mfma(x, p[t], acc[at]);
   }
   // Values of part `part`: [position][pair of dimensions].
   __device__ void add_values(int part, const uint32_t (&value)[8][kEach / 2], const u4 (&p)[kTerms]) {
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const u4 x = column(value, j);
-#pragma unroll
-      for (int t = kTerms - 1; t >= 0; --t) acc[part * kEach + j] = Half<CT>::mfma(x, p[t], acc[part * kEach + j]);
-    }
+    for (int j = 0; j < kEach; ++j) add_column(part * kEach + j, column(value, j), p);
   }
 
   // Which of eight new tokens from number j0 on the row sees, a bit each.
@@ -404,44 +407,47 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
     return (a.mask ? (int)(mask >> min(j0, 63)) & 255 : eight_bits(token + 1 - j0)) & eight_bits(u.q.fresh - j0);
   }
 
-  // A value that is not finite must not reach the rows that do not see it (0 times infinity is NaN).  Does the lane hold one?
-  static __device__ bool is_odd(uint32_t half) { return (half & Half<CT>::kExponent) == Half<CT>::kExponent; }
-  static __device__ bool has_odd(const uint32_t (&value)[8][kEach / 2]) {
-    bool odd = false;
+  // A value that is not finite must not reach the rows that do not see it (0 times infinity is NaN).  Which of the lane's eight
+  // positions have one?
+  static __device__ uint32_t odd_positions(const uint32_t (&value)[8][kEach / 2]) {
+    typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+    uint32_t odd = 0;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      us2 most{0, 0};
+#pragma unroll
+      for (int j = 0; j < kEach / 2; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, value[t][j] & 0x7fff7fffu));
+      odd |= most.x >= Half<CT>::kExponent || most.y >= Half<CT>::kExponent ? 1u << t : 0u;
+    }
+    return odd;
+  }
+  // These positions, one after the other, each as a product of its own that only the rows that see it take (seldom needed: a loop,
+  // and few registers).  Of the operands of a float weight the small ones make no infinite value what it is not.
+  __device__ void add_odd(int part, const uint32_t (&value)[8][kEach / 2], const u4 (&p)[kTerms], uint32_t odd, int seen, int n, int g) {
+    for (int t = 0; t < kTile; ++t) {
+      const bool mine = g == t >> 3 && odd >> (t & 7) & 1;
+      if (!__ballot(mine)) continue;
+      const bool sees = __shfl(seen, (t & ~7) * 2 + n) >> (t & 7) & 1;
+      const uint32_t even_halves = hidden(0x05040100), odd_halves = hidden(0x07060302);
+      u4 only;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) only[k] = mine && (t & 7) >> 1 == k ? (t & 1 ? 0xffff0000u : 0xffffu) : 0u;
+#pragma unroll
+      for (int j = 0; j < kEach; ++j)
+#pragma unroll
+        for (int k = 0; k < kTerms; ++k) {
+          const f4 x = Half<CT>::mfma(column(value, j, even_halves, odd_halves) & only, p[k], f4{0, 0, 0, 0});
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[part * kEach + j][i] += sees && (k == 0 || fabsf(x[i]) < INFINITY) ? x[i] : 0.f;
+        }
+    }
+  }
+  // And they are left out of what all rows take.
+  static __device__ void leave_out(uint32_t (&value)[8][kEach / 2], uint32_t odd) {
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
-      for (int j = 0; j < kEach / 2; ++j) odd |= is_odd(value[t][j]) || is_odd(value[t][j] >> 16);
-    return odd;
-  }
-  // As add_values, for such values: they are left out of the product, and sums of the weights of the positions that have
-  // +infinity or NaN, and -infinity or NaN, say where the result becomes what.
-  __device__ void add_odd_values(int part, const uint32_t (&value)[8][kEach / 2], const u4 (&p)[kTerms]) {
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      u4 x = column(value, j), up, down;
-      const uint32_t exponent = hidden(Half<CT>::kExponent), ones = hidden(Half<CT>::kOnes);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        uint32_t kept = x[t], more = 0, less = 0;
-#pragma unroll
-        for (int h = 0; h < 32; h += 16) {
-          const uint32_t half = x[t] >> h & 0xffff, one = ones & 0xffffu << h;
-          const bool nan = (half & 0x7fff) > exponent;
-          if ((half & exponent) == exponent) kept &= ~(0xffffu << h);
-          if (nan || half == exponent) more |= one;
-          if (nan || half == (exponent | 0x8000)) less |= one;
-        }
-        x[t] = kept, up[t] = more, down[t] = less;
-      }
-      f4& to = acc[part * kEach + j];
-#pragma unroll
-      for (int t = kTerms - 1; t >= 0; --t) to = Half<CT>::mfma(x, p[t], to);
-      const f4 plus = Half<CT>::mfma(up, p[0], f4{0, 0, 0, 0}), minus = Half<CT>::mfma(down, p[0], f4{0, 0, 0, 0});
-#pragma unroll
-      for (int i = 0; i < 4; ++i) to[i] += (plus[i] > 0.f ? INFINITY : 0.f) + (minus[i] > 0.f ? -INFINITY : 0.f);
-      __builtin_amdgcn_sched_barrier(0);  // (seldom taken: let it need few registers)
-    }
+      for (int j = 0; j < kEach / 2; ++j) value[t][j] = odd >> t & 1 ? 0u : value[t][j];
   }
 
   __device__ float maximum() const { return limit == kLimit ? base + kBias : -INFINITY; }
@@ -454,7 +460,7 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
 // ---- results ------------------------------------------------------------------------------------------------
 template <typename CT, bool FLOAT> __device__ inline void store(const Args& a, const Unit& u, int in, int d, f4 x, float total) {
   const int row = u.row0 + in, token = token_of(a, row);
-  const int64_t to = (u.q.first + token) * a.out_stride + (int64_t)(u.head * a.group + row - token * a.group) * a.dim + d;
+  const int64_t to = row_at(u.q.first + token, a.out_stride) + (u.head * a.group + row - token * a.group) * a.dim + d;
   const f4 o = total == 0.f ? f4{0, 0, 0, 0} : x * (1.f / total);
   if constexpr (FLOAT) *reinterpret_cast<f4*>(static_cast<float*>(a.out) + to) = o;
   else *reinterpret_cast<u2*>(static_cast<uint16_t*>(a.out) + to) = u2{pair_of<CT>(o[0], o[1]), pair_of<CT>(o[2], o[3])};
@@ -607,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
     uint32_t asked[kAsked];
     if (t1 > u.cached) {
       const int j = min((max(t0, u.cached) - u.cached) * kTile + (lane >> 1), u.q.fresh - 1);
-      const int64_t from = (u.q.first + j) * a.kv_stride + (int64_t)u.head * a.dim;
+      const int64_t from = row_at(u.q.first + j, a.kv_stride) + u.head * a.dim;
 #pragma unroll
       for (int i = 0; i < kAsked; ++i) {
         const int64_t at = from + min((lane & 1) * (FLOAT ? 32 : 64) + i / 2 * 64, a.dim - 2);
@@ -669,14 +675,9 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
         rows.exponents(x, s);
         if (__ballot(seen != 255)) {
 #pragma unroll
-          for (int t = 0; t < 8; ++t) {
-            const bool is = seen >> t & 1;
-            s[t] = is ? s[t] : -INFINITY;
+          for (int t = 0; t < 8; ++t) s[t] = seen >> t & 1 ? s[t] : -INFINITY;
 #pragma unroll
-            for (int part = 0; part < kParts; ++part)
-#pragma unroll
-              for (int j = 0; j < kEach / 2; ++j) value[part][t][j] = is ? value[part][t][j] : 0u;
-          }
+          for (int part = 0; part < kParts; ++part) R::leave_out(value[part], ~seen);  // (what lies on a page behind the last token)
         }
         rows.weigh(s, p);
 #pragma unroll
@@ -692,11 +693,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
     }
     for (int tile = max(t0, u.cached); tile < t1; ++tile) {
       const int j0 = (tile - u.cached) * kTile;
-      const int64_t in_row = (int64_t)u.head * a.dim;
+      const int in_row = u.head * a.dim;
       Eight<CT, FLOAT> e;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int64_t from = (u.q.first + min(j0 + 8 * (n >> 2) + (n & 3) + 4 * h, u.q.fresh - 1)) * a.kv_stride + in_row;
+        const int64_t from = row_at(u.q.first + min(j0 + 8 * (n >> 2) + (n & 3) + 4 * h, u.q.fresh - 1), a.kv_stride) + in_row;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
           e.load(a.k, from + within<FULL>(a, 32 * k + 8 * g, 8));
@@ -705,15 +706,15 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
       }
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const bool there = j0 + 8 * g + t < u.q.fresh;
-        const int64_t from = (u.q.first + min(j0 + 8 * g + t, u.q.fresh - 1)) * a.kv_stride + in_row;
+        // (behind the last token the last one again: its values meet weights of 0)
+        const int64_t from = row_at(u.q.first + min(j0 + 8 * g + t, u.q.fresh - 1), a.kv_stride) + in_row;
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
           const int d = within<FULL>(a, part * 16 * kEach + kEach * n, kEach);
           e.load(a.v, from + (d & ~7));  // (of eight dimensions the lane may take four)
           const u4 x = e.rounded();
 #pragma unroll
-          for (int j = 0; j < kEach / 2; ++j) value[part][t][j] = there ? (kEach == 4 && d & 4 ? x[2 + j] : x[j]) : 0u;
+          for (int j = 0; j < kEach / 2; ++j) value[part][t][j] = kEach == 4 && d & 4 ? x[2 + j] : x[j];
         }
       }
       f4 x[2];
@@ -722,20 +723,22 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
       u4 p[kTerms];
       rows.exponents(x, s);
       const int seen = rows.seen_new(a, u, j0 + 8 * g);
-      bool odd = false;
-      if (__ballot(seen != 255)) {
-#pragma unroll
-        for (int part = 0; part < kParts; ++part) odd |= R::has_odd(value[part]);
+      const bool partly = __ballot(seen != 255) != 0;
+      if (partly) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) s[t] = seen >> t & 1 ? s[t] : -INFINITY;
       }
       rows.weigh(s, p);
-      if (__ballot(odd)) {
 #pragma unroll
-        for (int part = 0; part < kParts; ++part) rows.add_odd_values(part, value[part], p);
-      } else {
-#pragma unroll
-        for (int part = 0; part < kParts; ++part) rows.add_values(part, value[part], p);
+      for (int part = 0; part < kParts; ++part) {
+        if (partly) {
+          const uint32_t odd = R::odd_positions(value[part]);
+          if (__ballot(odd)) {
+            rows.add_odd(part, value[part], p, odd, seen, n, g);
+            R::leave_out(value[part], odd);
+          }
+        }
+        rows.add_values(part, value[part], p);
       }
     }
 
@@ -799,11 +802,12 @@ template <int LOADS> __device__ inline void wait_for_all_but() {
   asm volatile("" ::: "memory");
 }
 
-template <typename CT, bool FLOAT, int DP, int WAVES, bool FULL>
+// MT: tiles of 16 rows of a wavefront.
+template <typename CT, bool FLOAT, int DP, int WAVES, int MT, bool FULL>
 __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend_shared(Args a) {
   typedef Rows<CT, FLOAT, DP> R;
   constexpr int kSteps = R::kSteps, kEach = R::kEach, kParts = R::kParts, kTerms = R::kTerms;
-  constexpr int kRows = 16 * WAVES;
+  constexpr int kRows = 16 * MT * WAVES;
   constexpr int kKeys = 2 * kSteps, kValues = DP == 64 ? 4 : 8 * kParts;   // fragments of a tile
   constexpr int kFragments = kKeys + kValues, kMine = kFragments / WAVES;  // that a wavefront fetches
   constexpr int kAhead = 3, kBuffers = kAhead + 1;
@@ -834,16 +838,19 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
     const int at = keys ? 8 * (n >> 2) : 8 * g;  // eight positions that lie on one page
     auto position = [&](int f) { return keys ? (n & 3) + 4 * (f / kSteps) : kEach == 8 ? f / kParts : 2 * f + (n >> 3); };
     auto dimension = [&](int f) { return within<FULL>(a, keys ? 32 * (f % kSteps) + 8 * g : kEach == 8 ? 128 * (f % kParts) + 8 * n : 8 * (n & 7), 8); };
-    R rows;
-    u4 query[kSteps][kTerms];
-    rows.begin(a, u, 16 * wave, n, g, query);
-    // (in registers now: a wait for these loads inside the loop would be one for all tiles that are on their way)
+    R rows[MT];
+    u4 query[MT][kSteps][kTerms];
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k)
+    for (int mt = 0; mt < MT; ++mt) {
+      rows[mt].begin(a, u, 16 * (MT * wave + mt), n, g, query[mt]);
+      // (in registers now: a wait for these loads inside the loop would be one for all tiles that are on their way)
 #pragma unroll
-      for (int t = 0; t < kTerms; ++t) asm volatile("" : "+v"(query[k][t]));
-    asm volatile("" : "+v"(rows.mask));
-    const bool idle = 16 * wave >= u.rows;  // no rows: fetches only
+      for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) asm volatile("" : "+v"(query[mt][k][t]));
+      asm volatile("" : "+v"(rows[mt].mask));
+    }
+    const bool idle = 16 * MT * wave >= u.rows;  // no rows: fetches only
 
     const int last_page = max(u.q.held - 1, 0) >> a.log2_page, in_page = (1 << a.log2_page) - 1, end = u.tile1;
     const int32_t* table = a.table + (int64_t)u.r * a.max_pages;
@@ -868,7 +875,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
         const int j0 = (tile - u.cached) * kTile + at;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-          const int64_t from = (u.q.first + min(j0 + position(fragment0 + i), u.q.fresh - 1)) * a.kv_stride + (int64_t)u.head * a.dim + dimension(fragment0 + i);
+          const int64_t from = row_at(u.q.first + min(j0 + position(fragment0 + i), u.q.fresh - 1), a.kv_stride) + u.head * a.dim + dimension(fragment0 + i);
           if constexpr (FLOAT) {
             // (these loads the compiler waits for, and with them for all that were made before)
             Eight<CT, FLOAT> e;
@@ -912,45 +919,71 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
       }
       fetch(next, into);
       if (!idle) {
-        f4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+        f4 x[MT][2];
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) R::add_score(lds.stage[buffer][k][lane], lds.stage[buffer][kSteps + k][lane], query[k], x);
-        float s[8];
-        u4 p[kTerms];
-        rows.exponents(x, s);
+        for (int mt = 0; mt < MT; ++mt) x[mt][0] = x[mt][1] = f4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+          const u4 lo = lds.stage[buffer][k][lane], hi = lds.stage[buffer][kSteps + k][lane];
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) R::add_score(lo, hi, query[mt][k], x[mt]);
+        }
         const bool is_new = tile >= u.cached;
         const int there = lds.seen[buffer][g];
-        const int seen = is_new ? rows.seen_new(a, u, (tile - u.cached) * kTile + 8 * g) : there;
-        const bool partly = __ballot(seen != 255) != 0;
+        uint32_t value[8][kEach / 2];
+        read_values(buffer, 0, value);  // (while the scores are worked out)
+        float s[MT][8];
+        u4 p[MT][kTerms];
+        bool whole = there == 255;
+        int seen[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          rows[mt].exponents(x[mt], s[mt]);
+          seen[mt] = is_new ? rows[mt].seen_new(a, u, (tile - u.cached) * kTile + 8 * g) : there;
+          whole &= seen[mt] == 255;
+        }
+        const bool partly = __ballot(!whole) != 0;
         if (partly) {
 #pragma unroll
-          for (int t = 0; t < 8; ++t) s[t] = seen >> t & 1 ? s[t] : -INFINITY;
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int t = 0; t < 8; ++t) s[mt][t] = seen[mt] >> t & 1 ? s[mt][t] : -INFINITY;
         }
-        rows.weigh(s, p);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) rows[mt].weigh(s[mt], p[mt]);
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-          bool odd = false;
-          uint32_t value[8][kEach / 2];
-          read_values(buffer, part, value);
+          if (part) read_values(buffer, part, value);
           if (partly) {
+            if (is_new) {
+              const uint32_t odd = R::odd_positions(value);
+              if (__ballot(odd)) {
 #pragma unroll
-            for (int t = 0; t < 8; ++t)
-#pragma unroll
-              for (int j = 0; j < kEach / 2; ++j) value[t][j] = there >> t & 1 ? value[t][j] : 0u;
-            if (is_new) odd = R::has_odd(value);
+                for (int mt = 0; mt < MT; ++mt) rows[mt].add_odd(part, value, p[mt], odd, seen[mt], n, g);
+                R::leave_out(value, odd);
+              }
+            } else {
+              R::leave_out(value, ~there);  // (what lies on a page behind the last token)
+            }
           }
-          if (__ballot(odd)) rows.add_odd_values(part, value, p);
-          else rows.add_values(part, value, p);
+#pragma unroll
+          for (int j = 0; j < kEach; ++j) {
+            const u4 v = R::column(value, j);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) rows[mt].add_column(part * kEach + j, v, p[mt]);
+          }
         }
       }
       buffer = buffer + 1 == kBuffers ? 0 : buffer + 1;
     }
     wait_for_all_but<0>();
 
-    const int in = 16 * wave + n;
-    if (in < u.rows) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int in = 16 * (MT * wave + mt) + n;
+      if (in >= u.rows) continue;
       float* const to = Partial<DP, kRows>::row(a, u.slot(u.piece), in);
-      if (u.pieces > 1 && g == 0) write_through(to + DP, rows.maximum(), rows.sum[0]);
+      if (u.pieces > 1 && g == 0) write_through(to + DP, rows[mt].maximum(), rows[mt].sum[0]);
 #pragma unroll
       for (int part = 0; part < kParts; ++part)
 #pragma unroll
@@ -959,8 +992,8 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
           for (int j = 0; j < kEach; j += 4) {
             const int d = part * 16 * kEach + kEach * (4 * g + i) + j;
             if (!FULL && d >= a.dim) continue;
-            if (u.pieces == 1) store<CT, FLOAT>(a, u, in, d, rows.four(part, i, j), rows.sum[0]);
-            else write_through(to + d, rows.four(part, i, j));
+            if (u.pieces == 1) store<CT, FLOAT>(a, u, in, d, rows[mt].four(part, i, j), rows[mt].sum[0]);
+            else write_through(to + d, rows[mt].four(part, i, j));
           }
     }
     if (u.pieces > 1) join<CT, FLOAT, DP, kRows, 64 * WAVES>(a, u, lds.joint);
@@ -985,6 +1018,7 @@ const char* fault_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads
 struct Shape {
   int dims;         // head_dim, padded
   int waves;        // of a workgroup of attend_shared, 0: attend_split
+  int row_tiles;    // of a wavefront of attend_shared
   int rows;         // of a workgroup
   int target;       // workgroups at most: those that the chip runs at once
   int64_t counters_bytes, bytes;  // of the workspace
@@ -994,9 +1028,11 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   Shape s;
   s.dims = cache->head_dim <= 64 ? 64 : cache->head_dim <= 128 ? 128 : 256;
   const int64_t rows = (int64_t)step->max_new * (heads / cache->kv_heads);
-  // (keys and values of 256 dimensions do not fit in the registers beside a result)
-  s.waves = rows <= 16 && s.dims < 256 ? 0 : rows <= 64 || s.dims == 256 || (floats && s.dims == 128) ? 4 : 8;
-  s.rows = s.waves ? 16 * s.waves : 16;
+  // (keys and values of 256 dimensions do not fit in the registers beside a result, nor do two tiles of rows of more than 64)
+  const bool two = !floats && s.dims == 64 && rows > 64;
+  s.waves = rows <= 16 && s.dims < 256 ? 0 : s.dims < 256 && rows > (two ? 128 : 64) && !(floats && s.dims == 128) ? 8 : 4;
+  s.row_tiles = two ? 2 : 1;
+  s.rows = s.waves ? 16 * s.waves * s.row_tiles : 16;
   s.target = s.waves == 4 && !floats && s.dims < 256 ? 512 : 256;
   s.counters_bytes = (int64_t)s.target * 4;
   s.bytes = s.counters_bytes + (int64_t)2 * s.target * s.rows * (s.dims + 4) * 4;
@@ -1004,12 +1040,15 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
 }
 
 template <typename CT, bool FLOAT, bool FULL> void (*kernel_of(const Shape& s))(Args) {
-  if (s.dims == 64) return !s.waves ? attend_split<CT, FLOAT, 64, FULL> : s.waves == 4 ? attend_shared<CT, FLOAT, 64, 4, FULL> : attend_shared<CT, FLOAT, 64, 8, FULL>;
-  if (s.dims == 256) return attend_shared<CT, FLOAT, 256, 4, FULL>;
+  if (s.dims == 256) return attend_shared<CT, FLOAT, 256, 4, 1, FULL>;
+  if (!s.waves) return s.dims == 64 ? attend_split<CT, FLOAT, 64, FULL> : attend_split<CT, FLOAT, 128, FULL>;
   if constexpr (!FLOAT) {
-    if (s.waves == 8) return attend_shared<CT, FLOAT, 128, 8, FULL>;
+    if (s.row_tiles == 2) return s.waves == 4 ? attend_shared<CT, FLOAT, 64, 4, 2, FULL> : attend_shared<CT, FLOAT, 64, 8, 2, FULL>;
+    if (s.waves == 8) return attend_shared<CT, FLOAT, 128, 8, 1, FULL>;
+  } else if (s.waves == 8) {
+    return attend_shared<CT, FLOAT, 64, 8, 1, FULL>;
   }
-  return s.waves ? attend_shared<CT, FLOAT, 128, 4, FULL> : attend_split<CT, FLOAT, 128, FULL>;
+  return s.dims == 64 ? attend_shared<CT, FLOAT, 64, 4, 1, FULL> : attend_shared<CT, FLOAT, 128, 4, 1, FULL>;
 }
 
 template <typename CT> void (*kernel_of(const Shape& s, bool floats, bool full))(Args) {
@@ -1041,13 +1080,14 @@ int rsr_tree_attention(const rsr_cache_t* cache, const rsr_step_t* step, const v
   if (!fault) fault = rsr_internal::fault_of_rows(k, kv_stride, kv_width, dtype);
   if (!fault) fault = rsr_internal::fault_of_rows(v, kv_stride, kv_width, dtype);
   if (!fault) fault = rsr_internal::fault_of_rows(out, out_stride, width, dtype);
+  if (!fault && (q_stride >> 31 || kv_stride >> 31 || out_stride >> 31)) fault = "strides must be below 2^31";
   if (!fault && (!workspace || !rsr_internal::aligned(workspace, 256) || workspace_bytes < s.bytes))
     fault = "the workspace is missing, too small or not 256-byte aligned";
   if (fault) return set_error(RSR_ERR_INVALID_ARGUMENT, fault);
   const int group = heads / cache->kv_heads;
   const Args a{q, k, v, out, static_cast<const uint16_t*>(cache->k), static_cast<const uint16_t*>(cache->v), step->table, step->held, step->start, step->mask,
                static_cast<uint32_t*>(workspace), reinterpret_cast<float*>(static_cast<char*>(workspace) + s.counters_bytes),
-               q_stride, kv_stride, out_stride, cache->head_stride, (uint32_t)cache->page_stride, (uint32_t)cache->token_stride, step->requests, step->tokens,
+               cache->head_stride, (uint32_t)q_stride, (uint32_t)kv_stride, (uint32_t)out_stride, (uint32_t)cache->page_stride, (uint32_t)cache->token_stride, step->requests, step->tokens,
                step->max_new, step->max_pages, rsr_internal::log2_of(cache->page_size), cache->pages, cache->kv_heads, cache->head_dim, group,
                group == 1 ? 0u : (uint32_t)(((uint64_t(1) << 32) + group - 1) / group), scale};
   const bool full = cache->head_dim == s.dims;
