@@ -386,10 +386,10 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
   }
 
   // Of eight positions the dimension that is number j of the lane's piece.
-  static __device__ u4 column(const uint32_t (&value)[8][kEach / 2], int j, uint32_t even = 0x05040100, uint32_t odd = 0x07060302) {
+  static __device__ u4 column(const uint32_t (&value)[8][kEach / 2], int j) {
     u4 x;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) x[t] = __builtin_amdgcn_perm(value[2 * t + 1][j >> 1], value[2 * t][j >> 1], j & 1 ? odd : even);
+    for (int t = 0; t < 4; ++t) x[t] = __builtin_amdgcn_perm(value[2 * t + 1][j >> 1], value[2 * t][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
     return x;
   }
   __device__ void add_column(int at, u4 x, const u4 (&p)[kTerms]) {
@@ -407,8 +407,7 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
     return (a.mask ? (int)(mask >> min(j0, 63)) & 255 : eight_bits(token + 1 - j0)) & eight_bits(u.q.fresh - j0);
   }
 
-  // A value that is not finite must not reach the rows that do not see it (0 times infinity is NaN).  Which of the lane's eight
-  // positions have one?
+  // Which of the lane's eight positions have a value that is not finite?
   static __device__ uint32_t odd_positions(const uint32_t (&value)[8][kEach / 2]) {
     typedef uint16_t us2 __attribute__((ext_vector_type(2)));
     uint32_t odd = 0;
@@ -421,33 +420,21 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
     }
     return odd;
   }
-  // These positions, one after the other, each as a product of its own that only the rows that see it take (seldom needed: a loop,
-  // and few registers).  Of the operands of a float weight the small ones make no infinite value what it is not.
-  __device__ void add_odd(int part, const uint32_t (&value)[8][kEach / 2], const u4 (&p)[kTerms], uint32_t odd, int seen, int n, int g) {
-    for (int t = 0; t < kTile; ++t) {
-      const bool mine = g == t >> 3 && odd >> (t & 7) & 1;
-      if (!__ballot(mine)) continue;
-      const bool sees = __shfl(seen, (t & ~7) * 2 + n) >> (t & 7) & 1;
-      const uint32_t even_halves = hidden(0x05040100), odd_halves = hidden(0x07060302);
-      u4 only;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) only[k] = mine && (t & 7) >> 1 == k ? (t & 1 ? 0xffff0000u : 0xffffu) : 0u;
-#pragma unroll
-      for (int j = 0; j < kEach; ++j)
-#pragma unroll
-        for (int k = 0; k < kTerms; ++k) {
-          const f4 x = Half<CT>::mfma(column(value, j, even_halves, odd_halves) & only, p[k], f4{0, 0, 0, 0});
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[part * kEach + j][i] += sees && (k == 0 || fabsf(x[i]) < INFINITY) ? x[i] : 0.f;
-        }
-    }
-  }
-  // And they are left out of what all rows take.
-  static __device__ void leave_out(uint32_t (&value)[8][kEach / 2], uint32_t odd) {
+  // What is not finite becomes zero, in positions that have such a value.
+  static __device__ void take_out(uint32_t (&value)[8][kEach / 2], uint32_t odd) {
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
-      for (int j = 0; j < kEach / 2; ++j) value[t][j] = odd >> t & 1 ? 0u : value[t][j];
+      for (int j = 0; j < kEach / 2; ++j) {
+        const uint32_t x = value[t][j], e = Half<CT>::kExponent;
+        value[t][j] = odd >> t & 1 ? x & ((x & e) == e ? 0xffff0000u : ~0u) & ((x >> 16 & e) == e ? 0xffffu : ~0u) : x;
+      }
+  }
+  static __device__ void leave_out(uint32_t (&value)[8][kEach / 2], uint32_t positions) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+#pragma unroll
+      for (int j = 0; j < kEach / 2; ++j) value[t][j] = positions >> t & 1 ? 0u : value[t][j];
   }
 
   __device__ float maximum() const { return limit == kLimit ? base + kBias : -INFINITY; }
@@ -559,6 +546,41 @@ template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inl
   }
 }
 
+// A value that is not finite must not reach the rows that do not see it, and a product would bring it there (0 times infinity is
+// NaN).  In tiles of new tokens that some rows see in part it is taken out of the products, and added here, with whatever weight,
+// to the rows that do see it: to what the workgroup has written of them, for the new tokens number j0 .. j1-1.
+template <typename CT, bool FLOAT, int DP, int ROWS> __device__ inline void add_odd_values(const Args& a, const Unit& u, int threads) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  const int j0 = max(u.tile0 - u.cached, 0) * kTile, j1 = min((u.tile1 - u.cached) * kTile, u.q.fresh), quarters = a.dim / 4;
+  for (int e = hidden(threadIdx.x); e < u.rows * quarters; e += threads) {
+    const int in = e / quarters, d = (e - in * quarters) * 4, row = u.row0 + in, token = token_of(a, row);
+    const uint64_t mask = a.mask ? a.mask[u.q.first + token] : 0;
+    f4 add{0, 0, 0, 0};
+    for (int j = j0; j < j1; ++j) {
+      if (!(a.mask ? mask >> j & 1 : j <= token)) continue;
+      const int64_t from = row_at(u.q.first + j, a.kv_stride) + u.head * a.dim + d;
+      for (int i = 0; i < 4; ++i) {
+        float x;
+        if constexpr (FLOAT) x = (float)(CT)static_cast<const float*>(a.v)[from + i];
+        else x = (float)static_cast<const CT*>(a.v)[from + i];
+        if (!(fabsf(x) < INFINITY)) add[i] += x;
+      }
+    }
+    if (u.pieces > 1) {
+      float* const to = Partial<DP, ROWS>::row(a, u.slot(u.piece), in) + d;
+      const f2 lo = read_through(to), hi = read_through(to + 2);
+      write_through(to, f4{lo[0], lo[1], hi[0], hi[1]} + add);
+    } else {
+      const int64_t to = row_at(u.q.first + token, a.out_stride) + (u.head * a.group + row - token * a.group) * a.dim + d;
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (FLOAT) static_cast<float*>(a.out)[to + i] += add[i];
+        else static_cast<CT*>(a.out)[to + i] = (CT)((float)static_cast<CT*>(a.out)[to + i] + add[i]);
+      }
+    }
+  }
+}
+
 // ---- few rows: the wavefronts split the positions -----------------------------------------------------------
 template <typename CT, bool FLOAT, int DP, bool FULL>
 __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
@@ -569,6 +591,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
   __shared__ __align__(16) float joined[kWaves][16][kLine];
   __shared__ __align__(16) u4 queries[FLOAT ? kSteps : 1][FLOAT ? kTerms : 1][64];  // the operands of floats fill too many registers
   __shared__ Joint<kThreads> joint;
+  __shared__ uint32_t any_odd;  // a value that is not finite was taken out of a product
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Plan<kRows> plan(a, threadIdx.x & 63);
 
@@ -579,6 +602,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
   while (at_tile < stop) {
     const int tid = hidden(threadIdx.x), lane = tid & 63, n = lane & 15, g = lane >> 4;
     const Unit u = plan.next(a, at_tile, stop);
+    if (tid == 0) any_odd = 0;
+    __syncthreads();
     const int t0 = u.tile0 + (u.tile1 - u.tile0) * wave / kWaves, t1 = u.tile0 + (u.tile1 - u.tile0) * (wave + 1) / kWaves;
     R rows;
     u4 query[kSteps][kTerms];
@@ -734,8 +759,8 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
         if (partly) {
           const uint32_t odd = R::odd_positions(value[part]);
           if (__ballot(odd)) {
-            rows.add_odd(part, value[part], p, odd, seen, n, g);
-            R::leave_out(value[part], odd);
+            R::take_out(value[part], odd);
+            any_odd = 1;
           }
         }
         rows.add_values(part, value[part], p);
@@ -777,6 +802,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
         if (d == 0) write_through(to + DP, all_m[in], all_l[in]);
       }
     }
+    if (any_odd) add_odd_values<CT, FLOAT, DP, kRows>(a, u, kThreads);
     if (u.pieces > 1) join<CT, FLOAT, DP, kRows, kThreads>(a, u, joint);
     __syncthreads();
   }
@@ -789,11 +815,11 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
 // after one to two microseconds, a tile's products take a third of that.
 constexpr int kWindow = 512;  // entries of a request's table in LDS
 
-// 16 bytes per lane from memory to the kilobyte of LDS at `to`.  The compiler does not know that LDS changes: wait_for_all_but waits
-// for it.  (Known to the compiler, every read of LDS would wait for all such loads.)
+// 16 bytes per lane from memory to the kilobyte of LDS at `to`, a place that nothing reads before wait_for_all_but has waited.  (The
+// compiler is not told that LDS changes: every read of LDS would wait for all such loads.)
 __device__ inline void to_lds(const void* from, uint32_t to) {
   uint32_t m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0" : "=&s"(m0) : "v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "memory");
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0" : "=&s"(m0) : "v"(from), "s"(__builtin_amdgcn_readfirstlane(to)));
 }
 // Until all but the last LOADS loads of the wavefront are done, and what it reads from and writes to LDS; then all wavefronts.
 template <int LOADS> __device__ inline void wait_for_all_but() {
@@ -817,6 +843,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
     int32_t seen[kBuffers][4];  // which of eight positions there are
     int32_t pages[kWindow];
     Joint<64 * WAVES> joint;
+    uint32_t any_odd;  // a value that is not finite was taken out of a product
   };
   __shared__ __align__(1024) Lds lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -904,6 +931,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
     };
 
     fill_window();
+    if (tid == 0) lds.any_odd = 0;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // from here on only tiles are on their way
     __syncthreads();
 #pragma unroll
@@ -958,9 +986,8 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
             if (is_new) {
               const uint32_t odd = R::odd_positions(value);
               if (__ballot(odd)) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) rows[mt].add_odd(part, value, p[mt], odd, seen[mt], n, g);
-                R::leave_out(value, odd);
+                R::take_out(value, odd);
+                lds.any_odd = 1;
               }
             } else {
               R::leave_out(value, ~there);  // (what lies on a page behind the last token)
@@ -996,6 +1023,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
             else write_through(to + d, rows[mt].four(part, i, j));
           }
     }
+    if (lds.any_odd) add_odd_values<CT, FLOAT, DP, kRows>(a, u, 64 * WAVES);
     if (u.pieces > 1) join<CT, FLOAT, DP, kRows, 64 * WAVES>(a, u, lds.joint);
     __syncthreads();
   }
@@ -1029,7 +1057,7 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   s.dims = cache->head_dim <= 64 ? 64 : cache->head_dim <= 128 ? 128 : 256;
   const int64_t rows = (int64_t)step->max_new * (heads / cache->kv_heads);
   // (keys and values of 256 dimensions do not fit in the registers beside a result, nor do two tiles of rows of more than 64)
-  const bool two = !floats && s.dims == 64 && rows > 64;
+  const bool two = !floats && s.dims < 256 && rows > 64;
   s.waves = rows <= 16 && s.dims < 256 ? 0 : s.dims < 256 && rows > (two ? 128 : 64) && !(floats && s.dims == 128) ? 8 : 4;
   s.row_tiles = two ? 2 : 1;
   s.rows = s.waves ? 16 * s.waves * s.row_tiles : 16;
@@ -1043,8 +1071,10 @@ template <typename CT, bool FLOAT, bool FULL> void (*kernel_of(const Shape& s))(
   if (s.dims == 256) return attend_shared<CT, FLOAT, 256, 4, 1, FULL>;
   if (!s.waves) return s.dims == 64 ? attend_split<CT, FLOAT, 64, FULL> : attend_split<CT, FLOAT, 128, FULL>;
   if constexpr (!FLOAT) {
-    if (s.row_tiles == 2) return s.waves == 4 ? attend_shared<CT, FLOAT, 64, 4, 2, FULL> : attend_shared<CT, FLOAT, 64, 8, 2, FULL>;
-    if (s.waves == 8) return attend_shared<CT, FLOAT, 128, 8, 1, FULL>;
+    if (s.row_tiles == 2) {
+      if (s.dims == 64) return s.waves == 4 ? attend_shared<CT, FLOAT, 64, 4, 2, FULL> : attend_shared<CT, FLOAT, 64, 8, 2, FULL>;
+      return s.waves == 4 ? attend_shared<CT, FLOAT, 128, 4, 2, FULL> : attend_shared<CT, FLOAT, 128, 8, 2, FULL>;
+    }
   } else if (s.waves == 8) {
     return attend_shared<CT, FLOAT, 64, 8, 1, FULL>;
   }
