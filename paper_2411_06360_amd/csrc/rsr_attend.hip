@@ -453,10 +453,22 @@ template <typename CT, bool FLOAT> __device__ inline void store(const Args& a, c
   else *reinterpret_cast<u2*>(static_cast<uint16_t*>(a.out) + to) = u2{pair_of<CT>(o[0], o[1]), pair_of<CT>(o[2], o[3])};
 }
 
-// A piece in the workspace: of every row DP values, their maximum and their sum of weights.
-template <int DP, int ROWS> struct Partial {
-  static constexpr int kRow = DP + 4, kPiece = ROWS * kRow;
-  static __device__ float* row(const Args& a, int slot, int in) { return a.partial + (int64_t)slot * kPiece + in * kRow; }
+// A piece in the workspace: its values in the order in which lanes hold them, so that a wavefront writes and reads whole lines (pairs of
+// floats, 512 bytes for 64 lanes), then a maximum and a sum of weights for every row.
+//   SPLIT  lane e % (16 * DP / 4) of attend_split has the four values e of rows of DP / 4
+//   else   a wavefront of attend_shared has 16 rows as in Rows: pair r of lane (n, g) are the values i and i + 1 of acc[r / 2]
+template <int DP, int ROWS, bool SPLIT> struct Partial {
+  static constexpr int kPiece = ROWS * (DP + 2);
+  static __device__ float* of(const Args& a, int slot) { return a.partial + (int64_t)slot * kPiece; }
+  static __device__ float* fours(float* piece, int e, int half) { return piece + (half * (ROWS * DP / 4) + e) * 2; }
+  static __device__ float* pair(float* piece, int tile, int r, int lane) { return piece + ((tile * (DP / 8) + r) * 64 + lane) * 2; }
+  static __device__ float* sums(float* piece, int in) { return piece + ROWS * DP + 2 * in; }
+  static __device__ float* value(float* piece, int in, int d) {
+    if constexpr (SPLIT) return fours(piece, in * (DP / 4) + d / 4, d >> 1 & 1) + (d & 1);
+    constexpr int kEach = DP / 16 < 8 ? DP / 16 : 8;
+    const int part = d / (16 * kEach), rest = d % (16 * kEach), j = rest % kEach, i = rest / kEach % 4, g = rest / kEach / 4;
+    return pair(piece, in / 16, (part * kEach + j) * 2 + i / 2, in % 16 + 16 * g) + (i & 1);
+  }
 };
 
 // Writes of a piece go past the L2 of the XCD, to where all XCDs read: no write-back of a whole L2 has to follow them.
@@ -464,7 +476,6 @@ __device__ inline void write_through(float* to, float x, float y) {
   __hip_atomic_store(reinterpret_cast<uint64_t*>(to), __builtin_bit_cast(uint64_t, u2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)}),
                      __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ inline void write_through(float* to, f4 x) { write_through(to, x[0], x[1]), write_through(to + 2, x[2], x[3]); }
 
 // And they are read past the caches, which may hold what was there before.
 __device__ inline f2 read_through(const float* from) {
@@ -479,6 +490,18 @@ __device__ inline float behind(float m, float top) { return m == -INFINITY ? 0.f
 // waits until its writes, which go through all caches, are done, then the workgroup counts itself.  (A release and an acquire
 // instead would write back and drop a whole L2 each, 0.1 and 0.3 us for every workgroup, one after the other.)  Bound by the latency of these reads: a lane has eight pieces of its four values under way at once,
 // and lanes that are left over take a share of the pieces.
+__device__ inline bool all_arrived(const Args& a, const Unit& u, uint32_t& arrived) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    arrived = __hip_atomic_fetch_add(&a.counters[u.counter], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (arrived == (uint32_t)u.pieces - 1) __hip_atomic_store(&a.counters[u.counter], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  return arrived == (uint32_t)u.pieces - 1;
+}
+
+// attend_split: a lane has four values of a row.
 template <int THREADS> struct Joint {
   f4 part[THREADS];
   float m[THREADS], l[THREADS];
@@ -487,51 +510,44 @@ template <int THREADS> struct Joint {
 
 template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inline void join(const Args& a, const Unit& u, Joint<THREADS>& lds) {
   constexpr int kAtOnce = 8;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  const int tid = hidden(threadIdx.x);
-  if (tid == 0) lds.arrived = __hip_atomic_fetch_add(&a.counters[u.counter], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  if (lds.arrived != (uint32_t)u.pieces - 1) return;
-  if (tid == 0) __hip_atomic_store(&a.counters[u.counter], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  typedef Partial<DP, ROWS> P;
-  const int items = u.rows * (DP / 4), shares = items < THREADS ? THREADS / items : 1;
-  for (int e0 = 0; e0 < items; e0 += THREADS) {
-    const int share = shares > 1 ? tid / items : 0, e = e0 + tid - share * items, in = e / (DP / 4), d = e % (DP / 4) * 4;
-    const bool there = e < items && d < a.dim && share < shares;
-    f4 x{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.f;
-    if (there) {
-      const float* const from = P::row(a, 0, in);
-      for (int c0 = share; c0 < u.pieces; c0 += kAtOnce * shares) {
-        f4 xc[kAtOnce];
-        f2 mlc[kAtOnce];
-        float top = m;
+  if (!all_arrived(a, u, lds.arrived)) return;
+  typedef Partial<DP, ROWS, true> P;
+  const int tid = hidden(threadIdx.x), items = u.rows * (DP / 4), shares = items < THREADS ? THREADS / items : 1;
+  const int share = tid / items, e = tid - share * items, in = e / (DP / 4), d = e % (DP / 4) * 4;
+  static_assert(ROWS * (DP / 4) <= THREADS);
+  const bool there = d < a.dim && share < shares;
+  f4 x{0, 0, 0, 0};
+  float m = -INFINITY, l = 0.f;
+  if (there) {
+    for (int c0 = share; c0 < u.pieces; c0 += kAtOnce * shares) {
+      f4 xc[kAtOnce];
+      f2 mlc[kAtOnce];
+      float top = m;
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-          const float* const p = from + (int64_t)u.slot(min(c0 + k * shares, u.pieces - 1)) * P::kPiece;
-          const f2 lo = read_through(p + d), hi = read_through(p + d + 2);
-          xc[k] = f4{lo[0], lo[1], hi[0], hi[1]}, mlc[k] = read_through(p + DP);
-        }
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-          if (c0 + k * shares >= u.pieces) mlc[k] = f2{-INFINITY, 0.f};
-          top = fmaxf(top, mlc[k][0]);
-        }
-        const float back = behind(m, top);
-        x *= back, l = m == -INFINITY ? l : l * back;
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-          const float w = behind(mlc[k][0], top);
-          x += xc[k] * w, l += mlc[k][0] == -INFINITY ? mlc[k][1] : mlc[k][1] * w;  // (without a maximum: 0, or NaN)
-        }
-        m = top;
+      for (int k = 0; k < kAtOnce; ++k) {
+        float* const piece = P::of(a, u.slot(min(c0 + k * shares, u.pieces - 1)));
+        const f2 lo = read_through(P::fours(piece, e, 0)), hi = read_through(P::fours(piece, e, 1));
+        xc[k] = f4{lo[0], lo[1], hi[0], hi[1]}, mlc[k] = read_through(P::sums(piece, in));
       }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        if (c0 + k * shares >= u.pieces) mlc[k] = f2{-INFINITY, 0.f};
+        top = fmaxf(top, mlc[k][0]);
+      }
+      const float back = behind(m, top);
+      x *= back, l = m == -INFINITY ? l : l * back;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const float w = behind(mlc[k][0], top);
+        x += xc[k] * w, l += mlc[k][0] == -INFINITY ? mlc[k][1] : mlc[k][1] * w;  // (without a maximum: 0, or NaN)
+      }
+      m = top;
     }
-    if (shares > 1) {
-      lds.part[tid] = x, lds.m[tid] = m, lds.l[tid] = l;
-      __syncthreads();
-      if (tid >= items) continue;
+  }
+  if (shares > 1) {
+    lds.part[tid] = x, lds.m[tid] = m, lds.l[tid] = l;
+    __syncthreads();
+    if (tid < items) {
       float top = m;
       for (int w = 1; w < shares; ++w) top = fmaxf(top, lds.m[w * items + tid]);
       const float back = behind(m, top);
@@ -542,14 +558,14 @@ template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inl
         x += lds.part[at] * by, l += mw == -INFINITY ? lw : lw * by;
       }
     }
-    if (there) store<CT, FLOAT>(a, u, in, d, x, l);
   }
+  if (there && tid < items) store<CT, FLOAT>(a, u, in, d, x, l);
 }
 
 // A value that is not finite must not reach the rows that do not see it, and a product would bring it there (0 times infinity is
 // NaN).  In tiles of new tokens that some rows see in part it is taken out of the products, and added here, with whatever weight,
 // to the rows that do see it: to what the workgroup has written of them, for the new tokens number j0 .. j1-1.
-template <typename CT, bool FLOAT, int DP, int ROWS> __device__ inline void add_odd_values(const Args& a, const Unit& u, int threads) {
+template <typename CT, bool FLOAT, int DP, int ROWS, bool SPLIT> __device__ inline void add_odd_values(const Args& a, const Unit& u, int threads) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   const int j0 = max(u.tile0 - u.cached, 0) * kTile, j1 = min((u.tile1 - u.cached) * kTile, u.q.fresh), quarters = a.dim / 4;
@@ -568,9 +584,11 @@ template <typename CT, bool FLOAT, int DP, int ROWS> __device__ inline void add_
       }
     }
     if (u.pieces > 1) {
-      float* const to = Partial<DP, ROWS>::row(a, u.slot(u.piece), in) + d;
-      const f2 lo = read_through(to), hi = read_through(to + 2);
-      write_through(to, f4{lo[0], lo[1], hi[0], hi[1]} + add);
+      for (int i = 0; i < 4; ++i) {
+        float* const to = Partial<DP, ROWS, SPLIT>::value(Partial<DP, ROWS, SPLIT>::of(a, u.slot(u.piece)), in, d + i);
+        const float x = __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(to, x + add[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
     } else {
       const int64_t to = row_at(u.q.first + token, a.out_stride) + (u.head * a.group + row - token * a.group) * a.dim + d;
       for (int i = 0; i < 4; ++i) {
@@ -587,6 +605,7 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
   typedef Rows<CT, FLOAT, DP> R;
   constexpr int kRows = 16, kSteps = R::kSteps, kEach = R::kEach, kParts = R::kParts, kTerms = R::kTerms;
   constexpr int kLine = DP + 4;  // floats between rows in LDS
+  typedef Partial<DP, kRows, true> P;
   __shared__ float row_m[kWaves][kRows], row_l[kWaves][kRows], all_m[kRows], all_l[kRows];
   __shared__ __align__(16) float joined[kWaves][16][kLine];
   __shared__ __align__(16) u4 queries[FLOAT ? kSteps : 1][FLOAT ? kTerms : 1][64];  // the operands of floats fill too many registers
@@ -797,12 +816,13 @@ __global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
       if (u.pieces == 1) {
         store<CT, FLOAT>(a, u, in, d, x, all_l[in]);
       } else {
-        float* to = Partial<DP, kRows>::row(a, u.slot(u.piece), in);
-        write_through(to + d, x);
-        if (d == 0) write_through(to + DP, all_m[in], all_l[in]);
+        float* const piece = P::of(a, u.slot(u.piece));
+        write_through(P::fours(piece, e, 0), x[0], x[1]);
+        write_through(P::fours(piece, e, 1), x[2], x[3]);
+        if (d == 0) write_through(P::sums(piece, in), all_m[in], all_l[in]);
       }
     }
-    if (any_odd) add_odd_values<CT, FLOAT, DP, kRows>(a, u, kThreads);
+    if (any_odd) add_odd_values<CT, FLOAT, DP, kRows, true>(a, u, kThreads);
     if (u.pieces > 1) join<CT, FLOAT, DP, kRows, kThreads>(a, u, joint);
     __syncthreads();
   }
@@ -842,7 +862,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
     u4 stage[kBuffers][kFragments][64];
     int32_t seen[kBuffers][4];  // which of eight positions there are
     int32_t pages[kWindow];
-    Joint<64 * WAVES> joint;
+    uint32_t arrived;
     uint32_t any_odd;  // a value that is not finite was taken out of a product
   };
   __shared__ __align__(1024) Lds lds;
@@ -1005,26 +1025,61 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
     }
     wait_for_all_but<0>();
 
+    auto store_rows = [&] {
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int in = 16 * (MT * wave + mt) + n;
-      if (in >= u.rows) continue;
-      float* const to = Partial<DP, kRows>::row(a, u.slot(u.piece), in);
-      if (u.pieces > 1 && g == 0) write_through(to + DP, rows[mt].maximum(), rows[mt].sum[0]);
+      for (int mt = 0; mt < MT; ++mt) {
+        const int in = 16 * (MT * wave + mt) + n;
+        if (in >= u.rows) continue;
 #pragma unroll
-      for (int part = 0; part < kParts; ++part)
+        for (int part = 0; part < kParts; ++part)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < kEach; j += 4) {
-            const int d = part * 16 * kEach + kEach * (4 * g + i) + j;
-            if (!FULL && d >= a.dim) continue;
-            if (u.pieces == 1) store<CT, FLOAT>(a, u, in, d, rows[mt].four(part, i, j), rows[mt].sum[0]);
-            else write_through(to + d, rows[mt].four(part, i, j));
-          }
+            for (int j = 0; j < kEach; j += 4) {
+              const int d = part * 16 * kEach + kEach * (4 * g + i) + j;
+              if (FULL || d < a.dim) store<CT, FLOAT>(a, u, in, d, rows[mt].four(part, i, j), rows[mt].sum[0]);
+            }
+      }
+    };
+    typedef Partial<DP, kRows, false> P;
+    if (u.pieces == 1) {
+      store_rows();
+    } else if (!idle) {
+      float* const piece = P::of(a, u.slot(u.piece));
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        if (g == 0) write_through(P::sums(piece, 16 * (MT * wave + mt) + n), rows[mt].maximum(), rows[mt].sum[0]);
+#pragma unroll
+        for (int r = 0; r < DP / 8; ++r) write_through(P::pair(piece, MT * wave + mt, r, lane), rows[mt].acc[r / 2][r % 2 * 2], rows[mt].acc[r / 2][r % 2 * 2 + 1]);
+      }
     }
-    if (lds.any_odd) add_odd_values<CT, FLOAT, DP, kRows>(a, u, 64 * WAVES);
-    if (u.pieces > 1) join<CT, FLOAT, DP, kRows, 64 * WAVES>(a, u, lds.joint);
+    if (lds.any_odd) add_odd_values<CT, FLOAT, DP, kRows, false>(a, u, 64 * WAVES);
+    if (u.pieces > 1 && all_arrived(a, u, lds.arrived) && !idle) {
+      // a lane takes up the pieces of the values that it has itself
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const int tile = MT * wave + mt;
+        float m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int j = 0; j < kParts * kEach; ++j) rows[mt].acc[j] = f4{0, 0, 0, 0};
+        for (int c = 0; c < u.pieces; ++c) {
+          float* const from = P::of(a, u.slot(c));
+          const f2 ml = read_through(P::sums(from, 16 * tile + n));
+          f2 x[DP / 8];
+#pragma unroll
+          for (int r = 0; r < DP / 8; ++r) x[r] = read_through(P::pair(from, tile, r, lane));
+          const float top = fmaxf(m, ml[0]), back = behind(m, top), by = behind(ml[0], top);
+          l = (m == -INFINITY ? l : l * back) + (ml[0] == -INFINITY ? ml[1] : ml[1] * by);  // (without a maximum: 0, or NaN)
+          m = top;
+#pragma unroll
+          for (int r = 0; r < DP / 8; ++r)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) rows[mt].acc[r / 2][r % 2 * 2 + i] = rows[mt].acc[r / 2][r % 2 * 2 + i] * back + x[r][i] * by;
+        }
+        rows[mt].sum[0] = l;
+      }
+      store_rows();
+    }
     __syncthreads();
   }
 }
@@ -1063,7 +1118,7 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   s.rows = s.waves ? 16 * s.waves * s.row_tiles : 16;
   s.target = s.waves == 4 && !floats && s.dims < 256 ? 512 : 256;
   s.counters_bytes = (int64_t)s.target * 4;
-  s.bytes = s.counters_bytes + (int64_t)2 * s.target * s.rows * (s.dims + 4) * 4;
+  s.bytes = s.counters_bytes + (int64_t)2 * s.target * s.rows * (s.dims + 2) * 4;
   return s;
 }
 
