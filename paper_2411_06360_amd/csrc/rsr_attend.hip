@@ -850,13 +850,14 @@ template <int LOADS> __device__ inline void wait_for_all_but() {
 
 // MT: tiles of 16 rows of a wavefront.
 template <typename CT, bool FLOAT, int DP, int WAVES, int MT, bool FULL>
-__global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend_shared(Args a) {
+__global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(Args a) {
   typedef Rows<CT, FLOAT, DP> R;
   constexpr int kSteps = R::kSteps, kEach = R::kEach, kParts = R::kParts, kTerms = R::kTerms;
   constexpr int kRows = 16 * MT * WAVES;
   constexpr int kKeys = 2 * kSteps, kValues = DP == 64 ? 4 : 8 * kParts;   // fragments of a tile
   constexpr int kFragments = kKeys + kValues, kMine = kFragments / WAVES;  // that a wavefront fetches
   constexpr int kAhead = 3, kBuffers = kAhead + 1;
+  constexpr bool kEarly = !(FLOAT && DP == 128);  // values are read from LDS while scores are worked out, where registers allow it
   static_assert(kFragments % WAVES == 0);
   struct Lds {
     u4 stage[kBuffers][kFragments][64];
@@ -979,7 +980,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
         const bool is_new = tile >= u.cached;
         const int there = lds.seen[buffer][g];
         uint32_t value[8][kEach / 2];
-        read_values(buffer, 0, value);  // (while the scores are worked out)
+        if constexpr (kEarly) read_values(buffer, 0, value);
         float s[MT][8];
         u4 p[MT][kTerms];
         bool whole = there == 255;
@@ -1001,7 +1002,7 @@ __global__ void __launch_bounds__(64 * WAVES, FLOAT || DP == 256 ? 1 : 2) attend
         for (int mt = 0; mt < MT; ++mt) rows[mt].weigh(s[mt], p[mt]);
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-          if (part) read_values(buffer, part, value);
+          if (part || !kEarly) read_values(buffer, part, value);
           if (partly) {
             if (is_new) {
               const uint32_t odd = R::odd_positions(value);
@@ -1116,7 +1117,7 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   s.waves = rows <= 16 && s.dims < 256 ? 0 : s.dims < 256 && rows > (two ? 128 : 64) && !(floats && s.dims == 128) ? 8 : 4;
   s.row_tiles = two ? 2 : 1;
   s.rows = s.waves ? 16 * s.waves * s.row_tiles : 16;
-  s.target = s.waves == 4 && !floats && s.dims < 256 ? 512 : 256;
+  s.target = s.waves == 4 && s.dims < 256 ? 512 : 256;
   s.counters_bytes = (int64_t)s.target * 4;
   s.bytes = s.counters_bytes + (int64_t)2 * s.target * s.rows * (s.dims + 2) * 4;
   return s;
