@@ -856,7 +856,8 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
   constexpr int kRows = 16 * MT * WAVES;
   constexpr int kKeys = 2 * kSteps, kValues = DP == 64 ? 4 : 8 * kParts;   // fragments of a tile
   constexpr int kFragments = kKeys + kValues, kMine = kFragments / WAVES;  // that a wavefront fetches
-  constexpr int kAhead = 3, kBuffers = kAhead + 1;
+  // Eight wavefronts take two tiles between barriers: they lose less to each other (four, whose other workgroup fills in, lose registers).
+  constexpr int kBuffers = 4, kTogether = WAVES == 8 ? 2 : 1, kAhead = kBuffers - kTogether;
   constexpr bool kEarly = !(FLOAT && DP == 128);  // values are read from LDS while scores are worked out, where registers allow it
   static_assert(kFragments % WAVES == 0);
   struct Lds {
@@ -957,17 +958,18 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fetch(min(u.tile0 + i, end - 1), i);  // (the last tile again instead of none: the count of loads stays)
-    int buffer = 0;
-    for (int tile = u.tile0; tile < end; ++tile) {
-      wait_for_all_but<(kAhead - 1) * kMine>();  // the tile is there, and all are done with the one before
-      const int next = min(tile + kAhead, end - 1), into = buffer ? buffer - 1 : kBuffers - 1;
-      if (next < u.cached && ((next * kTile + kTile - 1) >> a.log2_page) - window >= kWindow) {
+    for (int first = u.tile0; first < end; first += kTogether) {
+      wait_for_all_but<(kAhead - kTogether) * kMine>();  // these tiles are there, and all are done with those before
+      const int next = min(first + kAhead, end - 1);
+      if (next < u.cached && ((min(next + kTogether, u.cached) * kTile - 1) >> a.log2_page) - window >= kWindow) {
         window = (next * kTile) >> a.log2_page;
         fill_window();
         __syncthreads();
       }
-      fetch(next, into);
-      if (!idle) {
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i) fetch(min(next + i, end - 1), (first - u.tile0 + kAhead + i) % kBuffers);
+      for (int tile = first; tile < min(first + kTogether, end) && !idle; ++tile) {
+        const int buffer = (tile - u.tile0) % kBuffers;
         f4 x[MT][2];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) x[mt][0] = x[mt][1] = f4{0, 0, 0, 0};
@@ -1022,7 +1024,6 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
           }
         }
       }
-      buffer = buffer + 1 == kBuffers ? 0 : buffer + 1;
     }
     wait_for_all_but<0>();
 
@@ -1098,6 +1099,9 @@ const char* fault_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads
   return nullptr;
 }
 
+// The counters come first, at one place for calls of all shapes: what one leaves behind them no other takes for a count.
+constexpr int kMostGroups = 512, kCountersBytes = kMostGroups * 4;
+
 // The kernel for a call, and how it is launched.
 struct Shape {
   int dims;         // head_dim, padded
@@ -1105,7 +1109,7 @@ struct Shape {
   int row_tiles;    // of a wavefront of attend_shared
   int rows;         // of a workgroup
   int target;       // workgroups at most: those that the chip runs at once
-  int64_t counters_bytes, bytes;  // of the workspace
+  int64_t bytes;    // of the workspace
 };
 
 Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool floats) {
@@ -1117,9 +1121,8 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   s.waves = rows <= 16 && s.dims < 256 ? 0 : s.dims < 256 && rows > (two ? 128 : 64) && !(floats && s.dims == 128) ? 8 : 4;
   s.row_tiles = two ? 2 : 1;
   s.rows = s.waves ? 16 * s.waves * s.row_tiles : 16;
-  s.target = s.waves == 4 && s.dims < 256 ? 512 : 256;
-  s.counters_bytes = (int64_t)s.target * 4;
-  s.bytes = s.counters_bytes + (int64_t)2 * s.target * s.rows * (s.dims + 2) * 4;
+  s.target = s.waves == 4 && s.dims < 256 ? kMostGroups : kMostGroups / 2;
+  s.bytes = kCountersBytes + (int64_t)2 * s.target * s.rows * (s.dims + 2) * 4;
   return s;
 }
 
@@ -1172,7 +1175,7 @@ int rsr_tree_attention(const rsr_cache_t* cache, const rsr_step_t* step, const v
   if (fault) return set_error(RSR_ERR_INVALID_ARGUMENT, fault);
   const int group = heads / cache->kv_heads;
   const Args a{q, k, v, out, static_cast<const uint16_t*>(cache->k), static_cast<const uint16_t*>(cache->v), step->table, step->held, step->start, step->mask,
-               static_cast<uint32_t*>(workspace), reinterpret_cast<float*>(static_cast<char*>(workspace) + s.counters_bytes),
+               static_cast<uint32_t*>(workspace), reinterpret_cast<float*>(static_cast<char*>(workspace) + kCountersBytes),
                cache->head_stride, (uint32_t)q_stride, (uint32_t)kv_stride, (uint32_t)out_stride, (uint32_t)cache->page_stride, (uint32_t)cache->token_stride, step->requests, step->tokens,
                step->max_new, step->max_pages, rsr_internal::log2_of(cache->page_size), cache->pages, cache->kv_heads, cache->head_dim, group,
                group == 1 ? 0u : (uint32_t)(((uint64_t(1) << 32) + group - 1) / group), scale};

@@ -217,8 +217,9 @@ int rsr_cache_slots(const int32_t* held, const int32_t* add, int requests, int32
   if (free_left == free_count || (requests && (now == held || now == add || start == held || start == add)))
     return set_error(RSR_ERR_INVALID_ARGUMENT, "an output must not be an input");
   const SlotsArgs a{held, add, free_pages, free_count, table, free_left, slots, start, now, max_slots, requests, max_pages, rsr_internal::log2_of(page_size)};
-  const int64_t groups = (max_slots + kBatch - 1) / kBatch;
-  hipLaunchKernelGGL(slots_kernel, dim3((unsigned)(groups < 1 ? 1 : groups > 256 ? 256 : groups)), dim3(kSlotThreads), 0, static_cast<hipStream_t>(stream), a);
+  // two slots per lane: each is a search and two reads one after the other, and adding up the requests anew costs less than a third
+  const int64_t groups = (max_slots + 2 * kSlotThreads - 1) / (2 * kSlotThreads);
+  hipLaunchKernelGGL(slots_kernel, dim3((unsigned)(groups < 1 ? 1 : groups > 1024 ? 1024 : groups)), dim3(kSlotThreads), 0, static_cast<hipStream_t>(stream), a);
   return launched("rsr_cache_slots");
 }
 

@@ -284,6 +284,29 @@ def test_another_stream_and_a_graph():
         s.check()
 
 
+def test_calls_of_other_shapes_share_a_workspace():
+    """One after the other, as the layers and steps of a program do: few rows and many, heads of all sizes, cut into many pieces."""
+    shapes = [dict(held=[3000], new=[64], dim=128, act="bf16", cache="bf16", heads=8, kv_heads=1), dict(held=[5000, 900], new=[1, 2], dim=64, act="f32", cache="f16"),
+              dict(held=[4000], new=[9], dim=256, act="f16", cache="f16"), dict(held=[6000], new=[40], dim=64, act="bf16", cache="bf16"),
+              dict(held=[2500], new=[30], dim=128, act="f32", cache="bf16")]
+    steps = [Step(k.pop("held"), k.pop("new"), seed=28 + i, **k) for i, k in enumerate(shapes)]
+    want = [s.check().copy() for s in steps]
+    space = torch.zeros(max(s.workspace.numel() for s in steps), dtype=torch.uint8, device="cuda")
+    for turn in range(3):
+        for i in (0, 1, 2, 3, 4, 1, 0, 3, 2, 4)[turn:]:
+            say("shared workspace", turn, i)
+            steps[i].workspace = space
+            steps[i].out.fill_(float("nan"))
+            assert np.array_equal(steps[i].run(), want[i])
+
+
+@pytest.mark.parametrize("act,cache", [("bf16", "bf16"), ("f32", "f16")])
+def test_a_run_of_more_pages_than_lie_in_lds_at_once(act, cache):
+    """17 rows of 64 key heads over 1250 tiles each: a workgroup takes some 150 tiles, of four pages each."""
+    say("many pages", act, cache)
+    Step([40000], [17], heads=64, kv_heads=64, dim=8, act=act, cache=cache, page=8, seed=29).check()
+
+
 def refused(s, code=-1, **changes):
     for name, value in changes.items():
         setattr(s, name, value)
