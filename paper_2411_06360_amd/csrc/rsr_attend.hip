@@ -31,7 +31,6 @@ namespace {
 
 using rsr_internal::set_error;
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;  // of attend_split
 constexpr int kTile = 32;        // positions of a tile
 constexpr int kLeastTiles = 16;  // of a workgroup, unless a set has fewer
 constexpr float kBias = 7.f;     // weights are 2^(s - m + 7): as float16 they keep their bits down to 2^-21 of the largest
@@ -513,53 +512,54 @@ template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inl
   if (!all_arrived(a, u, lds.arrived)) return;
   typedef Partial<DP, ROWS, true> P;
   const int tid = hidden(threadIdx.x), items = u.rows * (DP / 4), shares = items < THREADS ? THREADS / items : 1;
-  const int share = tid / items, e = tid - share * items, in = e / (DP / 4), d = e % (DP / 4) * 4;
-  static_assert(ROWS * (DP / 4) <= THREADS);
-  const bool there = d < a.dim && share < shares;
-  f4 x{0, 0, 0, 0};
-  float m = -INFINITY, l = 0.f;
-  if (there) {
-    for (int c0 = share; c0 < u.pieces; c0 += kAtOnce * shares) {
-      f4 xc[kAtOnce];
-      f2 mlc[kAtOnce];
-      float top = m;
+  for (int e0 = 0; e0 < items; e0 += THREADS) {
+    const int share = shares > 1 ? tid / items : 0, e = e0 + tid - share * items, in = e / (DP / 4), d = e % (DP / 4) * 4;
+    const bool there = e < items && d < a.dim && share < shares;
+    f4 x{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.f;
+    if (there) {
+      for (int c0 = share; c0 < u.pieces; c0 += kAtOnce * shares) {
+        f4 xc[kAtOnce];
+        f2 mlc[kAtOnce];
+        float top = m;
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        float* const piece = P::of(a, u.slot(min(c0 + k * shares, u.pieces - 1)));
-        const f2 lo = read_through(P::fours(piece, e, 0)), hi = read_through(P::fours(piece, e, 1));
-        xc[k] = f4{lo[0], lo[1], hi[0], hi[1]}, mlc[k] = read_through(P::sums(piece, in));
-      }
+        for (int k = 0; k < kAtOnce; ++k) {
+          float* const piece = P::of(a, u.slot(min(c0 + k * shares, u.pieces - 1)));
+          const f2 lo = read_through(P::fours(piece, e, 0)), hi = read_through(P::fours(piece, e, 1));
+          xc[k] = f4{lo[0], lo[1], hi[0], hi[1]}, mlc[k] = read_through(P::sums(piece, in));
+        }
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        if (c0 + k * shares >= u.pieces) mlc[k] = f2{-INFINITY, 0.f};
-        top = fmaxf(top, mlc[k][0]);
-      }
-      const float back = behind(m, top);
-      x *= back, l = m == -INFINITY ? l : l * back;
+        for (int k = 0; k < kAtOnce; ++k) {
+          if (c0 + k * shares >= u.pieces) mlc[k] = f2{-INFINITY, 0.f};
+          top = fmaxf(top, mlc[k][0]);
+        }
+        const float back = behind(m, top);
+        x *= back, l = m == -INFINITY ? l : l * back;
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        const float w = behind(mlc[k][0], top);
-        x += xc[k] * w, l += mlc[k][0] == -INFINITY ? mlc[k][1] : mlc[k][1] * w;  // (without a maximum: 0, or NaN)
-      }
-      m = top;
-    }
-  }
-  if (shares > 1) {
-    lds.part[tid] = x, lds.m[tid] = m, lds.l[tid] = l;
-    __syncthreads();
-    if (tid < items) {
-      float top = m;
-      for (int w = 1; w < shares; ++w) top = fmaxf(top, lds.m[w * items + tid]);
-      const float back = behind(m, top);
-      x *= back, l = m == -INFINITY ? l : l * back;
-      for (int w = 1; w < shares; ++w) {
-        const int at = w * items + tid;
-        const float mw = lds.m[at], lw = lds.l[at], by = behind(mw, top);
-        x += lds.part[at] * by, l += mw == -INFINITY ? lw : lw * by;
+        for (int k = 0; k < kAtOnce; ++k) {
+          const float w = behind(mlc[k][0], top);
+          x += xc[k] * w, l += mlc[k][0] == -INFINITY ? mlc[k][1] : mlc[k][1] * w;  // (without a maximum: 0, or NaN)
+        }
+        m = top;
       }
     }
+    if (shares > 1) {
+      lds.part[tid] = x, lds.m[tid] = m, lds.l[tid] = l;
+      __syncthreads();
+      if (tid < items) {
+        float top = m;
+        for (int w = 1; w < shares; ++w) top = fmaxf(top, lds.m[w * items + tid]);
+        const float back = behind(m, top);
+        x *= back, l = m == -INFINITY ? l : l * back;
+        for (int w = 1; w < shares; ++w) {
+          const int at = w * items + tid;
+          const float mw = lds.m[at], lw = lds.l[at], by = behind(mw, top);
+          x += lds.part[at] * by, l += mw == -INFINITY ? lw : lw * by;
+        }
+      }
+    }
+    if (there && share == 0) store<CT, FLOAT>(a, u, in, d, x, l);
   }
-  if (there && tid < items) store<CT, FLOAT>(a, u, in, d, x, l);
 }
 
 // A value that is not finite must not reach the rows that do not see it, and a product would bring it there (0 times infinity is
@@ -600,8 +600,9 @@ template <typename CT, bool FLOAT, int DP, int ROWS, bool SPLIT> __device__ inli
 }
 
 // ---- few rows: the wavefronts split the positions -----------------------------------------------------------
-template <typename CT, bool FLOAT, int DP, bool FULL>
-__global__ void __launch_bounds__(kThreads, 2) attend_split(Args a) {
+template <typename CT, bool FLOAT, int DP, int WAVES, bool FULL>
+__global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
+  constexpr int kWaves = WAVES, kThreads = 64 * WAVES;
   typedef Rows<CT, FLOAT, DP> R;
   constexpr int kRows = 16, kSteps = R::kSteps, kEach = R::kEach, kParts = R::kParts, kTerms = R::kTerms;
   constexpr int kLine = DP + 4;  // floats between rows in LDS
@@ -1105,7 +1106,8 @@ constexpr int kMostGroups = 512, kCountersBytes = kMostGroups * 4;
 // The kernel for a call, and how it is launched.
 struct Shape {
   int dims;         // head_dim, padded
-  int waves;        // of a workgroup of attend_shared, 0: attend_split
+  bool shared;      // attend_shared
+  int waves;        // of a workgroup
   int row_tiles;    // of a wavefront of attend_shared
   int rows;         // of a workgroup
   int target;       // workgroups at most: those that the chip runs at once
@@ -1117,10 +1119,14 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   s.dims = cache->head_dim <= 64 ? 64 : cache->head_dim <= 128 ? 128 : 256;
   const int64_t rows = (int64_t)step->max_new * (heads / cache->kv_heads);
   // (keys and values of 256 dimensions do not fit in the registers beside a result, nor do two tiles of rows of more than 64)
-  const bool two = !floats && s.dims < 256 && rows > 64;
-  s.waves = rows <= 16 && s.dims < 256 ? 0 : s.dims < 256 && rows > (two ? 128 : 64) && !(floats && s.dims == 128) ? 8 : 4;
+  s.shared = rows > 16 || s.dims == 256;
+  const bool two = s.shared && !floats && s.dims < 256 && rows > 64;
   s.row_tiles = two ? 2 : 1;
-  s.rows = s.waves ? 16 * s.waves * s.row_tiles : 16;
+  // attend_split: eight wavefronts, one workgroup per CU, make the fewest pieces of few sets; with a set for every other CU or more
+  // four are better, of which two workgroups per CU hide each other's waits (@@)
+  if (s.shared) s.waves = s.dims < 256 && rows > (two ? 128 : 64) && !(floats && s.dims == 128) ? 8 : 4;
+  else s.waves = (int64_t)step->requests * cache->kv_heads < 128 ? 8 : 4;
+  s.rows = s.shared ? 16 * s.waves * s.row_tiles : 16;
   s.target = s.waves == 4 && s.dims < 256 ? kMostGroups : kMostGroups / 2;
   s.bytes = kCountersBytes + (int64_t)2 * s.target * s.rows * (s.dims + 2) * 4;
   return s;
@@ -1128,7 +1134,10 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
 
 template <typename CT, bool FLOAT, bool FULL> void (*kernel_of(const Shape& s))(Args) {
   if (s.dims == 256) return attend_shared<CT, FLOAT, 256, 4, 1, FULL>;
-  if (!s.waves) return s.dims == 64 ? attend_split<CT, FLOAT, 64, FULL> : attend_split<CT, FLOAT, 128, FULL>;
+  if (!s.shared) {
+    if (s.waves == 8) return s.dims == 64 ? attend_split<CT, FLOAT, 64, 8, FULL> : attend_split<CT, FLOAT, 128, 8, FULL>;
+    return s.dims == 64 ? attend_split<CT, FLOAT, 64, 4, FULL> : attend_split<CT, FLOAT, 128, 4, FULL>;
+  }
   if constexpr (!FLOAT) {
     if (s.row_tiles == 2) {
       if (s.dims == 64) return s.waves == 4 ? attend_shared<CT, FLOAT, 64, 4, 2, FULL> : attend_shared<CT, FLOAT, 64, 8, 2, FULL>;
@@ -1187,7 +1196,7 @@ int rsr_tree_attention(const rsr_cache_t* cache, const rsr_step_t* step, const v
   const int64_t most = std::min((int64_t)s.target, (int64_t)step->requests * cache->kv_heads * blocks * ((tiles + kLeastTiles - 1) / kLeastTiles));
   if ((double)step->requests * cache->kv_heads * blocks * tiles >= 0x1p42)
     return set_error(RSR_ERR_UNSUPPORTED, "the tables could name more tokens than the kernels count");
-  hipLaunchKernelGGL(kern, dim3((unsigned)most), dim3(s.waves ? 64 * s.waves : kThreads), 0, static_cast<hipStream_t>(stream), a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)most), dim3(64 * s.waves), 0, static_cast<hipStream_t>(stream), a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(RSR_ERR_HIP, std::string("rsr_tree_attention: ") + hipGetErrorString(e));
   return RSR_OK;
