@@ -1114,6 +1114,11 @@ struct Shape {
   int64_t bytes;    // of the workspace
 };
 
+// of a request: as many as its row of the table can name, and the new ones
+int64_t most_tiles(const rsr_cache_t* cache, const rsr_step_t* step) {
+  return ((int64_t)step->max_pages * cache->page_size + kTile - 1) / kTile + (step->max_new + kTile - 1) / kTile;
+}
+
 Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool floats) {
   Shape s;
   s.dims = cache->head_dim <= 64 ? 64 : cache->head_dim <= 128 ? 128 : 256;
@@ -1122,10 +1127,12 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   s.shared = rows > 16 || s.dims == 256;
   const bool two = s.shared && !floats && s.dims < 256 && rows > 64;
   s.row_tiles = two ? 2 : 1;
-  // attend_split: eight wavefronts, one workgroup per CU, make the fewest pieces of few sets; with a set for every other CU or more
-  // four are better, of which two workgroups per CU hide each other's waits (@@)
+  // attend_split: four wavefronts, of which two workgroups per CU hide each other's waits.  Eight, one workgroup per CU, where few
+  // sets have so many tiles that they are cut into more pieces than there are CUs: half as many to join (20 heads of 128, 16
+  // tokens: 41 against 50 us over 16384 cached ones, but 19.1 against 17.5 us over 4096).
+  const int64_t sets = (int64_t)step->requests * cache->kv_heads;
   if (s.shared) s.waves = s.dims < 256 && rows > (two ? 128 : 64) && !(floats && s.dims == 128) ? 8 : 4;
-  else s.waves = (int64_t)step->requests * cache->kv_heads < 128 ? 8 : 4;
+  else s.waves = sets < 128 && sets * most_tiles(cache, step) > kMostGroups / 2 * kLeastTiles ? 8 : 4;
   s.rows = s.shared ? 16 * s.waves * s.row_tiles : 16;
   s.target = s.waves == 4 && s.dims < 256 ? kMostGroups : kMostGroups / 2;
   s.bytes = kCountersBytes + (int64_t)2 * s.target * s.rows * (s.dims + 2) * 4;
@@ -1192,7 +1199,7 @@ int rsr_tree_attention(const rsr_cache_t* cache, const rsr_step_t* step, const v
   auto kern = cache->dtype == RSR_F16 ? kernel_of<_Float16>(s, floats, full) : kernel_of<__bf16>(s, floats, full);
   // no more workgroups than there can be pieces
   const int64_t blocks = ((int64_t)step->max_new * group + s.rows - 1) / s.rows;
-  const int64_t tiles = (((int64_t)step->max_pages * cache->page_size) + kTile - 1) / kTile + (step->max_new + kTile - 1) / kTile;
+  const int64_t tiles = most_tiles(cache, step);
   const int64_t most = std::min((int64_t)s.target, (int64_t)step->requests * cache->kv_heads * blocks * ((tiles + kLeastTiles - 1) / kLeastTiles));
   if ((double)step->requests * cache->kv_heads * blocks * tiles >= 0x1p42)
     return set_error(RSR_ERR_UNSUPPORTED, "the tables could name more tokens than the kernels count");
