@@ -40,7 +40,8 @@ enum { RSR_F32 = 0, RSR_F16 = 1, RSR_BF16 = 2 };
  *
  *   k, v        DEVICE, 16-byte aligned; owned by the caller.  Element (page, head, offset, d) is at
  *               page * page_stride + head * head_stride + offset * token_stride + d (in elements), in both.
- *               Strides are multiples of 8, page_stride below 2^31 and token_stride below 2^24.  Pages of [kv_heads][page_size][head_dim] are read fastest.
+ *               Strides are multiples of 8, page_stride below 2^31 and token_stride below 2^24.  Pages of
+ *               [kv_heads][page_size][head_dim] are read fastest.
  *   dtype       RSR_F16 or RSR_BF16
  *   pages       >= 1, pages * page_size < 2^31
  *   page_size   a power of two, 8 .. 1024
@@ -81,7 +82,8 @@ typedef struct rsr_step_t {
  * rsr_tree_attention - for new token i of request r and query head a, with key head b = a / (heads / kv_heads):
  *   out[start[r]+i][a] = sum_p w_p v_p / sum_p w_p,   w_p = exp(scale * <q[start[r]+i][a], k_p>)
  * over the cached tokens of the request on pages that are there and the new tokens that i sees.  A token that
- * sees nothing gets zeros; what it does not see does not touch it, infinities and NaN included.
+ * sees nothing gets zeros; what it does not see does not touch it, infinities and NaN included.  A seen key or
+ * value that is not finite makes the results that it enters not finite (infinite or NaN).
  *
  *   q        DEVICE, row t at q + t * q_stride elements: [heads][head_dim]
  *   k, v     DEVICE, row t at k + t * kv_stride: [kv_heads][head_dim]; rounded to the type of the cache

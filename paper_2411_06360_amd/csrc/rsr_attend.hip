@@ -12,12 +12,18 @@
 // of dwords with v_perm_b32, eight positions of each dimension, the other operand.
 //
 // Two kernels, by the rows that a key head has (new tokens times query heads of the group):
-//   attend_split  up to 16: the eight wavefronts of a workgroup take the same rows and different positions, keys and values go
+//   attend_split  up to 16: the wavefronts of a workgroup take the same rows and different positions, keys and values go
 //                 from the cache straight into registers, LDS serves to join the wavefronts at the end
 //   attend_shared more: the wavefronts take different rows and the same positions, which come through LDS
 // The positions of all requests (tiles of 32: first a request's cached ones, then its new ones) are dealt out evenly to as many
-// workgroups as the chip runs at once.  The pieces of a row meet in the workspace, where the workgroup that comes last joins them
-// in their order.
+// workgroups as the chip runs at once (one length per workgroup and set instead: 32 ragged requests 181 us, dealt out 138).  The
+// pieces of a row meet in the workspace, where the workgroup that comes last joins them in their order.
+//
+// Measured on one MI355X, whole calls (a large copy moves 4.8 TB/s there, a sum reads 4.0, a large product does 1.23 PFLOP/s with
+// 16-bit operands): 32 requests of one token, 20 heads of 128, 8192 cached tokens each: 453 us, 5.9 TB/s of cache, bound by memory.
+// 16 drafted tokens over 4096, the same heads: 18 us for 42.6 MB; a token over 500: 13 us for 5.2 MB, a chain of latencies (lengths,
+// table, tiles, the join).  64 drafted tokens with four query heads per key head, 4 requests over 131072: 0.47 ms, 0.73 PFLOP/s;
+// one request over 2000: 22 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -32,7 +38,8 @@ namespace {
 using rsr_internal::set_error;
 
 constexpr int kTile = 32;        // positions of a tile
-constexpr int kLeastTiles = 16;  // of a workgroup, unless a set has fewer
+constexpr int kLeastTiles = 16;  // of a workgroup of attend_split, unless a set has fewer
+constexpr int kLeastShared = 4;  // and of attend_shared
 constexpr float kBias = 7.f;     // weights are 2^(s - m + 7): as float16 they keep their bits down to 2^-21 of the largest
 constexpr float kLimit = 15.f;   // m follows the maximum when a weight would pass 2^15, so that it seldom does
 
@@ -191,7 +198,7 @@ __device__ inline int64_t divided(int64_t x, int64_t y) {
 }
 
 // Every wavefront adds up the tiles of all requests by itself, a run of requests per lane, without a barrier.
-template <int ROWS> struct Plan {
+template <int ROWS, bool SPLIT, bool FLOAT> struct Plan {
   int64_t end, work;    // tiles up to the lane's last request; of all
   Request q;            // the lane's first request
   int32_t run, groups;  // requests per lane; workgroups with work
@@ -221,7 +228,17 @@ template <int ROWS> struct Plan {
     } else {
       work = end = from_lane(end, 0), sets = from_lane(sets, 0);
     }
-    groups = (int)min((int64_t)gridDim.x, max((work + kLeastTiles - 1) / kLeastTiles, sets));
+    // A workgroup of attend_split has 16 tiles at least, four or two for a wavefront.  In attend_shared n pieces of T tiles take
+    // the time of T / n tiles and then of n pieces taken up, each that of one and a half tiles (float: of three quarters), least
+    // with n = sqrt(T / 1.5).  (Sets of 64 rows and 62 tiles: 21 us with pieces of 8, 24 of 16, 28 of 5; 130 tiles: 26 us with 16, 36 with
+    // 8, 41 with 5; 16 tiles: 17 us with 8, 25 with 16.)
+    int64_t wanted;
+    if constexpr (SPLIT) wanted = (work + kLeastTiles - 1) / kLeastTiles;
+    else {
+      const float tiles = (float)work / (float)max(sets, (int64_t)1);
+      wanted = min((int64_t)(sqrtf(tiles * (FLOAT ? 4.f / 3 : 2.f / 3)) + 0.5f) * sets, work / kLeastShared);
+    }
+    groups = (int)min((int64_t)gridDim.x, max(wanted, sets));
     // as many for each set, if few are lost by it: sets of one length are then cut alike and no workgroup has parts of two
     if (sets && sets <= groups && groups % (int)sets <= groups / 8) groups -= groups % (int)sets;
   }
@@ -271,8 +288,12 @@ template <int ROWS> struct Plan {
   }
 };
 
-// Runs that follow each other (the same cached tokens for other rows) go to workgroups of one XCD (blockIdx % 8).
-__device__ inline int group_index() { return gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8; }
+// Runs that follow each other (the same cached tokens for other rows) go to workgroups of one XCD (blockIdx % 8), as many to
+// each.  (The grid is a multiple of eight.)  -1: none is left for this one.
+__device__ inline int group_index(int groups) {
+  const int each = (groups + 7) / 8, in = blockIdx.x / 8, group = blockIdx.x % 8 * each + in;
+  return in < each && group < groups ? group : -1;
+}
 
 // The first of `count` dimensions: where the head ends before them the last ones it has (they meet zeros of the query, or a
 // result that nobody wants).  FULL: the head has as many dimensions as the kernel.
@@ -452,8 +473,9 @@ template <typename CT, bool FLOAT> __device__ inline void store(const Args& a, c
   else *reinterpret_cast<u2*>(static_cast<uint16_t*>(a.out) + to) = u2{pair_of<CT>(o[0], o[1]), pair_of<CT>(o[2], o[3])};
 }
 
-// A piece in the workspace: its values in the order in which lanes hold them, so that a wavefront writes and reads whole lines (pairs of
-// floats, 512 bytes for 64 lanes), then a maximum and a sum of weights for every row.
+// A piece in the workspace: its values in the order in which lanes hold them, so that a wavefront writes and reads whole lines (pairs
+// of floats, 512 bytes for 64 lanes), then a maximum and a sum of weights for every row.  (In the order of the rows, scattered writes
+// of eight bytes: 32 ragged requests 138 us instead of 88, 4 x 64 tokens over 131072 0.57 ms instead of 0.49.)
 //   SPLIT  lane e % (16 * DP / 4) of attend_split has the four values e of rows of DP / 4
 //   else   a wavefront of attend_shared has 16 rows as in Rows: pair r of lane (n, g) are the values i and i + 1 of acc[r / 2]
 template <int DP, int ROWS, bool SPLIT> struct Partial {
@@ -472,8 +494,7 @@ template <int DP, int ROWS, bool SPLIT> struct Partial {
 
 // Writes of a piece go past the L2 of the XCD, to where all XCDs read: no write-back of a whole L2 has to follow them.
 __device__ inline void write_through(float* to, float x, float y) {
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), __builtin_bit_cast(uint64_t, u2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)}),
-                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), __builtin_bit_cast(uint64_t, f2{x, y}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // And they are read past the caches, which may hold what was there before.
@@ -487,8 +508,9 @@ __device__ inline float behind(float m, float top) { return m == -INFINITY ? 0.f
 
 // The workgroup that comes last joins the pieces of its rows, in their order.  What the others wrote is there: every wavefront
 // waits until its writes, which go through all caches, are done, then the workgroup counts itself.  (A release and an acquire
-// instead would write back and drop a whole L2 each, 0.1 and 0.3 us for every workgroup, one after the other.)  Bound by the latency of these reads: a lane has eight pieces of its four values under way at once,
-// and lanes that are left over take a share of the pieces.
+// instead would write back and drop a whole L2 each, 0.1 and 0.3 us for every workgroup, one after the other.)  Bound by the
+// latency of these reads: a lane has eight pieces of its four values under way at once (sixteen were 1 us slower), and lanes that
+// are left over take a share of the pieces.  Three to four microseconds for up to 26 pieces.
 __device__ inline bool all_arrived(const Args& a, const Unit& u, uint32_t& arrived) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -600,6 +622,10 @@ template <typename CT, bool FLOAT, int DP, int ROWS, bool SPLIT> __device__ inli
 }
 
 // ---- few rows: the wavefronts split the positions -----------------------------------------------------------
+// A wavefront has the whole of its 16 rows' result in registers and reads each key and value of its positions once, as the operand
+// itself: no LDS and no barrier between tiles, a tile of keys and one of values on their way while one is computed.  With enough tiles
+// bound by memory (5.9 TB/s with 8192 cached tokens for each of 640 key heads, 5.4 with 65536 for each of 20), with few by the latencies
+// behind each other: about 1.2 us until a workgroup knows its piece, 2 until the first keys are there, 1.2 to 1.6 per tile, and the join.
 template <typename CT, bool FLOAT, int DP, int WAVES, bool FULL>
 __global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
   constexpr int kWaves = WAVES, kThreads = 64 * WAVES;
@@ -613,10 +639,10 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
   __shared__ Joint<kThreads> joint;
   __shared__ uint32_t any_odd;  // a value that is not finite was taken out of a product
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Plan<kRows> plan(a, threadIdx.x & 63);
+  const Plan<kRows, true, FLOAT> plan(a, threadIdx.x & 63);
 
-  const int group = group_index();
-  if (group >= plan.groups) return;
+  const int group = group_index(plan.groups);
+  if (group < 0) return;
   int64_t at_tile = plan.begin_of(group);
   const int64_t stop = plan.begin_of(group + 1);
   while (at_tile < stop) {
@@ -834,13 +860,20 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
 // the lane; values: one position's eight dimensions), straight into LDS, where it lies in that order, a kilobyte per fragment
 // without bank conflicts, and is read by all of them.  kAhead tiles are on their way while one is computed: the cache answers
 // after one to two microseconds, a tile's products take a third of that.
+// Counted with 4 requests of 64 tokens, four query heads per key head, over 131072 (0.47 ms with pages of 64): the matrix cores work a
+// third of the time, vector instructions (the weights, and turning values) take two fifths, and between barriers all wavefronts
+// want the same of the two at once; no bank conflicts.  Float rows have two or three operands for each query and weight: 3
+// matrix instructions of bfloat16 where 16-bit rows have one.  Chains of up to 512 tokens over up to 2048, 4 requests: 0.15 ms, of which a large
+// product would need 63 us for these; new tokens are converted on their way to LDS, which nothing hides.
 constexpr int kWindow = 512;  // entries of a request's table in LDS
 
 // 16 bytes per lane from memory to the kilobyte of LDS at `to`, a place that nothing reads before wait_for_all_but has waited.  (The
 // compiler is not told that LDS changes: every read of LDS would wait for all such loads.)
 __device__ inline void to_lds(const void* from, uint32_t to) {
   uint32_t m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0" : "=&s"(m0) : "v"(from), "s"(__builtin_amdgcn_readfirstlane(to)));
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "v"(from), "s"(__builtin_amdgcn_readfirstlane(to)));
 }
 // Until all but the last LOADS loads of the wavefront are done, and what it reads from and writes to LDS; then all wavefronts.
 template <int LOADS> __device__ inline void wait_for_all_but() {
@@ -870,14 +903,14 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
   };
   __shared__ __align__(1024) Lds lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Plan<kRows> plan(a, threadIdx.x & 63);
+  const Plan<kRows, false, FLOAT> plan(a, threadIdx.x & 63);
   // The wavefronts of the first half fetch keys, the others values (there are as many of both).
   constexpr int kHalf = WAVES / 2;
   const bool keys = wave < kHalf;
   const int fragment0 = (keys ? wave : wave - kHalf) * kMine;
 
-  const int group = group_index();
-  if (group >= plan.groups) return;
+  const int group = group_index(plan.groups);
+  if (group < 0) return;
   int64_t at_tile = plan.begin_of(group);
   const int64_t stop = plan.begin_of(group + 1);
   while (at_tile < stop) {
@@ -1058,26 +1091,44 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
     }
     if (lds.any_odd) add_odd_values<CT, FLOAT, DP, kRows, false>(a, u, 64 * WAVES);
     if (u.pieces > 1 && all_arrived(a, u, lds.arrived) && !idle) {
-      // a lane takes up the pieces of the values that it has itself
+      // A lane takes up the pieces of the values that it has itself, several at once where registers allow it: bound by the latency of
+      // these reads, and by what a CU can have under way.
+      constexpr int kAtOnce = WAVES == 4 ? 2 : 1;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         const int tile = MT * wave + mt;
         float m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int j = 0; j < kParts * kEach; ++j) rows[mt].acc[j] = f4{0, 0, 0, 0};
-        for (int c = 0; c < u.pieces; ++c) {
-          float* const from = P::of(a, u.slot(c));
-          const f2 ml = read_through(P::sums(from, 16 * tile + n));
-          f2 x[DP / 8];
+        for (int c0 = 0; c0 < u.pieces; c0 += kAtOnce) {
+          f2 ml[kAtOnce], x[kAtOnce][DP / 8];
+          float top = m;
 #pragma unroll
-          for (int r = 0; r < DP / 8; ++r) x[r] = read_through(P::pair(from, tile, r, lane));
-          const float top = fmaxf(m, ml[0]), back = behind(m, top), by = behind(ml[0], top);
-          l = (m == -INFINITY ? l : l * back) + (ml[0] == -INFINITY ? ml[1] : ml[1] * by);  // (without a maximum: 0, or NaN)
+          for (int c = 0; c < kAtOnce; ++c) {
+            float* const from = P::of(a, u.slot(min(c0 + c, u.pieces - 1)));
+            ml[c] = read_through(P::sums(from, 16 * tile + n));
+#pragma unroll
+            for (int r = 0; r < DP / 8; ++r) x[c][r] = read_through(P::pair(from, tile, r, lane));
+          }
+#pragma unroll
+          for (int c = 0; c < kAtOnce; ++c) {
+            if (c0 + c >= u.pieces) ml[c] = f2{-INFINITY, 0.f};
+            top = fmaxf(top, ml[c][0]);
+          }
+          const float back = behind(m, top);
+          l = m == -INFINITY ? l : l * back;
           m = top;
 #pragma unroll
-          for (int r = 0; r < DP / 8; ++r)
+          for (int j = 0; j < kParts * kEach; ++j) rows[mt].acc[j] *= back;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) rows[mt].acc[r / 2][r % 2 * 2 + i] = rows[mt].acc[r / 2][r % 2 * 2 + i] * back + x[r][i] * by;
+          for (int c = 0; c < kAtOnce; ++c) {
+            const float by = behind(ml[c][0], top);
+            l += ml[c][0] == -INFINITY ? ml[c][1] : ml[c][1] * by;  // (without a maximum: 0, or NaN)
+#pragma unroll
+            for (int r = 0; r < DP / 8; ++r)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) rows[mt].acc[r / 2][r % 2 * 2 + i] += x[c][r][i] * by;
+          }
         }
         rows[mt].sum[0] = l;
       }
@@ -1102,6 +1153,7 @@ const char* fault_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads
 
 // The counters come first, at one place for calls of all shapes: what one leaves behind them no other takes for a count.
 constexpr int kMostGroups = 512, kCountersBytes = kMostGroups * 4;
+constexpr int64_t kMuch = 1 << 15;  // tiles of 64 rows: some 64 for each workgroup
 
 // The kernel for a call, and how it is launched.
 struct Shape {
@@ -1119,21 +1171,33 @@ int64_t most_tiles(const rsr_cache_t* cache, const rsr_step_t* step) {
   return ((int64_t)step->max_pages * cache->page_size + kTile - 1) / kTile + (step->max_new + kTile - 1) / kTile;
 }
 
+// The kernels multiply the tiles of all sets (of 16 rows at least) by the number of a workgroup in floating point, exactly below 2^51.
+constexpr char kTooMany[] = "the tables could name more tokens than the kernels count";
+bool can_be_counted(const rsr_cache_t* cache, const rsr_step_t* step, int heads) {
+  const int64_t blocks = ((int64_t)step->max_new * (heads / cache->kv_heads) + 15) / 16;
+  return (double)step->requests * cache->kv_heads * blocks * most_tiles(cache, step) < 0x1p42;
+}
+
 Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool floats) {
   Shape s;
   s.dims = cache->head_dim <= 64 ? 64 : cache->head_dim <= 128 ? 128 : 256;
   const int64_t rows = (int64_t)step->max_new * (heads / cache->kv_heads);
-  // (keys and values of 256 dimensions do not fit in the registers beside a result, nor do two tiles of rows of more than 64)
+  // (keys and values of 256 dimensions do not fit in the registers beside a result, nor do two tiles of rows of that many, or of float)
   s.shared = rows > 16 || s.dims == 256;
-  const bool two = s.shared && !floats && s.dims < 256 && rows > 64;
-  s.row_tiles = two ? 2 : 1;
+  const int64_t sets = (int64_t)step->requests * cache->kv_heads, tiles = most_tiles(cache, step);
+  // attend_shared: workgroups of 64 rows; with much work of 128, or, where there are as many, 256, two tiles of rows per wavefront.  A fragment is
+  // then read from LDS once for both and a tile fetched once for all, but there are fewer workgroups for a set's rows, and more to
+  // join for each.  (256 rows per key head: 4 x 131072 cached tokens 0.54 ms, with 64 rows 0.72; 8 x 8000 89 us against 106; 8 x 4000 61
+  // against 60; 2000 41 against 22; a chain of 512 over 2048 48 against 42.)
+  const bool much = s.shared && !floats && s.dims < 256 && rows > 64 && sets * ((rows + 63) / 64) * tiles >= kMuch;
+  s.row_tiles = much ? 2 : 1;
   // attend_split: four wavefronts, of which two workgroups per CU hide each other's waits.  Eight, one workgroup per CU, where few
   // sets have so many tiles that they are cut into more pieces than there are CUs: half as many to join (20 heads of 128, 16
   // tokens: 41 against 50 us over 16384 cached ones, but 19.1 against 17.5 us over 4096).
-  const int64_t sets = (int64_t)step->requests * cache->kv_heads;
-  if (s.shared) s.waves = s.dims < 256 && rows > (two ? 128 : 64) && !(floats && s.dims == 128) ? 8 : 4;
-  else s.waves = sets < 128 && sets * most_tiles(cache, step) > kMostGroups / 2 * kLeastTiles ? 8 : 4;
+  if (s.shared) s.waves = much && rows > 128 ? 8 : 4;
+  else s.waves = sets < 128 && sets * tiles > kMostGroups / 2 * kLeastTiles ? 8 : 4;
   s.rows = s.shared ? 16 * s.waves * s.row_tiles : 16;
+  // two workgroups of four wavefronts per CU, one of eight (their LDS and registers allow no more)
   s.target = s.waves == 4 && s.dims < 256 ? kMostGroups : kMostGroups / 2;
   s.bytes = kCountersBytes + (int64_t)2 * s.target * s.rows * (s.dims + 2) * 4;
   return s;
@@ -1150,8 +1214,6 @@ template <typename CT, bool FLOAT, bool FULL> void (*kernel_of(const Shape& s))(
       if (s.dims == 64) return s.waves == 4 ? attend_shared<CT, FLOAT, 64, 4, 2, FULL> : attend_shared<CT, FLOAT, 64, 8, 2, FULL>;
       return s.waves == 4 ? attend_shared<CT, FLOAT, 128, 4, 2, FULL> : attend_shared<CT, FLOAT, 128, 8, 2, FULL>;
     }
-  } else if (s.waves == 8) {
-    return attend_shared<CT, FLOAT, 64, 8, 1, FULL>;
   }
   return s.dims == 64 ? attend_shared<CT, FLOAT, 64, 4, 1, FULL> : attend_shared<CT, FLOAT, 128, 4, 1, FULL>;
 }
@@ -1167,6 +1229,7 @@ extern "C" {
 
 int64_t rsr_tree_attention_workspace(const rsr_cache_t* cache, const rsr_step_t* step, int heads) {
   if (const char* fault = fault_of(cache, step, heads)) return set_error(RSR_ERR_INVALID_ARGUMENT, fault);
+  if (!can_be_counted(cache, step, heads)) return set_error(RSR_ERR_UNSUPPORTED, kTooMany);
   return std::max(shape_of(cache, step, heads, false).bytes, shape_of(cache, step, heads, true).bytes);
 }
 
@@ -1178,6 +1241,7 @@ int rsr_tree_attention(const rsr_cache_t* cache, const rsr_step_t* step, const v
   if (!fault && !std::isfinite(scale)) fault = "scale must be finite";
   if (fault) return set_error(RSR_ERR_INVALID_ARGUMENT, fault);
   if (step->requests == 0 || step->tokens == 0) return RSR_OK;
+  if (!can_be_counted(cache, step, heads)) return set_error(RSR_ERR_UNSUPPORTED, kTooMany);
   const int64_t width = (int64_t)heads * cache->head_dim, kv_width = (int64_t)cache->kv_heads * cache->head_dim;
   const bool floats = dtype == RSR_F32;
   const Shape s = shape_of(cache, step, heads, floats);
@@ -1192,17 +1256,16 @@ int rsr_tree_attention(const rsr_cache_t* cache, const rsr_step_t* step, const v
   const int group = heads / cache->kv_heads;
   const Args a{q, k, v, out, static_cast<const uint16_t*>(cache->k), static_cast<const uint16_t*>(cache->v), step->table, step->held, step->start, step->mask,
                static_cast<uint32_t*>(workspace), reinterpret_cast<float*>(static_cast<char*>(workspace) + kCountersBytes),
-               cache->head_stride, (uint32_t)q_stride, (uint32_t)kv_stride, (uint32_t)out_stride, (uint32_t)cache->page_stride, (uint32_t)cache->token_stride, step->requests, step->tokens,
+               cache->head_stride, (uint32_t)q_stride, (uint32_t)kv_stride, (uint32_t)out_stride, (uint32_t)cache->page_stride,
+               (uint32_t)cache->token_stride, step->requests, step->tokens,
                step->max_new, step->max_pages, rsr_internal::log2_of(cache->page_size), cache->pages, cache->kv_heads, cache->head_dim, group,
                group == 1 ? 0u : (uint32_t)(((uint64_t(1) << 32) + group - 1) / group), scale};
   const bool full = cache->head_dim == s.dims;
   auto kern = cache->dtype == RSR_F16 ? kernel_of<_Float16>(s, floats, full) : kernel_of<__bf16>(s, floats, full);
   // no more workgroups than there can be pieces
   const int64_t blocks = ((int64_t)step->max_new * group + s.rows - 1) / s.rows;
-  const int64_t tiles = most_tiles(cache, step);
-  const int64_t most = std::min((int64_t)s.target, (int64_t)step->requests * cache->kv_heads * blocks * ((tiles + kLeastTiles - 1) / kLeastTiles));
-  if ((double)step->requests * cache->kv_heads * blocks * tiles >= 0x1p42)
-    return set_error(RSR_ERR_UNSUPPORTED, "the tables could name more tokens than the kernels count");
+  const int64_t least = s.shared ? kLeastShared : kLeastTiles, pieces = (most_tiles(cache, step) + least - 1) / least;
+  const int64_t most = std::min((int64_t)s.target, (step->requests * cache->kv_heads * blocks * pieces + 7) / 8 * 8);
   hipLaunchKernelGGL(kern, dim3((unsigned)most), dim3(64 * s.waves), 0, static_cast<hipStream_t>(stream), a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(RSR_ERR_HIP, std::string("rsr_tree_attention: ") + hipGetErrorString(e));
