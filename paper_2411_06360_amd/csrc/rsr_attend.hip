@@ -38,7 +38,7 @@ namespace {
 using rsr_internal::set_error;
 
 constexpr int kTile = 32;        // positions of a tile
-constexpr int kLeastTiles = 16;  // of a workgroup of attend_split, unless a set has fewer
+constexpr int kLeastTiles = 16;  // of a workgroup of attend_split, about, unless a set has fewer
 constexpr int kLeastShared = 4;  // and of attend_shared
 constexpr float kBias = 7.f;     // weights are 2^(s - m + 7): as float16 they keep their bits down to 2^-21 of the largest
 constexpr float kLimit = 15.f;   // m follows the maximum when a weight would pass 2^15, so that it seldom does
@@ -183,74 +183,84 @@ struct Unit {
   __device__ int slot(int c) const { return slot0 + 2 * c - (c > 0); }
 };
 
-// x / y for x below 2^51 (rsr_tree_attention sees to that): a quotient in floating point that is off by one at most.  (A workgroup
-// waits for some of these before its first load.)
+// Quotients in floating point that are off by one at most, and put right: n / d where that is below 2^20; x / y for x below 2^51
+// (rsr_tree_attention sees to that).  (A workgroup waits for some of these before its first load.)
+__device__ inline int quotient(int n, int d) {
+  const int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d)), left = n - q * d;
+  return q + (left >= d) - (left < 0);
+}
 __device__ inline int64_t divided(int64_t x, int64_t y) {
-  if (x < (1 << 22)) {
-    const int n = (int)x, d = (int)min(y, (int64_t)1 << 22);
-    int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d));
-    const int left = n - q * d;
-    return q + (left >= d) - (left < 0);
-  }
+  if (x < (1 << 20)) return quotient((int)x, (int)min(y, (int64_t)1 << 20));
   int64_t q = (int64_t)((double)x / (double)y);
   const int64_t left = x - q * y;
   return q + (left >= y) - (left < 0);
 }
 
 // Every wavefront adds up the tiles of all requests by itself, a run of requests per lane, without a barrier.
+//
+// Where the chip has room for that many workgroups, each set is cut into as many equal pieces as suit it, a workgroup each.  A workgroup of
+// attend_split has some 16 tiles, four or two for a wavefront.  In attend_shared n pieces of T tiles take the time of T / n tiles and
+// then of n pieces taken up, each that of one and a half tiles (float: of three quarters), least with n = sqrt(T / 1.5).  (Sets
+// of 64 rows and 62 tiles: 21 us with pieces of 8, 24 of 16, 28 of 5; 130 tiles: 26 us with 16, 36 with 8, 41 with 5; 16 tiles: 17 us with 8,
+// 25 with 16.)  With more work the tiles of all sets, one set behind the other, are dealt out in equal runs.
 template <int ROWS, bool SPLIT, bool FLOAT> struct Plan {
-  int64_t end, work;    // tiles up to the lane's last request; of all
-  Request q;            // the lane's first request
-  int32_t run, groups;  // requests per lane; workgroups with work
+  int64_t end, work;        // tiles up to the lane's last request; of all
+  Request q;                // the lane's first request
+  int32_t run, groups;      // requests per lane; workgroups with work
+  int32_t pieces_end;       // pieces up to the lane's last request, if the sets are cut
+  bool cut;
+  static constexpr int kMany = 1 << 24;  // more sets or pieces than a chip has workgroups
 
   static __device__ int blocks_of(const Args& a, const Request& q) { return (q.fresh * a.group + ROWS - 1) / ROWS; }
   static __device__ int tiles_in(const Request& q) { return tiles_of(q.held) + tiles_of(q.fresh); }
-  static __device__ int64_t work_of(const Args& a, const Request& q) { return (int64_t)blocks_of(a, q) * a.kv_heads * tiles_in(q); }
+  static __device__ int64_t sets_of(const Args& a, const Request& q) { return (int64_t)blocks_of(a, q) * a.kv_heads; }
+  static __device__ int pieces_of(const Request& q) {
+    const int tiles = tiles_in(q);
+    if constexpr (SPLIT) return max((tiles + kLeastTiles / 2) / kLeastTiles, 1);
+    else return max(min((int)(sqrtf((float)tiles * (FLOAT ? 4.f / 3 : 2.f / 3)) + 0.5f), tiles / kLeastShared), 1);
+  }
 
   __device__ explicit Plan(const Args& a, int lane) {
     run = (a.requests + 63) / 64;
     const int r0 = min(lane * run, a.requests), r1 = min(r0 + run, a.requests);
-    int64_t sets = 0;
-    end = 0;
+    int sets = 0;
+    end = 0, pieces_end = 0;
     q = {0, 0, 0};
     for (int r = r1 - 1; r >= r0; --r) {
       q = request_of(a, r);
-      end += work_of(a, q);
-      sets += (int64_t)blocks_of(a, q) * a.kv_heads;
+      const int64_t more = sets_of(a, q);
+      end += more * tiles_in(q);
+      sets = (int)min(sets + more, (int64_t)kMany);
+      pieces_end = (int)min(pieces_end + more * pieces_of(q), (int64_t)kMany);
     }
     if (a.requests > 1) {
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
-        const int64_t u = __shfl_up(end, d), v = __shfl_up(sets, d);
-        if (lane >= d) end += u, sets += v;
+        const int64_t u = __shfl_up(end, d);
+        const int v = __shfl_up(sets, d), w = __shfl_up(pieces_end, d);
+        if (lane >= d) end += u, sets += v, pieces_end += w;
       }
-      work = from_lane(end, 63), sets = from_lane(sets, 63);
+      work = from_lane(end, 63), sets = from_lane(sets, 63), groups = from_lane(pieces_end, 63);
     } else {
-      work = end = from_lane(end, 0), sets = from_lane(sets, 0);
+      work = end = from_lane(end, 0), sets = from_lane(sets, 0), groups = pieces_end = from_lane(pieces_end, 0);
     }
-    // A workgroup of attend_split has 16 tiles at least, four or two for a wavefront.  In attend_shared n pieces of T tiles take
-    // the time of T / n tiles and then of n pieces taken up, each that of one and a half tiles (float: of three quarters), least
-    // with n = sqrt(T / 1.5).  (Sets of 64 rows and 62 tiles: 21 us with pieces of 8, 24 of 16, 28 of 5; 130 tiles: 26 us with 16, 36 with
-    // 8, 41 with 5; 16 tiles: 17 us with 8, 25 with 16.)
-    int64_t wanted;
-    if constexpr (SPLIT) wanted = (work + kLeastTiles - 1) / kLeastTiles;
-    else {
-      const float tiles = (float)work / (float)max(sets, (int64_t)1);
-      wanted = min((int64_t)(sqrtf(tiles * (FLOAT ? 4.f / 3 : 2.f / 3)) + 0.5f) * sets, work / kLeastShared);
+    cut = groups <= (int)gridDim.x;
+    if (!cut) {
+      groups = gridDim.x;
+      // as many for each set, if few are lost by it: sets of one length are then cut alike and no workgroup has parts of two
+      if (sets && sets <= groups && groups % sets <= groups / 8) groups -= groups % sets;
     }
-    groups = (int)min((int64_t)gridDim.x, max(wanted, sets));
-    // as many for each set, if few are lost by it: sets of one length are then cut alike and no workgroup has parts of two
-    if (sets && sets <= groups && groups % (int)sets <= groups / 8) groups -= groups % (int)sets;
   }
 
-  __device__ int64_t begin_of(int group) const { return divided(work * group, groups); }
+  // Where a workgroup begins: a piece, or a tile of all.
+  __device__ int64_t begin_of(int group) const { return cut ? group : divided(work * group, groups); }
   __device__ int group_of(int64_t tile) const { return (int)divided((tile + 1) * groups - 1, work); }  // whose run it is in
 
-  // The piece that begins at tile `at` of all and ends at `stop` at the latest; the tiles that it takes are added to `at`.
+  // The piece that begins at `at` and, if it is a tile, ends at `stop` at the latest; `at` moves on behind it.
   __device__ Unit next(const Args& a, int64_t& at, int64_t stop) const {
     Unit u;
-    const int lane = __builtin_amdgcn_readfirstlane(__builtin_ctzll(__ballot(end > at)));
-    int64_t before = lane ? from_lane(end, lane - 1) : 0;
+    const int lane = __builtin_amdgcn_readfirstlane(__builtin_ctzll(__ballot(cut ? pieces_end > at : end > at)));
+    int64_t before = !lane ? 0 : cut ? from_lane(pieces_end, lane - 1) : from_lane(end, lane - 1);
     u.r = lane * run;
     if (run == 1) {
       u.q = {from_lane(q.first, lane), from_lane(q.fresh, lane), from_lane(q.held, lane)};
@@ -258,32 +268,43 @@ template <int ROWS, bool SPLIT, bool FLOAT> struct Plan {
       for (;; ++u.r) {
         const Request q = request_of(a, u.r);
         u.q = {from_lane(q.first, 0), from_lane(q.fresh, 0), from_lane(q.held, 0)};
-        const int64_t work = work_of(a, u.q);
-        if (at < before + work) break;
-        before += work;
+        const int64_t here = sets_of(a, u.q) * (cut ? pieces_of(u.q) : tiles_in(u.q));
+        if (at < before + here) break;
+        before += here;
       }
     }
-    const int all = tiles_in(u.q), blocks = blocks_of(a, u.q), set = (int)divided(at - before, all);
-    const int64_t from = before + (int64_t)set * all, last = min(from + all, stop);
-    u.head = blocks == 1 ? set : (int)divided(set, blocks);
+    const int all = tiles_in(u.q), blocks = blocks_of(a, u.q);
+    int set;
+    if (cut) {
+      // (512 pieces at most, and so fewer than 2^19 tiles)
+      const int in = (int)(at - before);
+      u.pieces = __builtin_amdgcn_readfirstlane(pieces_of(u.q));
+      set = quotient(in, u.pieces);
+      u.piece = in - set * u.pieces, u.counter = (int)at - u.piece;
+      u.tile0 = quotient(all * u.piece, u.pieces), u.tile1 = quotient(all * (u.piece + 1), u.pieces);
+      u.head = blocks == 1 ? set : quotient(set, blocks);
+      at += 1;
+    } else {
+      set = (int)divided(at - before, all);
+      const int64_t from = before + (int64_t)set * all, last = min(from + all, stop);
+      u.tile0 = (int)(at - from), u.tile1 = (int)(last - from);
+      u.pieces = 1, u.piece = 0, u.counter = 0;
+      if (at > from || last < from + all) {
+        u.counter = group_of(from);
+        u.pieces = group_of(from + all - 1) - u.counter + 1, u.piece = group_of(at) - u.counter;
+      }
+      u.head = blocks == 1 ? set : (int)divided(set, blocks);
+      at = last;
+    }
+    u.slot0 = 2 * u.counter + 1;  // the first workgroup's last run; of the others their first: 2 (first + c)
     // (long and short blocks of a chain in turn: a run of tiles has some of both)
     const int in = set - u.head * blocks, block = in & 1 ? blocks - 1 - (in >> 1) : in >> 1;
     u.row0 = block * ROWS, u.rows = min(ROWS, u.q.fresh * a.group - u.row0);
     u.cached = tiles_of(u.q.held);
-    u.tile0 = (int)(at - from), u.tile1 = (int)(last - from);
     if (!a.mask) {  // a chain's rows see no further than themselves: a share of fewer tiles
       const int tiles = u.cached + tiles_of(token_of(a, u.row0 + u.rows - 1) + 1);
       if (tiles < all) u.tile0 = (int)divided((int64_t)u.tile0 * tiles, all), u.tile1 = (int)divided((int64_t)u.tile1 * tiles, all);
     }
-    u.pieces = 1, u.piece = 0;
-    int first = 0;
-    if (at > from || last < from + all) {
-      first = group_of(from);
-      u.pieces = group_of(from + all - 1) - first + 1, u.piece = group_of(at) - first;
-    }
-    u.counter = first;
-    u.slot0 = 2 * first + 1;  // the first workgroup's last run; of the others their first: 2 (first + c)
-    at = last;
     return u;
   }
 };
@@ -935,12 +956,12 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
     }
     const bool idle = 16 * MT * wave >= u.rows;  // no rows: fetches only
 
-    const int last_page = max(u.q.held - 1, 0) >> a.log2_page, in_page = (1 << a.log2_page) - 1, end = u.tile1;
+    const int last_page = max(u.q.held - 1, 0) >> a.log2_page, in_page = (1 << a.log2_page) - 1, end = u.tile1, last = max(end - 1, 0);
     const int32_t* table = a.table + (int64_t)u.r * a.max_pages;
     const uint16_t* const cache = (keys ? a.cache_k : a.cache_v) + (int64_t)u.head * a.head_stride;
     const void* const fresh = keys ? a.k : a.v;
     const uint32_t lane_part = (at & in_page) * a.token_stride;
-    int window = (u.tile0 * kTile) >> a.log2_page;  // the entry that pages[0] holds
+    int window = (min(u.tile0, last) * kTile) >> a.log2_page;  // the entry that pages[0] holds
     auto fill_window = [&] {
       for (int i = tid; i < kWindow; i += 64 * WAVES) lds.pages[i] = table[min(window + i, last_page)];
     };
@@ -991,17 +1012,17 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // from here on only tiles are on their way
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) fetch(min(u.tile0 + i, end - 1), i);  // (the last tile again instead of none: the count of loads stays)
+    for (int i = 0; i < kAhead; ++i) fetch(min(u.tile0 + i, last), i);  // (the last tile again instead of none: the count of loads stays)
     for (int first = u.tile0; first < end; first += kTogether) {
       wait_for_all_but<(kAhead - kTogether) * kMine>();  // these tiles are there, and all are done with those before
-      const int next = min(first + kAhead, end - 1);
+      const int next = min(first + kAhead, last);
       if (next < u.cached && ((min(next + kTogether, u.cached) * kTile - 1) >> a.log2_page) - window >= kWindow) {
         window = (next * kTile) >> a.log2_page;
         fill_window();
         __syncthreads();
       }
 #pragma unroll
-      for (int i = 0; i < kTogether; ++i) fetch(min(next + i, end - 1), (first - u.tile0 + kAhead + i) % kBuffers);
+      for (int i = 0; i < kTogether; ++i) fetch(min(next + i, last), (first - u.tile0 + kAhead + i) % kBuffers);
       for (int tile = first; tile < min(first + kTogether, end) && !idle; ++tile) {
         const int buffer = (tile - u.tile0) % kBuffers;
         f4 x[MT][2];
