@@ -4,7 +4,7 @@ TEST INFRASTRUCTURE ONLY: imported by tests/, by the smoke check and by the
 benchmark's cpu_baseline leg.  The HIP library never imports, links or calls
 anything in this package, and nothing here imports the HIP package.
 
-Two layers:
+Three layers:
 
 * ``oracle.dense``  - the plain definition ``out[b][c] = sum_r v[b][r]*A[r][c]``
   (Section 2.2, Problems 1 and 2) as straightforward C loops (``rsr_oracle.c``),
@@ -15,5 +15,6 @@ Two layers:
   segmentation, segmented sums, the RSR block product and the RSR++ fold), used
   to check the index tables the library builds and to pin the readings of the
   paper that the build relies on.
+* ``oracle.cache``  - the operators around the paged cache by their definitions, in float64 and Python integers.
 """
-from . import dense, steps  # noqa: F401
+from . import cache, dense, steps  # noqa: F401

@@ -15,13 +15,13 @@
 //   attend_split  up to 16: the wavefronts of a workgroup take the same rows and different positions, keys and values go
 //                 from the cache straight into registers, LDS serves to join the wavefronts at the end
 //   attend_shared more: the wavefronts take different rows and the same positions, which come through LDS
-// The positions of all requests (tiles of 32: first a request's cached ones, then its new ones) are dealt out evenly to as many
-// workgroups as the chip runs at once (one length per workgroup and set instead: 32 ragged requests 181 us, dealt out 138).  The
-// pieces of a row meet in the workspace, where the workgroup that comes last joins them in their order.
+// The positions (tiles of 32: first a request's cached ones, then its new ones) are cut into equal pieces, or, if these were more
+// than the workgroups that the chip runs at once, dealt out evenly to those (32 ragged requests of up to 8192: 138 us, with pieces
+// of one length 181).  The pieces of a row meet in the workspace, where the workgroup that comes last joins them in their order.
 //
 // Measured on one MI355X, whole calls (a large copy moves 4.8 TB/s there, a sum reads 4.0, a large product does 1.23 PFLOP/s with
 // 16-bit operands): 32 requests of one token, 20 heads of 128, 8192 cached tokens each: 453 us, 5.9 TB/s of cache, bound by memory.
-// 16 drafted tokens over 4096, the same heads: 18 us for 42.6 MB; a token over 500: 13 us for 5.2 MB, a chain of latencies (lengths,
+// 16 drafted tokens over 4096, the same heads: 18 us for 42.6 MB; a token over 500: 12 us for 5.2 MB, a chain of latencies (lengths,
 // table, tiles, the join).  64 drafted tokens with four query heads per key head, 4 requests over 131072: 0.47 ms, 0.73 PFLOP/s;
 // one request over 2000: 22 us.
 #include <hip/hip_runtime.h>
@@ -38,7 +38,7 @@ namespace {
 using rsr_internal::set_error;
 
 constexpr int kTile = 32;        // positions of a tile
-constexpr int kLeastTiles = 16;  // of a workgroup of attend_split, about, unless a set has fewer
+constexpr int kLeastTiles = 16;  // of a workgroup of attend_split, about (a set may have fewer)
 constexpr int kLeastShared = 4;  // and of attend_shared
 constexpr float kBias = 7.f;     // weights are 2^(s - m + 7): as float16 they keep their bits down to 2^-21 of the largest
 constexpr float kLimit = 15.f;   // m follows the maximum when a weight would pass 2^15, so that it seldom does
@@ -172,8 +172,8 @@ template <typename T> __device__ inline T from_lane(T x, int lane) {
 
 __device__ inline int token_of(const Args& a, int row) { return a.group_inverse ? (int)__umulhi((uint32_t)row, a.group_inverse) : row; }
 
-// A set: the rows of a key head that a workgroup takes together.  The tiles of all sets, one set behind the other, are dealt
-// out to the workgroups in equal runs, so that a workgroup has the end of one set, whole sets, and the beginning of another.
+// A set: the rows of a key head that a workgroup takes together.  A workgroup has one piece of a set, or, where the tiles of all
+// sets are dealt out, the end of one set, whole sets, and the beginning of another.
 struct Unit {
   Request q;
   int32_t r, head, row0, rows;   // request, key head, first row and rows
@@ -198,11 +198,12 @@ __device__ inline int64_t divided(int64_t x, int64_t y) {
 
 // Every wavefront adds up the tiles of all requests by itself, a run of requests per lane, without a barrier.
 //
-// Where the chip has room for that many workgroups, each set is cut into as many equal pieces as suit it, a workgroup each.  A workgroup of
-// attend_split has some 16 tiles, four or two for a wavefront.  In attend_shared n pieces of T tiles take the time of T / n tiles and
-// then of n pieces taken up, each that of one and a half tiles (float: of three quarters), least with n = sqrt(T / 1.5).  (Sets
-// of 64 rows and 62 tiles: 21 us with pieces of 8, 24 of 16, 28 of 5; 130 tiles: 26 us with 16, 36 with 8, 41 with 5; 16 tiles: 17 us with 8,
-// 25 with 16.)  With more work the tiles of all sets, one set behind the other, are dealt out in equal runs.
+// Where the chip has room for that many workgroups, each set is cut into as many equal pieces as suit it, a workgroup each.  A
+// workgroup of attend_split has some 16 tiles, four or two for a wavefront.  In attend_shared n pieces of T tiles take the time of
+// T / n tiles and then of n pieces taken up, each that of one and a half tiles (float: of three quarters), least with n = sqrt(T /
+// 1.5).  (Sets of 64 rows and 62 tiles: 21 us with pieces of 8, 24 of 16, 28 of 5; 130 tiles: 26 us with 16, 36 with 8, 41 with 5;
+// 16 tiles: 17 us with 8, 25 with 16.)  With more work the tiles of all sets, one set behind the other, are dealt out in equal
+// runs.  (Seven ragged requests of 13 tokens over up to 3001: 28 us cut, 34 dealt out.)
 template <int ROWS, bool SPLIT, bool FLOAT> struct Plan {
   int64_t end, work;        // tiles up to the lane's last request; of all
   Request q;                // the lane's first request
@@ -644,9 +645,10 @@ template <typename CT, bool FLOAT, int DP, int ROWS, bool SPLIT> __device__ inli
 
 // ---- few rows: the wavefronts split the positions -----------------------------------------------------------
 // A wavefront has the whole of its 16 rows' result in registers and reads each key and value of its positions once, as the operand
-// itself: no LDS and no barrier between tiles, a tile of keys and one of values on their way while one is computed.  With enough tiles
-// bound by memory (5.9 TB/s with 8192 cached tokens for each of 640 key heads, 5.4 with 65536 for each of 20), with few by the latencies
-// behind each other: about 1.2 us until a workgroup knows its piece, 2 until the first keys are there, 1.2 to 1.6 per tile, and the join.
+// itself: no LDS and no barrier between tiles, a tile of keys and one of values on their way while one is computed.  With enough
+// tiles bound by memory (5.9 TB/s with 8192 cached tokens for each of 640 key heads, 5.4 with 65536 for each of 20), with few by
+// the latencies behind each other: about 1.2 us until a workgroup knows its piece, 2 until the first keys are there, 1.2 to 1.6
+// per tile, and the join.
 template <typename CT, bool FLOAT, int DP, int WAVES, bool FULL>
 __global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
   constexpr int kWaves = WAVES, kThreads = 64 * WAVES;
@@ -877,15 +879,15 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
 }
 
 // ---- many rows: the wavefronts share the positions ----------------------------------------------------------
-// A tile is fetched by all wavefronts, a share each, as the 16 bytes that every lane will want of it (keys: fragment (h, k) of
-// the lane; values: one position's eight dimensions), straight into LDS, where it lies in that order, a kilobyte per fragment
-// without bank conflicts, and is read by all of them.  kAhead tiles are on their way while one is computed: the cache answers
-// after one to two microseconds, a tile's products take a third of that.
-// Counted with 4 requests of 64 tokens, four query heads per key head, over 131072 (0.47 ms with pages of 64): the matrix cores work a
-// third of the time, vector instructions (the weights, and turning values) take two fifths, and between barriers all wavefronts
-// want the same of the two at once; no bank conflicts.  Float rows have two or three operands for each query and weight: 3
-// matrix instructions of bfloat16 where 16-bit rows have one.  Chains of up to 512 tokens over up to 2048, 4 requests: 0.15 ms, of which a large
-// product would need 63 us for these; new tokens are converted on their way to LDS, which nothing hides.
+// A tile is fetched by all wavefronts, a share each, as the 16 bytes that every lane will want of it (keys: fragment (h, k) of the
+// lane; values: one position's eight dimensions), straight into LDS, where it lies in that order, a kilobyte per fragment without
+// bank conflicts, and is read by all of them.  kAhead tiles are on their way while one is computed: the cache answers after one to
+// two microseconds, a tile's products take a third of that. Counted with 4 requests of 64 tokens, four query heads per key head,
+// over 131072 (0.47 ms with pages of 64): the matrix cores work a third of the time, vector instructions (the weights, and turning
+// values) take two fifths, and between barriers all wavefronts want the same of the two at once; no bank conflicts.  Float rows
+// have two or three operands for each query and weight: 3 matrix instructions of bfloat16 where 16-bit rows have one.  Chains of
+// up to 512 tokens over up to 2048, 4 requests: 0.15 ms, of which a large product would need 63 us for these; new tokens are
+// converted on their way to LDS, which nothing hides.
 constexpr int kWindow = 512;  // entries of a request's table in LDS
 
 // 16 bytes per lane from memory to the kilobyte of LDS at `to`, a place that nothing reads before wait_for_all_but has waited.  (The
@@ -911,7 +913,8 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
   constexpr int kRows = 16 * MT * WAVES;
   constexpr int kKeys = 2 * kSteps, kValues = DP == 64 ? 4 : 8 * kParts;   // fragments of a tile
   constexpr int kFragments = kKeys + kValues, kMine = kFragments / WAVES;  // that a wavefront fetches
-  // Eight wavefronts take two tiles between barriers: they lose less to each other (four, whose other workgroup fills in, lose registers).
+  // Eight wavefronts take two tiles between barriers: they lose less to each other (four, whose other workgroup fills in, lose
+  // registers).
   constexpr int kBuffers = 4, kTogether = WAVES == 8 ? 2 : 1, kAhead = kBuffers - kTogether;
   constexpr bool kEarly = !(FLOAT && DP == 128);  // values are read from LDS while scores are worked out, where registers allow it
   static_assert(kFragments % WAVES == 0);
@@ -1112,8 +1115,8 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
     }
     if (lds.any_odd) add_odd_values<CT, FLOAT, DP, kRows, false>(a, u, 64 * WAVES);
     if (u.pieces > 1 && all_arrived(a, u, lds.arrived) && !idle) {
-      // A lane takes up the pieces of the values that it has itself, several at once where registers allow it: bound by the latency of
-      // these reads, and by what a CU can have under way.
+      // A lane takes up the pieces of the values that it has itself, several at once where registers allow it: bound by the
+      // latency of these reads, and by what a CU can have under way.
       constexpr int kAtOnce = WAVES == 4 ? 2 : 1;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
@@ -1192,7 +1195,8 @@ int64_t most_tiles(const rsr_cache_t* cache, const rsr_step_t* step) {
   return ((int64_t)step->max_pages * cache->page_size + kTile - 1) / kTile + (step->max_new + kTile - 1) / kTile;
 }
 
-// The kernels multiply the tiles of all sets (of 16 rows at least) by the number of a workgroup in floating point, exactly below 2^51.
+// The kernels multiply the tiles of all sets (of 16 rows at least) by the number of a workgroup in floating point, exactly below
+// 2^51.
 constexpr char kTooMany[] = "the tables could name more tokens than the kernels count";
 bool can_be_counted(const rsr_cache_t* cache, const rsr_step_t* step, int heads) {
   const int64_t blocks = ((int64_t)step->max_new * (heads / cache->kv_heads) + 15) / 16;
@@ -1203,13 +1207,14 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   Shape s;
   s.dims = cache->head_dim <= 64 ? 64 : cache->head_dim <= 128 ? 128 : 256;
   const int64_t rows = (int64_t)step->max_new * (heads / cache->kv_heads);
-  // (keys and values of 256 dimensions do not fit in the registers beside a result, nor do two tiles of rows of that many, or of float)
+  // (keys and values of 256 dimensions do not fit in the registers beside a result, nor do two tiles of rows of that many, or of
+  // float)
   s.shared = rows > 16 || s.dims == 256;
   const int64_t sets = (int64_t)step->requests * cache->kv_heads, tiles = most_tiles(cache, step);
-  // attend_shared: workgroups of 64 rows; with much work of 128, or, where there are as many, 256, two tiles of rows per wavefront.  A fragment is
-  // then read from LDS once for both and a tile fetched once for all, but there are fewer workgroups for a set's rows, and more to
-  // join for each.  (256 rows per key head: 4 x 131072 cached tokens 0.54 ms, with 64 rows 0.72; 8 x 8000 89 us against 106; 8 x 4000 61
-  // against 60; 2000 41 against 22; a chain of 512 over 2048 48 against 42.)
+  // attend_shared: workgroups of 64 rows; with much work of 128, or, where there are as many, 256, two tiles of rows per
+  // wavefront.  A fragment is then read from LDS once for both and a tile fetched once for all, but there are fewer workgroups for
+  // a set's rows, and more to join for each.  (256 rows per key head: 4 x 131072 cached tokens 0.54 ms, with 64 rows 0.72; 8 x
+  // 8000 89 us against 106; 8 x 4000 61 against 60; 2000 41 against 22; a chain of 512 over 2048 48 against 42.  128 rows: 4 x 131072 352 us against 435, 8 x 16000 114 against 107.)
   const bool much = s.shared && !floats && s.dims < 256 && rows > 64 && sets * ((rows + 63) / 64) * tiles >= kMuch;
   s.row_tiles = much ? 2 : 1;
   // attend_split: four wavefronts, of which two workgroups per CU hide each other's waits.  Eight, one workgroup per CU, where few
