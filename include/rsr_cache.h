@@ -83,7 +83,8 @@ typedef struct rsr_step_t {
  *   out[start[r]+i][a] = sum_p w_p v_p / sum_p w_p,   w_p = exp(scale * <q[start[r]+i][a], k_p>)
  * over the cached tokens of the request on pages that are there and the new tokens that i sees.  A token that
  * sees nothing gets zeros; what it does not see does not touch it, infinities and NaN included.  A seen key or
- * value that is not finite makes the results that it enters not finite (infinite or NaN).
+ * value that is not finite makes the results that it enters not finite (infinite or NaN), whatever the sign of the score; so does a
+ * score beyond the range of float.
  *
  *   q        DEVICE, row t at q + t * q_stride elements: [heads][head_dim]
  *   k, v     DEVICE, row t at k + t * kv_stride: [kv_heads][head_dim]; rounded to the type of the cache

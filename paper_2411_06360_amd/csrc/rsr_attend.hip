@@ -27,6 +27,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -41,6 +42,7 @@ constexpr int kTile = 32;        // positions of a tile
 constexpr int kLeastTiles = 16;  // of a workgroup of attend_split, about (a set may have fewer)
 constexpr int kLeastShared = 4;  // and of attend_shared
 constexpr float kBias = 7.f;     // weights are 2^(s - m + 7): as float16 they keep their bits down to 2^-21 of the largest
+constexpr float kUnseen = -FLT_MAX;  // the exponent of what a row does not see: a weight of 0, and not a maximum
 constexpr float kLimit = 15.f;   // m follows the maximum when a weight would pass 2^15, so that it seldom does
 
 typedef float f2 __attribute__((ext_vector_type(2)));
@@ -136,6 +138,12 @@ __device__ inline float over_groups_max(float x) {
 __device__ inline float max3(float x, float y, float z) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+  return r;
+}
+
+__device__ inline float min3(float x, float y, float z) {
+  float r;
+  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
   return r;
 }
 
@@ -328,23 +336,23 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
   static constexpr int kEach = DP / 16 < 8 ? DP / 16 : 8;  // neighbouring dimensions of a lane's piece of a value
   static constexpr int kParts = DP / (16 * kEach);         // such pieces
 
-  f4 acc[kParts * kEach], sum;
+  f4 acc[kParts * kEach];
+  f4 sum;        // four times the same for finite scores
   float factor;  // of a score to its exponent of two
   float base;    // taken off the exponents: m - kBias
-  float limit;   // of an exponent: kLimit, and -infinity before the row has seen anything
-  int token;
-  uint64_t mask;  // new tokens that the row sees
+  float limit;   // of an exponent: kLimit, and kUnseen before the row has seen anything
+  uint64_t sees;  // new tokens, a bit each; in a chain how many
 
   // Queries of the 16 rows from `first` on: operand B of the scores, zeros behind the last dimension and the last row.
   __device__ void begin(const Args& a, const Unit& u, int first, int n, int g, u4 (&query)[kSteps][kTerms]) {
     const int in = first + n, row = u.row0 + in;
     const bool there = in < u.rows;
-    token = there ? token_of(a, row) : 0;
+    const int token = there ? token_of(a, row) : 0;
     const int64_t from = row_at(u.q.first + token, a.q_stride) + (u.head * a.group + (there ? row - token * a.group : 0)) * a.dim;
-    mask = there && a.mask ? a.mask[u.q.first + token] : ~0ull;
-    if (!there) token = a.max_new;  // (a row that is not there sees all: it must not make a tile one that has to be masked)
+    // (a row that is not there sees all: it must not make a tile one that has to be masked)
+    sees = a.mask ? there ? a.mask[u.q.first + token] : ~0ull : there ? token + 1 : a.max_new;
     factor = a.scale * 1.44269504088896341f;
-    base = 0.f, limit = -INFINITY;
+    base = 0.f, limit = kUnseen;
     sum = f4{0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < kParts * kEach; ++j) acc[j] = f4{0, 0, 0, 0};
@@ -403,7 +411,13 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
   }
 
   // Exponents to weights and to operand B of the result.
+  //
+  // A score of minus infinity (a key that is not finite, products beyond the range of float) would drop out with a weight of 0, and a
+  // row of such scores would look like one that sees nothing.  Zero times the lowest exponent is NaN there and 0 else, and goes into
+  // one of a lane's four sums, which finish() looks at: five instructions a tile, no register and no branch (4 x 64 tokens over 131072
+  // 472 us, without it 467; with a branch 723, with the lowest exponent in a register of its own 631).
   __device__ void weigh(float (&s)[8], u4 (&p)[kTerms]) {
+    sum[1] = fmaf(min3(min3(s[0], s[1], s[2]), min3(s[3], s[4], s[5]), min3(s[6], s[7], s[7])), 0.f, sum[1]);
     float top = max3(max3(max3(s[0], s[1], s[2]), s[3], s[4]), max3(s[5], s[6], s[7]), -INFINITY);
     if (__ballot(top > limit)) {
       // the maximum follows where it is left behind: a row's matter alone, so that no other row's scores move it
@@ -427,6 +441,13 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
     for (int t = kTerms - 1; t >= 0; --t) sum = Half<CT>::mfma(ones, p[t], sum);
   }
 
+  // Behind the last tile.
+  __device__ void finish() {
+    float x = sum[1] + __shfl_xor(sum[1], 16);
+    x += __shfl_xor(x, 32);
+    if (x != x) sum[0] = x;
+  }
+
   // Of eight positions the dimension that is number j of the lane's piece.
   static __device__ u4 column(const uint32_t (&value)[8][kEach / 2], int j) {
     u4 x;
@@ -446,7 +467,7 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
 
   // Which of eight new tokens from number j0 on the row sees, a bit each.
   __device__ int seen_new(const Args& a, const Unit& u, int j0) const {
-    return (a.mask ? (int)(mask >> min(j0, 63)) & 255 : eight_bits(token + 1 - j0)) & eight_bits(u.q.fresh - j0);
+    return (a.mask ? (int)(sees >> min(j0, 63)) & 255 : eight_bits((int)sees - j0)) & eight_bits(u.q.fresh - j0);
   }
 
   // Which of the lane's eight positions have a value that is not finite?
@@ -769,7 +790,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
         rows.exponents(x, s);
         if (__ballot(seen != 255)) {
 #pragma unroll
-          for (int t = 0; t < 8; ++t) s[t] = seen >> t & 1 ? s[t] : -INFINITY;
+          for (int t = 0; t < 8; ++t) s[t] = seen >> t & 1 ? s[t] : kUnseen;
 #pragma unroll
           for (int part = 0; part < kParts; ++part) R::leave_out(value[part], ~seen);  // (what lies on a page behind the last token)
         }
@@ -820,7 +841,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
       const bool partly = __ballot(seen != 255) != 0;
       if (partly) {
 #pragma unroll
-        for (int t = 0; t < 8; ++t) s[t] = seen >> t & 1 ? s[t] : -INFINITY;
+        for (int t = 0; t < 8; ++t) s[t] = seen >> t & 1 ? s[t] : kUnseen;
       }
       rows.weigh(s, p);
 #pragma unroll
@@ -837,6 +858,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
     }
 
     // ---- the wavefronts
+    rows.finish();
     if (g == 0) row_m[wave][n] = rows.maximum(), row_l[wave][n] = rows.sum[0];
     __syncthreads();
     float top = row_m[0][n];
@@ -955,7 +977,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
       for (int k = 0; k < kSteps; ++k)
 #pragma unroll
         for (int t = 0; t < kTerms; ++t) asm volatile("" : "+v"(query[mt][k][t]));
-      asm volatile("" : "+v"(rows[mt].mask));
+      asm volatile("" : "+v"(rows[mt].sees));
     }
     const bool idle = 16 * MT * wave >= u.rows;  // no rows: fetches only
 
@@ -1056,7 +1078,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int t = 0; t < 8; ++t) s[mt][t] = seen[mt] >> t & 1 ? s[mt][t] : -INFINITY;
+            for (int t = 0; t < 8; ++t) s[mt][t] = seen[mt] >> t & 1 ? s[mt][t] : kUnseen;
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) rows[mt].weigh(s[mt], p[mt]);
@@ -1084,6 +1106,8 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
       }
     }
     wait_for_all_but<0>();
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) rows[mt].finish();
 
     auto store_rows = [&] {
 #pragma unroll
