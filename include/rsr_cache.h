@@ -19,7 +19,8 @@
  * message through rsr_last_error(), no exceptions.  All calls are asynchronous on `stream`, allocate nothing,
  * keep nothing from one call to the next and may be captured in a HIP graph.  The device that holds the
  * buffers must be current.  Lengths live on the device and are not seen by the host: a length, page or slot
- * out of range there is left out as stated below, and never leads outside the buffers.
+ * out of range there is left out as stated below, and never leads outside the buffers.  (rsr_cache_slots alone is not
+ * told how long the list of free pages is; rsr_cache_slots_bounded is.)
  */
 #ifndef RSR_CACHE_H_
 #define RSR_CACHE_H_
@@ -117,7 +118,7 @@ int rsr_tree_attention(const rsr_cache_t *cache, const rsr_step_t *step, const v
  *   held, add    DEVICE [requests] int32 (negative: 0)
  *   table        DEVICE [requests][max_pages] int32, in and out: the new entries are written, no others
  *   page_size    as in rsr_cache_t
- *   free_pages   DEVICE int32, its first free_count[0] entries are free pages; not written
+ *   free_pages   DEVICE int32, its first free_count[0] entries are free pages; not written.  The list must have that many.
  *   free_count   DEVICE int32 [1]
  *   free_left    DEVICE int32 [1] out: free_count[0] minus the pages needed; negative if there were too few.
  *                The free list of the next call is free_pages up to free_left[0].
@@ -127,10 +128,15 @@ int rsr_tree_attention(const rsr_cache_t *cache, const rsr_step_t *step, const v
  *   now          DEVICE [requests] int32 out: held[r] and those of the added tokens that the request's pages have room
  *                for (places on a page that it gave up count as room)
  * No output may overlap an input or another output.  requests 0 .. 65535, max_pages >= 1, max_slots >= 0.
+ *
+ * rsr_cache_slots_bounded - the same with the length of the list: a free_count[0] above max_free (>= 0) is taken as max_free.
  */
 int rsr_cache_slots(const int32_t *held, const int32_t *add, int requests, int32_t *table, int max_pages, int page_size,
                     const int32_t *free_pages, const int32_t *free_count, int32_t *free_left, int32_t *slots, int64_t max_slots,
                     int32_t *start, int32_t *now, void *stream);
+int rsr_cache_slots_bounded(const int32_t *held, const int32_t *add, int requests, int32_t *table, int max_pages, int page_size,
+                            const int32_t *free_pages, int64_t max_free, const int32_t *free_count, int32_t *free_left, int32_t *slots,
+                            int64_t max_slots, int32_t *start, int32_t *now, void *stream);
 
 /*
  * rsr_cache_append - writes keys and values of `count` tokens into the cache, rounded to its type (to the nearest, ties to even).

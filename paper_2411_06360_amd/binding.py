@@ -150,6 +150,8 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     L.rsr_tree_attention.restype = ci
     L.rsr_cache_slots.argtypes = [vp, vp, ci, vp, ci, ci, vp, vp, vp, vp, i64, vp, vp, vp]
     L.rsr_cache_slots.restype = ci
+    L.rsr_cache_slots_bounded.argtypes = [vp, vp, ci, vp, ci, ci, vp, i64, vp, vp, vp, i64, vp, vp, vp]
+    L.rsr_cache_slots_bounded.restype = ci
     L.rsr_cache_append.argtypes = [vp, vp, vp, i64, i64, ci, vp, vp, i64, vp]
     L.rsr_cache_append.restype = ci
     L.rsr_tree_masks.argtypes = [vp, vp, ci, ci, vp, vp, vp]
@@ -408,13 +410,14 @@ def rsr_tree_attention(cache: RsrCache, step: RsrStep, q, k, v, out, heads: int,
 
 
 def rsr_cache_slots(held, add, table, page_size: int, free_pages, free_count, slots, start, now, free_left, stream=None) -> None:
-    """Pages and slots for the next ``add[r]`` tokens of every request; all device int32, see the header."""
+    """Pages and slots for the next ``add[r]`` tokens of every request; all device int32, see the header.  A ``free_count`` above the
+    length of ``free_pages`` is taken as that."""
     requests = held.numel()
     if table.dim() != 2 or table.shape[0] != requests:
         raise ValueError("the table has a row for each request")
-    code = (_lib or load()).rsr_cache_slots(
+    code = (_lib or load()).rsr_cache_slots_bounded(
         _whole(held, 32, 0), _whole(add, 32, requests), requests, _whole(table, 32, 0), table.shape[1], int(page_size), _whole(free_pages, 32, 0),
-        _whole(free_count, 32, 1), _whole(free_left, 32, 1), _whole(slots, 32, 0), slots.numel(), _whole(start, 32, requests + 1),
+        free_pages.numel(), _whole(free_count, 32, 1), _whole(free_left, 32, 1), _whole(slots, 32, 0), slots.numel(), _whole(start, 32, requests + 1),
         _whole(now, 32, requests), _addr(stream))
     if code:
         _check(code)

@@ -33,7 +33,7 @@ constexpr int kBatch = kSlotThreads * kPerThread;
 struct SlotsArgs {
   const int32_t *held, *add, *free_pages, *free_count;
   int32_t *table, *free_left, *slots, *start, *now;
-  int64_t max_slots;
+  int64_t max_free, max_slots;
   int32_t requests, max_pages, log2_page;
 };
 
@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(SlotsArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t every = (int64_t)gridDim.x * kSlotThreads, mine = (int64_t)blockIdx.x * kSlotThreads + tid;
   const int64_t size = int64_t(1) << a.log2_page, width = a.max_pages;
-  const int64_t count = max(a.free_count[0], 0);
+  const int64_t count = min((int64_t)max(a.free_count[0], 0), a.max_free);
   int64_t slots0 = 0, pages0 = 0;
   for (int r0 = 0; r0 < a.requests; r0 += kBatch) {
     const int n = min(kBatch, a.requests - r0);
@@ -211,20 +211,29 @@ __global__ void __launch_bounds__(kMaskThreads) masks_kernel(const int32_t* __re
 
 extern "C" {
 
-int rsr_cache_slots(const int32_t* held, const int32_t* add, int requests, int32_t* table, int max_pages, int page_size, const int32_t* free_pages,
-                    const int32_t* free_count, int32_t* free_left, int32_t* slots, int64_t max_slots, int32_t* start, int32_t* now, void* stream) {
+int rsr_cache_slots_bounded(const int32_t* held, const int32_t* add, int requests, int32_t* table, int max_pages, int page_size,
+                            const int32_t* free_pages, int64_t max_free, const int32_t* free_count, int32_t* free_left, int32_t* slots, int64_t max_slots,
+                            int32_t* start, int32_t* now, void* stream) {
   if (requests < 0 || requests > 65535) return set_error(RSR_ERR_INVALID_ARGUMENT, "requests must be in 0..65535");
-  if (max_slots < 0 || max_pages < 1) return set_error(RSR_ERR_INVALID_ARGUMENT, "max_slots must be at least 0 and max_pages at least 1");
+  if (max_slots < 0 || max_free < 0 || max_pages < 1)
+    return set_error(RSR_ERR_INVALID_ARGUMENT, "max_slots and max_free must be at least 0 and max_pages at least 1");
   if (!rsr_internal::is_page_size(page_size)) return set_error(RSR_ERR_INVALID_ARGUMENT, "page_size must be a power of two in 8..1024");
-  if (!free_count || !free_left || !start || (max_slots && !slots) || (requests && (!held || !add || !table || !free_pages || !now)))
+  if (!free_count || !free_left || !start || (max_slots && !slots) || (requests && (!held || !add || !table || (max_free && !free_pages) || !now)))
     return set_error(RSR_ERR_INVALID_ARGUMENT, "null pointer");
   if (free_left == free_count || (requests && (now == held || now == add || start == held || start == add)))
     return set_error(RSR_ERR_INVALID_ARGUMENT, "an output must not be an input");
-  const SlotsArgs a{held, add, free_pages, free_count, table, free_left, slots, start, now, max_slots, requests, max_pages, rsr_internal::log2_of(page_size)};
+  const SlotsArgs a{held,     add,       free_pages, free_count, table,     free_left, slots, start, now,
+                    max_free, max_slots, requests,   max_pages,  rsr_internal::log2_of(page_size)};
   // two slots per lane: each is a search and two reads one after the other, and adding up the requests anew costs less than a third
   const int64_t groups = (max_slots + 2 * kSlotThreads - 1) / (2 * kSlotThreads);
   hipLaunchKernelGGL(slots_kernel, dim3((unsigned)(groups < 1 ? 1 : groups > 1024 ? 1024 : groups)), dim3(kSlotThreads), 0, static_cast<hipStream_t>(stream), a);
   return launched("rsr_cache_slots");
+}
+
+int rsr_cache_slots(const int32_t* held, const int32_t* add, int requests, int32_t* table, int max_pages, int page_size, const int32_t* free_pages,
+                    const int32_t* free_count, int32_t* free_left, int32_t* slots, int64_t max_slots, int32_t* start, int32_t* now, void* stream) {
+  return rsr_cache_slots_bounded(held, add, requests, table, max_pages, page_size, free_pages, INT32_MAX, free_count, free_left, slots, max_slots, start, now,
+                                 stream);
 }
 
 int rsr_cache_append(const rsr_cache_t* cache, const void* k, const void* v, int64_t stride, int64_t nrows, int dtype, const int32_t* rows,

@@ -1,0 +1,32 @@
+"""rsr_cache_slots and rsr_cache_append at the limits of what they are given (include/rsr_cache.h)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_06360_amd as R
+from oracle import cache as oracle
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+@pytest.mark.parametrize("have", [0, 1, 5, 12])
+@pytest.mark.parametrize("beyond", [1, 40, 2**31 - 1])
+def test_a_count_beyond_the_list_of_free_pages_is_taken_as_its_length(have, beyond):
+    """The list is the beginning of a larger tensor, whose other entries are not free."""
+    print("free list", have, beyond, flush=True)
+    held, add, old, page = [10, 0, 40], [30, 100, 3], np.full((3, 9), 500, np.int32), 16
+    all_pages = ints(100 + np.arange(60))
+    table, slots, start, now, left = ints(old), ints([-7] * 140), ints([-7] * 4), ints([-7] * 3), ints([-7])
+    R.rsr_cache_slots(ints(held), ints(add), table, page, all_pages[:have], ints([min(have + beyond, 2**31 - 1)]), slots, start, now, left, stream())
+    torch.cuda.synchronize()
+    want = oracle.slots(held, add, old, page, list(range(100, 100 + have)), have, 140)
+    assert slots.tolist() == want[0] and np.array_equal(table.cpu().numpy(), want[1])
+    assert start.tolist() == want[2] and now.tolist() == want[3] and left.item() == want[4]
