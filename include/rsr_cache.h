@@ -96,7 +96,8 @@ typedef struct rsr_step_t {
  *   scale    finite
  *   strides  at least a row's elements, below 2^31; rows and pointers 16-byte aligned
  *   workspace  DEVICE, rsr_tree_attention_workspace bytes, 256-byte aligned, zero before its first use; calls leave it
- *            ready for the next one.  Calls that share it must not overlap.
+ *            ready for the next one.  Calls that share it must not overlap.  More requests, max_new, max_pages or heads never
+ *            need fewer bytes: what is enough for a program's largest step over a cache is enough for all of them.
  *
  * Statistics, sums and, with RSR_F32, everything is held to 32 bits: float queries and weights are carried
  * through the matrix cores as sums of two float16 or three bfloat16.  With 16-bit activations the weights

@@ -1212,6 +1212,9 @@ struct Shape {
   int rows;         // of a workgroup
   int target;       // workgroups at most: those that the chip runs at once
   int64_t bytes;    // of the workspace
+
+  // of a workspace with room for so many workgroups' pieces
+  int64_t bytes_for(int groups) const { return kCountersBytes + (int64_t)2 * groups * rows * (dims + 2) * 4; }
 };
 
 // of a request: as many as its row of the table can name, and the new ones
@@ -1249,7 +1252,7 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   s.rows = s.shared ? 16 * s.waves * s.row_tiles : 16;
   // two workgroups of four wavefronts per CU, one of eight (their LDS and registers allow no more)
   s.target = s.waves == 4 && s.dims < 256 ? kMostGroups : kMostGroups / 2;
-  s.bytes = kCountersBytes + (int64_t)2 * s.target * s.rows * (s.dims + 2) * 4;
+  s.bytes = s.bytes_for(s.target);
   return s;
 }
 
@@ -1280,7 +1283,14 @@ extern "C" {
 int64_t rsr_tree_attention_workspace(const rsr_cache_t* cache, const rsr_step_t* step, int heads) {
   if (const char* fault = fault_of(cache, step, heads)) return set_error(RSR_ERR_INVALID_ARGUMENT, fault);
   if (!can_be_counted(cache, step, heads)) return set_error(RSR_ERR_UNSUPPORTED, kTooMany);
-  return std::max(shape_of(cache, step, heads, false).bytes, shape_of(cache, step, heads, true).bytes);
+  // Not less for more work, so that a workspace for a program's largest step does for all: attend_split with eight wavefronts itself needs
+  // half as much as with four.
+  int64_t bytes = 0;
+  for (const bool floats : {false, true}) {
+    const Shape s = shape_of(cache, step, heads, floats);
+    bytes = std::max(bytes, s.shared ? s.bytes : s.bytes_for(kMostGroups));
+  }
+  return bytes;
 }
 
 int rsr_tree_attention(const rsr_cache_t* cache, const rsr_step_t* step, const void* q, int64_t q_stride, const void* k, const void* v,

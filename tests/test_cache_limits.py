@@ -1,6 +1,8 @@
 """What the entry points of include/rsr_cache.h answer at the limits of their arguments, before anything is launched."""
 import ctypes
 
+import pytest
+
 import paper_2411_06360_amd as R
 
 INVALID = -1
@@ -18,3 +20,33 @@ def test_lists_of_free_pages_that_are_refused():
     assert slots(most_free=-1) == INVALID and "max_free" in R.rsr_last_error()
     assert slots(free=0) == INVALID and slots(count=0) == INVALID
     assert slots(page=12) == INVALID and slots(now=AT) == INVALID
+
+
+# ---- workspace ----
+def workspace(dim, kv_heads, heads, requests, new, pages, page=32):
+    c = R.RsrCache(AT, AT, kv_heads * page * dim, page * dim, dim, R.RSR_BF16, 10, page, kv_heads, dim, 0)
+    s = R.RsrStep(AT, AT, AT, None, requests, requests * new, new, pages)
+    return R.rsr_tree_attention_workspace(c, s, heads)
+
+
+@pytest.mark.parametrize("dim", [40, 64, 128, 256])
+@pytest.mark.parametrize("kv_heads", [1, 5, 20, 127, 128])
+def test_a_workspace_for_more_work_is_not_smaller(dim, kv_heads):
+    """A program asks once, for its longest table, most requests and tokens: shorter steps must not need more."""
+    least = {}
+    for requests in (1, 2, 7, 64, 1000):
+        for new in (1, 3, 16, 17, 64, 65, 300):
+            for pages in (1, 50, 250, 500, 4000, 20000):
+                for group in (1, 2, 4, 64):
+                    here = (requests, new, pages, group)
+                    least[here] = workspace(dim, kv_heads, group * kv_heads, requests, new, pages)
+    for (r, n, p, g), bytes_ in least.items():
+        for (r1, n1, p1, g1), more in least.items():
+            if r <= r1 and n <= n1 and p <= p1 and g <= g1:
+                assert bytes_ <= more, ((r, n, p, g), (r1, n1, p1, g1))
+
+
+def test_the_workspace_of_one_sequence_with_a_table_of_any_length():
+    """20 heads of 128, one request, one token: a table of 500 pages of 32 asks for what one of 250 asks for."""
+    sizes = [workspace(128, 20, 20, 1, 1, pages) for pages in (1, 250, 500, 8192)]
+    assert sizes == sorted(sizes)
