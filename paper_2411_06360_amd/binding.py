@@ -347,11 +347,11 @@ def _dtype(x) -> int:
 
 
 def _rows(x, rows: int, width: int) -> int:
-    """Stride of a 2-D tensor of `rows` rows of `width` elements that lie side by side."""
+    """Stride of a 2-D tensor of `rows` rows of `width` elements that lie side by side (that of a single row means nothing)."""
     shape, stride = x.shape, x.stride()
     if len(shape) != 2 or shape[0] != rows or shape[1] != width or (stride[1] != 1 and width > 1):
         raise ValueError(f"a 2-D tensor with {rows} contiguous rows of {width} elements is wanted")
-    return stride[0] if rows > 1 else max(stride[0], width)
+    return stride[0] if rows > 1 else width
 
 
 _WHOLE: dict = {32: {"torch.int32"}, 64: {"torch.int64", "torch.uint64"}}  # names, and then the types themselves

@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 import paper_2411_06360_amd as R
 
@@ -50,3 +51,17 @@ def test_the_workspace_of_one_sequence_with_a_table_of_any_length():
     """20 heads of 128, one request, one token: a table of 500 pages of 32 asks for what one of 250 asks for."""
     sizes = [workspace(128, 20, 20, 1, 1, pages) for pages in (1, 250, 500, 8192)]
     assert sizes == sorted(sizes)
+
+
+# ---- strides ----
+def test_the_stride_of_a_single_row_means_nothing():
+    """One token's rows come out of tensors of any width, keys and values out of different ones.  (Here the call ends at the workspace,
+    which is the last thing that is looked at.)"""
+    k = torch.zeros((3, 2, 16, 8), dtype=torch.bfloat16)
+    ints = torch.zeros(4, dtype=torch.int32)
+    cache, step = R.make_cache(k, k), R.make_step(torch.zeros((1, 2), dtype=torch.int32), ints[:1], ints[:2], 1, 1)
+    row = lambda width, stride: torch.zeros(stride)[:width].as_strided((1, width), (stride, 1))  # noqa: E731
+    for strides in ((32, 16, 16, 32), (37, 16, 16, 33), (32, 16, 51, 32), (32, 96, 21, 41)):
+        q, key, value, out = (row(w, s) for w, s in zip((32, 16, 16, 32), strides))
+        with pytest.raises(R.RsrError, match="workspace"):
+            R.rsr_tree_attention(cache, step, q, key, value, out, 4, 1.0, torch.zeros(16, dtype=torch.uint8))
