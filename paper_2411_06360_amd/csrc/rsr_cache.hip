@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(SlotsArgs a) {
   __shared__ int64_t wave_slots[kSlotThreads / 64], wave_pages[kSlotThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t every = (int64_t)gridDim.x * kSlotThreads, mine = (int64_t)blockIdx.x * kSlotThreads + tid;
-  const int64_t size = int64_t(1) << a.log2_page, width = a.max_pages;
+  const int64_t size = int64_t(1) << a.log2_page, width = a.max_pages, most_start = min(a.max_slots, (int64_t)INT32_MAX);
   const int64_t count = min((int64_t)max(a.free_count[0], 0), a.max_free);
   int64_t slots0 = 0, pages0 = 0;
   for (int r0 = 0; r0 < a.requests; r0 += kBatch) {
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(SlotsArgs a) {
     for (int j = 0; j < kPerThread; ++j) {
       const int r = tid * kPerThread + j;
       if (writes && r < n) {
-        a.start[r0 + r] = (int32_t)min(s_at, a.max_slots);
+        a.start[r0 + r] = (int32_t)min(s_at, most_start);
         const int64_t granted = min(max(count - p_at, int64_t(0)), need[j]);
         a.now[r0 + r] = (int32_t)max(held[j], min(held[j] + added[j], (before[j] + granted) << a.log2_page));
       }
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(SlotsArgs a) {
   }
   for (int64_t i = mine + (slots0 > mine ? (slots0 - mine + every - 1) / every * every : 0); i < a.max_slots; i += every) a.slots[i] = -1;
   if (mine == 0) {
-    a.start[a.requests] = (int32_t)min(slots0, a.max_slots);
+    a.start[a.requests] = (int32_t)min(slots0, most_start);
     a.free_left[0] = (int32_t)max(count - pages0, (int64_t)INT32_MIN);
   }
 }

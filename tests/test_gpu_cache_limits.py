@@ -30,3 +30,18 @@ def test_a_count_beyond_the_list_of_free_pages_is_taken_as_its_length(have, beyo
     want = oracle.slots(held, add, old, page, list(range(100, 100 + have)), have, 140)
     assert slots.tolist() == want[0] and np.array_equal(table.cpu().numpy(), want[1])
     assert start.tolist() == want[2] and now.tolist() == want[3] and left.item() == want[4]
+
+
+def test_slots_beyond_31_bits_do_not_wrap():
+    """More added tokens than an int32 counts, with room for their slots: `start` stays at the largest that it can say."""
+    print("2^31 slots", flush=True)
+    most = 2**31 - 1
+    table = ints([[7], [-1], [9], [3]])
+    slots, start, now, left = torch.full((most + 300,), -7, dtype=torch.int32, device="cuda"), ints([0] * 5), ints([0] * 4), ints([0])
+    R.rsr_cache_slots(ints([2, 0, 3, 1]), ints([most - 1, 100, 7, 50]), table, 8, ints([4]), ints([1]), slots, start, now, left, stream())
+    torch.cuda.synchronize()
+    assert start.tolist() == [0, most - 1, most, most, most] and now.tolist() == [8, 8, 8, 8]
+    # (request 1 takes the free page; of request 0 six tokens have a place, of the others eight, five and seven)
+    assert slots[:6].tolist() == list(range(58, 64)) and slots[most - 1:most + 7].tolist() == list(range(32, 40))
+    assert slots[most + 99:most + 104].tolist() == list(range(75, 80)) and slots[most + 106:most + 113].tolist() == list(range(25, 32))
+    assert int((slots >= 0).sum()) == 6 + 8 + 5 + 7 and int(slots.min()) == -1
