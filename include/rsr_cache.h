@@ -127,7 +127,7 @@ int rsr_tree_attention(const rsr_cache_t *cache, const rsr_step_t *step, const v
  *                that gets none (no page was left, or the table is full) and behind the last token
  *   start        DEVICE [requests+1] int32 out: where a request's slots begin (at most max_slots, and 2^31-1)
  *   now          DEVICE [requests] int32 out: held[r] and those of the added tokens that the request's pages have room
- *                for (places on a page that it gave up count as room)
+ *                for (places on a page that it gave up count as room); at most 2^31-1
  * No output may overlap an input or another output.  requests 0 .. 65535, max_pages >= 1, max_slots >= 0.
  *
  * rsr_cache_slots_bounded - the same with the length of the list: a free_count[0] above max_free (>= 0) is taken as max_free.

@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(SlotsArgs a) {
       if (writes && r < n) {
         a.start[r0 + r] = (int32_t)min(s_at, most_start);
         const int64_t granted = min(max(count - p_at, int64_t(0)), need[j]);
-        a.now[r0 + r] = (int32_t)max(held[j], min(held[j] + added[j], (before[j] + granted) << a.log2_page));
+        a.now[r0 + r] = (int32_t)min(max(held[j], min(held[j] + added[j], (before[j] + granted) << a.log2_page)), (int64_t)INT32_MAX);
       }
       s_at += added[j];
       p_at += need[j];

@@ -45,3 +45,16 @@ def test_slots_beyond_31_bits_do_not_wrap():
     assert slots[:6].tolist() == list(range(58, 64)) and slots[most - 1:most + 7].tolist() == list(range(32, 40))
     assert slots[most + 99:most + 104].tolist() == list(range(75, 80)) and slots[most + 106:most + 113].tolist() == list(range(25, 32))
     assert int((slots >= 0).sum()) == 6 + 8 + 5 + 7 and int(slots.min()) == -1
+
+
+def test_a_length_beyond_31_bits_does_not_wrap():
+    """A table for more tokens than an int32 counts, all but full of them."""
+    print("2^31 tokens", flush=True)
+    width = 2**21 + 2
+    table = torch.full((1, width), 3, dtype=torch.int32, device="cuda")
+    slots, start, now, left = ints([-7] * 101), ints([-7] * 2), ints([-7]), ints([-7])
+    R.rsr_cache_slots(ints([2**31 - 10]), ints([100]), table, 1024, ints([8, 5]), ints([2]), slots, start, now, left, stream())
+    torch.cuda.synchronize()
+    assert now.tolist() == [2**31 - 1] and start.tolist() == [0, 100] and left.item() == 1
+    assert slots.tolist() == list(range(4 * 1024 - 10, 4 * 1024)) + list(range(5 * 1024, 5 * 1024 + 90)) + [-1]
+    assert table[0, -3:].tolist() == [3, 5, 3]
