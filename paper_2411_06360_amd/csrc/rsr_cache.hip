@@ -2,6 +2,7 @@
 // the masks of drafted trees.  The attention over the cache is in rsr_attend.hip.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <string>
 
@@ -249,10 +250,13 @@ int rsr_cache_append(const rsr_cache_t* cache, const void* k, const void* v, int
   if (fault) return set_error(RSR_ERR_INVALID_ARGUMENT, fault);
   AppendArgs a{k, v, rows, slots, static_cast<uint16_t*>(cache->k), static_cast<uint16_t*>(cache->v), stride, nrows, cache->page_stride, cache->head_stride,
                cache->token_stride, count, rsr_internal::log2_of(cache->page_size), cache->pages, (int32_t)(width / 8), cache->head_dim / 8, 1};
-  // as many tokens per workgroup as give its lanes an eight or two each
-  a.tokens_per_group = 2 * a.eights >= 2 * kAppendThreads ? 1 : 2 * kAppendThreads / (2 * a.eights);
-  const int64_t groups = (count + a.tokens_per_group - 1) / a.tokens_per_group;
-  if (groups > INT32_MAX) return set_error(RSR_ERR_INVALID_ARGUMENT, "count is too large");
+  // as many tokens per workgroup as give its lanes an eight or two each, or, if that made more lanes than a launch may have, as many as
+  // do not (their eights are numbered in 32 bits)
+  const int64_t most_groups = UINT32_MAX / kAppendThreads, few = 2 * a.eights >= 2 * kAppendThreads ? 1 : 2 * kAppendThreads / (2 * a.eights);
+  const int64_t tokens = std::max(few, (count - 1) / most_groups + 1);
+  if (tokens > UINT32_MAX / (2 * a.eights)) return set_error(RSR_ERR_INVALID_ARGUMENT, "count is too large");
+  a.tokens_per_group = (int32_t)tokens;
+  const int64_t groups = (count - 1) / tokens + 1;
   auto kern = cache->dtype == RSR_F16 ? (dtype == RSR_F32 ? append_kernel<_Float16, true> : append_kernel<_Float16, false>)
                                       : (dtype == RSR_F32 ? append_kernel<__bf16, true> : append_kernel<__bf16, false>);
   hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kAppendThreads), 0, static_cast<hipStream_t>(stream), a);

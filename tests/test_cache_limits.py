@@ -65,3 +65,11 @@ def test_the_stride_of_a_single_row_means_nothing():
         q, key, value, out = (row(w, s) for w, s in zip((32, 16, 16, 32), strides))
         with pytest.raises(R.RsrError, match="workspace"):
             R.rsr_tree_attention(cache, step, q, key, value, out, 4, 1.0, torch.zeros(16, dtype=torch.uint8))
+
+
+# ---- append ----
+def test_more_tokens_than_an_append_can_number_are_refused():
+    c = R.RsrCache(AT, AT, 1024 * 8 * 256, 8 * 256, 256, R.RSR_BF16, 10, 8, 1024, 256, 0)
+    append = lambda count: R.load().rsr_cache_append(ctypes.addressof(c), AT, AT, 1024 * 256, 4, R.RSR_BF16, None, AT, count, None)  # noqa: E731
+    for count in (2**41, 2**62, 2**63 - 1):
+        assert append(count) == INVALID and "count" in R.rsr_last_error()

@@ -58,3 +58,22 @@ def test_a_length_beyond_31_bits_does_not_wrap():
     assert now.tolist() == [2**31 - 1] and start.tolist() == [0, 100] and left.item() == 1
     assert slots.tolist() == list(range(4 * 1024 - 10, 4 * 1024)) + list(range(5 * 1024, 5 * 1024 + 90)) + [-1]
     assert table[0, -3:].tolist() == [3, 5, 3]
+
+
+def test_more_tokens_than_a_launch_has_workgroups():
+    """2^24 wide tokens, of which a few have a slot."""
+    print("many tokens", flush=True)
+    count, kv_heads, dim = 2**24 + 5, 16, 128
+    k, v = (torch.randn((7, kv_heads * dim), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    caches = [torch.zeros((2, kv_heads, 8, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    rows, slots = torch.zeros(count, dtype=torch.int32, device="cuda"), torch.full((count,), -1, dtype=torch.int32, device="cuda")
+    kept = {0: (3, 4), 1: (2, 9), 2**24 - 2: (6, 0), 2**24: (1, 15), count - 2: (5, 8), count - 1: (4, 7)}
+    for at, (row, slot) in kept.items():
+        rows[at], slots[at] = row, slot
+    R.rsr_cache_append(R.make_cache(*caches), k, v, slots, rows, stream())
+    torch.cuda.synchronize()
+    for cache, x in zip(caches, (k, v)):
+        want = torch.zeros_like(cache)
+        for row, slot in kept.values():
+            want[slot // 8, :, slot % 8] = x[row].view(kv_heads, dim)
+        assert torch.equal(cache, want)
