@@ -595,7 +595,7 @@ template <typename CT, bool FLOAT, int DP, int ROWS, int THREADS> __device__ inl
         }
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
-          if (c0 + k * shares >= u.pieces) mlc[k] = f2{-INFINITY, 0.f};
+          if (c0 + k * shares >= u.pieces) mlc[k] = f2{-INFINITY, 0.f}, xc[k] = f4{0, 0, 0, 0};  // (0 times an infinite value is NaN)
           top = fmaxf(top, mlc[k][0]);
         }
         const float back = behind(m, top);
@@ -1170,6 +1170,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 1 : 2) attend_shared(A
           for (int j = 0; j < kParts * kEach; ++j) rows[mt].acc[j] *= back;
 #pragma unroll
           for (int c = 0; c < kAtOnce; ++c) {
+            if (c0 + c >= u.pieces) break;  // (0 times an infinite value is NaN)
             const float by = behind(ml[c][0], top);
             l += ml[c][0] == -INFINITY ? ml[c][1] : ml[c][1] * by;  // (without a maximum: 0, or NaN)
 #pragma unroll

@@ -56,6 +56,27 @@ def test_one_sequence_of_twenty_heads(act, cache, new):
     s.check()
 
 
+@pytest.mark.parametrize("act,cache", KINDS)
+@pytest.mark.parametrize("dim", [64, 80, 128])
+@pytest.mark.parametrize("form", ["four", "eight", "shared"])
+@pytest.mark.parametrize("held", [20, 3000])
+def test_infinite_values_arrive_where_they_are_seen_and_nowhere_else(act, cache, dim, form, held):
+    print("infinite value", act, cache, dim, form, held, flush=True)
+    if form == "shared":
+        s = Step([held], [12], heads=4, kv_heads=2, dim=dim, act=act, cache=cache, seed=46)
+    else:
+        s = few_rows(form == "eight", [held], [8], heads=4, dim=dim, act=act, cache=cache, seed=46)
+    want = s.check().copy()
+    s.v[3, 5], s.v[3, 9] = float("inf"), -float("inf")  # token 3, two dimensions of the first key head
+    got = s.run()
+    sees = np.array([bool(int(m) >> 3 & 1) for m in s.mask.tolist()])
+    assert sees.any() and not sees.all()
+    at = np.array([a * dim + d for a in range(2) for d in (5, 9)])
+    assert (got[np.ix_(sees, at[0::2])] == np.inf).all() and (got[np.ix_(sees, at[1::2])] == -np.inf).all()
+    got[np.ix_(sees, at)] = want[np.ix_(sees, at)]
+    assert np.array_equal(got, want)
+
+
 def exact(s):
     """What oracle.attention gives for one request, in float64 on the GPU: many heads over long caches."""
     held, group, tokens = int(s.held[0]), s.heads // s.kv_heads, s.tokens
