@@ -63,7 +63,9 @@ typedef struct rsr_cache_t {
  *   requests   0 .. 65535
  *   tokens     rows in q, k, v and out (0 .. 2^31-1)
  *   max_new    no request has more new tokens (what goes beyond is left out); 1 .. 65535, at most 64 with a mask
- *   max_pages  length of a row of `table`
+ *   max_pages  length of a row of `table`.  The host sees no lengths: how rsr_tree_attention shares out its work goes by
+ *              requests, max_new and the tokens that max_pages could name, and tables far wider than what is held cost
+ *              time (up to twice as much: see there).
  *   table      DEVICE [requests][max_pages] int32, the block tables.  An entry outside 0 .. pages-1 stands for a
  *              page that is not there: its tokens are not seen (pages that were given up).
  *   held       DEVICE [requests] int32, tokens in the cache (taken as 0 if negative, and as what the table
@@ -84,8 +86,8 @@ typedef struct rsr_step_t {
  *   out[start[r]+i][a] = sum_p w_p v_p / sum_p w_p,   w_p = exp(scale * <q[start[r]+i][a], k_p>)
  * over the cached tokens of the request on pages that are there and the new tokens that i sees.  A token that
  * sees nothing gets zeros; what it does not see does not touch it, infinities and NaN included.  A seen key or
- * value that is not finite makes the results that it enters not finite (infinite or NaN), whatever the sign of the score; so does a
- * score beyond the range of float.
+ * value that is not finite makes the results that it enters not finite (infinite or NaN), whatever the sign of
+ * the score; so does a score beyond the range of float.
  *
  *   q        DEVICE, row t at q + t * q_stride elements: [heads][head_dim]
  *   k, v     DEVICE, row t at k + t * kv_stride: [kv_heads][head_dim]; rounded to the type of the cache
@@ -99,10 +101,16 @@ typedef struct rsr_step_t {
  *            ready for the next one.  Calls that share it must not overlap.  More requests, max_new, max_pages or heads never
  *            need fewer bytes: what is enough for a program's largest step over a cache is enough for all of them.
  *
- * Statistics, sums and, with RSR_F32, everything is held to 32 bits: float queries and weights are carried
- * through the matrix cores as sums of two float16 or three bfloat16.  With 16-bit activations the weights
- * are rounded to that type before they meet the values.  The order of additions is fixed for given lengths:
- * results are reproducible.
+ * Statistics and sums are held in 32 bits.  Float queries and weights are carried through the matrix cores as sums of
+ * three bfloat16 (all their 24 bits) or two float16 (22 bits).  With 16-bit activations the weights are rounded to
+ * that type before they meet the values: the error of the result is 1.4 times that of its own rounding (bfloat16
+ * 2.3e-3 for 1.7e-3, float16 2.8e-4 for 2.1e-4 of its norm).
+ * The order of additions is fixed for given lengths, sizes and max_pages of a step: the same call gives the same bits.  A request
+ * alone, in another batch or with a wider table may differ by rounding.
+ * More than 64 rows (new tokens times query heads) per key head: with tables for some 32768 tiles of 32 tokens and 64 rows, over all
+ * key heads, workgroups take 128 or 256 rows together, which pays over long caches alone.  (5 key heads, 64 tokens with four query
+ * heads each over 2000 tokens: 21 us with a table for up to 32768 tokens, 41 with one for 131072.  Eight requests of 32 such tokens: 28 us
+ * with tables for 2000 tokens, 46 from 32768 on.  One token over 500, 20 key heads: 12 and 14.)
  * Errors: RSR_ERR_INVALID_ARGUMENT, RSR_ERR_UNSUPPORTED (tables that could name more than some 2^47 tokens of all key heads),
  * RSR_ERR_HIP (launch failure).
  */

@@ -22,8 +22,8 @@
 // Measured on one MI355X, whole calls (a large copy moves 4.8 TB/s there, a sum reads 4.0, a large product does 1.23 PFLOP/s with
 // 16-bit operands): 32 requests of one token, 20 heads of 128, 8192 cached tokens each: 453 us, 5.9 TB/s of cache, bound by memory.
 // 16 drafted tokens over 4096, the same heads: 18 us for 42.6 MB; a token over 500: 12 us for 5.2 MB, a chain of latencies (lengths,
-// table, tiles, the join).  64 drafted tokens with four query heads per key head, 4 requests over 131072: 0.47 ms, 0.73 PFLOP/s;
-// one request over 2000: 22 us.
+// table, tiles, the join).  64 drafted tokens with four query heads per key head, 4 requests over 131072: 0.47 to 0.49 ms, 0.7 PFLOP/s;
+// one request over 2000: 21 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -410,7 +410,10 @@ template <typename CT, bool FLOAT, int DP> struct Rows {
     for (int j = 0; j < 8; ++j) s[j] = fmaf(x[j >> 2][j & 3], factor, -base);
   }
 
-  // Exponents to weights and to operand B of the result.
+  // Exponents to weights and to operand B of the result.  With 16-bit rows a weight is one operand of that type, 8 or 11 bits, and the
+  // sum is that of the rounded weights: the error is 1.4 times that of rounding the result.  (The rest as a second operand takes that
+  // away and costs twice the matrix instructions of the result: 4 x 64 tokens over 131072 762 us instead of 482, spilling in the loop;
+  // chains of 512 over 2048 110 instead of 79; with one tile of rows 1 to 7 % more.)
   //
   // A score of minus infinity (a key that is not finite, products beyond the range of float) would drop out with a weight of 0, and a
   // row of such scores would look like one that sees nothing.  Zero times the lowest exponent is NaN there and 0 else, and goes into
@@ -905,11 +908,13 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attend_split(Args a) {
 // lane; values: one position's eight dimensions), straight into LDS, where it lies in that order, a kilobyte per fragment without
 // bank conflicts, and is read by all of them.  kAhead tiles are on their way while one is computed: the cache answers after one to
 // two microseconds, a tile's products take a third of that. Counted with 4 requests of 64 tokens, four query heads per key head,
-// over 131072 (0.47 ms with pages of 64): the matrix cores work a third of the time, vector instructions (the weights, and turning
-// values) take two fifths, and between barriers all wavefronts want the same of the two at once; no bank conflicts.  Float rows
-// have two or three operands for each query and weight: 3 matrix instructions of bfloat16 where 16-bit rows have one.  Chains of
-// up to 512 tokens over up to 2048, 4 requests: 0.15 ms, of which a large product would need 63 us for these; new tokens are
-// converted on their way to LDS, which nothing hides.
+// over 131072 (0.47 to 0.49 ms with pages of 64): the matrix cores work a third of the time, vector instructions (the weights, and turning
+// values) take two fifths, and between barriers all wavefronts want the same of the two at once; no bank conflicts.  Two tiles of rows
+// of 128 dimensions spill 30 to 40 registers, with full heads and eight wavefronts none of them inside the loop over tiles, else one or
+// two a tile; one reload there waits for all tiles that are on their way (4 x 64 over 131072: 700 us).  Float rows have two or three
+// operands for each query and weight: 3 matrix instructions of bfloat16 where 16-bit rows have one, and 4 to 20 registers spilled, none
+// inside the loop.  Chains of up to 512 tokens over up to 2048, 4 requests: 145 us, of which a large product would need 63 us for these
+// (bfloat16 rows 79 us of 21); new float tokens are converted on their way to LDS, which nothing hides.
 constexpr int kWindow = 512;  // entries of a request's table in LDS
 
 // 16 bytes per lane from memory to the kilobyte of LDS at `to`, a place that nothing reads before wait_for_all_but has waited.  (The
@@ -1242,7 +1247,9 @@ Shape shape_of(const rsr_cache_t* cache, const rsr_step_t* step, int heads, bool
   // attend_shared: workgroups of 64 rows; with much work of 128, or, where there are as many, 256, two tiles of rows per
   // wavefront.  A fragment is then read from LDS once for both and a tile fetched once for all, but there are fewer workgroups for
   // a set's rows, and more to join for each.  (256 rows per key head: 4 x 131072 cached tokens 0.54 ms, with 64 rows 0.72; 8 x
-  // 8000 89 us against 106; 8 x 4000 61 against 60; 2000 41 against 22; a chain of 512 over 2048 48 against 42.  128 rows: 4 x 131072 352 us against 435, 8 x 16000 114 against 107.)
+  // 8000 89 us against 106; 8 x 4000 61 against 60; 2000 41 against 22; a chain of 512 over 2048 48 against 42.  128 rows: 4 x 131072
+  // 352 us against 435, 8 x 16000 114 against 107.)  The work is what the tables could name: the host knows no lengths, and a table for 131072
+  // tokens takes the 41 us where 2000 are held.
   const bool much = s.shared && !floats && s.dims < 256 && rows > 64 && sets * ((rows + 63) / 64) * tiles >= kMuch;
   s.row_tiles = much ? 2 : 1;
   // attend_split: four wavefronts, of which two workgroups per CU hide each other's waits.  Eight, one workgroup per CU, where few
