@@ -156,6 +156,14 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     L.rsr_cache_append.restype = ci
     L.rsr_tree_masks.argtypes = [vp, vp, ci, ci, vp, vp, vp]
     L.rsr_tree_masks.restype = ci
+    L.rsr_head_rotate.argtypes = [vp, vp, i64, ci, vp, i64, ci, ci, vp, i64, vp, i64, vp, i64, ci, vp]
+    L.rsr_head_rotate.restype = ci
+    L.rsr_sample_workspace.argtypes = [i64, i64]
+    L.rsr_sample_workspace.restype = i64
+    L.rsr_sample.argtypes = [vp, i64, i64, i64, ci, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.rsr_sample.restype = ci
+    L.rsr_tree_keep.argtypes = [vp, vp, vp, vp, ci, ci, vp, vp, vp, vp, vp]
+    L.rsr_tree_keep.restype = ci
     _lib = L
     return L
 
@@ -441,6 +449,98 @@ def rsr_tree_masks(parent, start, mask, depth, stream=None) -> None:
     tokens, requests = parent.numel(), start.numel() - 1
     code = (_lib or load()).rsr_tree_masks(_whole(parent, 32, 0), _whole(start, 32, 1), requests, tokens, _whole(mask, 64, tokens),
                                            _whole(depth, 32, tokens), _addr(stream))
+    if code:
+        _check(code)
+
+
+# ---- both sides of the attention (include/rsr_decode.h) ----
+class RsrRotary(ctypes.Structure):
+    _fields_ = [
+        ("frequency", ctypes.c_void_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+        ("norm", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rotated", ctypes.c_int32), ("pairs", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+def _numbers(x, kind: str, count: int) -> Optional[int]:
+    """Address of a contiguous tensor of floating-point numbers of that type, with at least `count` elements (None stays None)."""
+    if x is None:
+        return None
+    if str(x.dtype) != kind or x.numel() < count or not x.is_contiguous():
+        raise ValueError(f"a contiguous tensor of {count} numbers of {kind} is wanted")
+    return x.data_ptr()
+
+
+def make_rotary(frequency, head_dim: int, eps=None, q_weight=None, k_weight=None, pairs: bool = False) -> RsrRotary:
+    """rsr_rotary_t: ``frequency`` device float64, one for each pair of rotated dimensions (None: none are rotated); ``eps`` of the
+    norm (None: heads are not normed); ``q_weight``, ``k_weight`` device float32 ``[head_dim]`` or None.  It keeps the tensors alive."""
+    if eps is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("weights are the norm's: without eps there is none")
+    rotated = 0 if frequency is None else 2 * frequency.numel()
+    rotary = RsrRotary(_numbers(frequency, "torch.float64", 0), _numbers(q_weight, "torch.float32", head_dim), _numbers(k_weight, "torch.float32", head_dim),
+                       0.0 if eps is None else eps, eps is not None, head_dim, rotated, bool(pairs), 0)
+    rotary.tensors = frequency, q_weight, k_weight
+    return rotary
+
+
+def _heads(x, out, tokens: int, dim: int):
+    """(stride, heads, stride of the results) of rows of heads; nothing of None."""
+    if x is None or out is None:
+        if x is not out:
+            raise ValueError("rows and their results come together")
+        return 0, 0, 0
+    width = x.shape[-1]
+    if width % dim:
+        raise ValueError("a row is not a whole number of heads")
+    return _rows(x, tokens, width), width // dim, _rows(out, tokens, width)
+
+
+def rsr_head_rotate(rotary: RsrRotary, q, k, position, q_out, k_out, stream=None) -> None:
+    """``q``, ``q_out``: device ``[tokens][heads * head_dim]``, ``k``, ``k_out``: ``[tokens][kv_heads * head_dim]`` (slices of wider rows
+    will do; either pair may be None), inputs of one type and results of one type; ``position``: device int32 ``[tokens]``."""
+    some, result = (q, q_out) if q is not None else (k, k_out)
+    tokens, dim = position.numel(), rotary.head_dim
+    q_stride, heads, q_out_stride = _heads(q, q_out, tokens, dim)
+    k_stride, kv_heads, k_out_stride = _heads(k, k_out, tokens, dim)
+    dtype, out_dtype = some.dtype, result.dtype
+    if kv_heads and (k.dtype != dtype or k_out.dtype != out_dtype):
+        raise ValueError("queries and keys must have one type, and their results")
+    code = (_lib or load()).rsr_head_rotate(
+        ctypes.addressof(rotary), _addr(q), q_stride, heads, _addr(k), k_stride, kv_heads, _dtypes.get(dtype) or _dtype(some), _whole(position, 32, 0), tokens,
+        _addr(q_out), q_out_stride, _addr(k_out), k_out_stride, _dtypes.get(out_dtype) or _dtype(result), _addr(stream))
+    if code:
+        _check(code)
+
+
+def rsr_sample_workspace(rows: int, columns: int) -> int:
+    """Bytes of workspace that rsr_sample takes (zero it once)."""
+    n = load().rsr_sample_workspace(int(rows), int(columns))
+    if n < 0:
+        raise RsrError(n, rsr_last_error())
+    return n
+
+
+def rsr_sample(logits, uniform, token, workspace, temperature=None, top_k=None, top_p=None, min_p=None, probability=None, kept=None, stream=None) -> None:
+    """A ``token`` (device int32 ``[rows]``) for every row of ``logits`` (device ``[rows][columns]``, float32, float16 or bfloat16): the
+    parameters are device tensors with one number a row (``top_k`` int32, the others float32) or None, ``uniform`` float32 in [0, 1);
+    ``probability`` (float32) and ``kept`` (int32) are written unless they are None; ``workspace``: device bytes that were zero at first."""
+    rows, columns = logits.shape
+    real = "torch.float32"
+    code = (_lib or load()).rsr_sample(
+        logits.data_ptr(), rows, columns, _rows(logits, rows, columns), _dtypes.get(logits.dtype) or _dtype(logits), _numbers(temperature, real, rows),
+        None if top_k is None else _whole(top_k, 32, rows), _numbers(top_p, real, rows), _numbers(min_p, real, rows), _numbers(uniform, real, rows),
+        _whole(token, 32, rows), _numbers(probability, real, rows), None if kept is None else _whole(kept, 32, rows), workspace.data_ptr(), workspace.nbytes,
+        _addr(stream))
+    if code:
+        _check(code)
+
+
+def rsr_tree_keep(drafted, chosen, parent, start, rows, found, add, first, stream=None) -> None:
+    """The paths of drafted trees that agree with what was chosen: ``rows`` and ``found`` (device int32, one a token), ``add`` (one a
+    request) and ``first`` (one more), from ``drafted``, ``chosen`` and ``parent`` (None: chains) of the tokens; all int32."""
+    tokens, requests = drafted.numel(), start.numel() - 1
+    code = (_lib or load()).rsr_tree_keep(
+        _whole(drafted, 32, 0), _whole(chosen, 32, tokens), None if parent is None else _whole(parent, 32, tokens), _whole(start, 32, 1), requests, tokens,
+        _whole(rows, 32, tokens), _whole(found, 32, tokens), _whole(add, 32, requests), _whole(first, 32, requests + 1), _addr(stream))
     if code:
         _check(code)
 

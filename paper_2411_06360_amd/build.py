@@ -13,7 +13,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librsr.so")
-SOURCES = ["rsr_lib.hip", "rsr_dense.hip", "rsr_prep.hip", "rsr_pack.cpp", "rsr_export.cpp", "rsr_qbit.cpp", "rsr_cache.hip", "rsr_attend.hip"]
+SOURCES = ["rsr_lib.hip", "rsr_dense.hip", "rsr_prep.hip", "rsr_pack.cpp", "rsr_export.cpp", "rsr_qbit.cpp", "rsr_cache.hip", "rsr_attend.hip",
+           "rsr_decode.hip", "rsr_sample.hip"]
 ARCH = "gfx950"
 
 # -packed-fp32-ops off: the compiler must not form packed fp32 instructions from the float adds.
