@@ -1,14 +1,18 @@
 // A token for every row of scores (include/rsr_decode.h).
 //
 // With the scores in order, the highest first, everything that is asked for is a place in one running sum: of tokens (top-k), of
-// weights (top-p, the token itself), or a score (min-p).  No row is sorted for that.
-//   1. One pass finds the highest score and counts the scores in 16383 steps between the lowest and the highest of some of
-//      them (those above go into a list).  Counts times the weights at a step's ends bound every sum of weights from both sides, by some
-//      hundredths or tenths of a percent, and so the steps in which the places can be.
-//   2. A second pass adds up what lies before these steps, in 64 bits, and gathers what is in them in LDS, where it is sorted and the
-//      places are found.
-// If too many tokens are there (thousands of equal scores, say), the slow way is taken: a histogram with count and weight of each bin, 2048
+// weights (top-p, the token itself), or a score (min-p).  No row is sorted for that; a look at some thousand of its scores comes first.
+//   Where few tokens can be kept (a small top_k, or min_p without top_p) it says above which score all of them lie, and enough, and one pass
+// gathers those in LDS, where they are sorted and the places found.
+//   Else one pass counts the scores in some thousand steps between those that were looked at (the few above go into a list).  Counts
+// times the weights of the steps' middles tell every sum of weights to some hundredths of a percent, and so in which steps the places are.  A
+// second pass adds up what lies before these, in 64 bits, and gathers what is in them.  It computes a weight for every score, which
+// takes longer than reading it, and several workgroups share it.
+//   If too many tokens are there (thousands of equal scores, say) the slow way is taken: a histogram with count and weight of each bin, 2048
 // bins of 1/32 of an octave of weight, and place after place with finer ones of what is left.
+//
+// A row is one workgroup's, of sixteen wavefronts: what all of them compute alike costs four times what one of them takes, so one
+// alone plans and finds, and the others wait.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -29,8 +33,13 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 2 * kThreads;  // two for each thread
 constexpr int kPerOctave = 32;       // bins
 constexpr int kList = 2 * kThreads;  // tokens that are sorted at once
-constexpr int kSteps = 16 * kThreads;  // of counted scores; the first has what is above all others
-constexpr int kPeaks = 2 * kThreads;   // scores above the steps
+constexpr int kSteps = 8 * kThreads;  // of counted scores; the first has what is above all others
+constexpr int kPeaks = 2 * kThreads;  // scores above the steps
+constexpr int kBounded = 512;         // top_k up to here is looked up in one pass
+constexpr int kGroups = 256;          // workgroups of a launch: one for each CU
+constexpr int kLeastPiece = 8192;     // scores of a workgroup, where several have a row
+constexpr int kLeastGathering = 2;    // workgroups of a row in the second pass
+constexpr int kMostRows = 1024;       // of a launch
 constexpr int kPrefix = 1024;        // tokens that are rather gathered from the first one on than counted
 
 // What a bin adds up in one word: for each token a one above, and below how much less than the bin's most its weight is, in units of
@@ -51,37 +60,104 @@ struct Args {
   int32_t columns, log2_columns;  // log2_columns: bits of a column's number
 };
 
-constexpr int kPlaces = 7, kMostRuns = 4;
+constexpr int kMostRuns = 4;
 
-// The bin or step of a place, with the sums up to it and up to and with it.
+// The step of a place, with the sums up to it and up to and with it.
 struct Mark {
   int bin;
   uint32_t before, count;
-  double mass_before, mass;
+  float mass_before, mass;
 };
 
-struct Lds {
-  union {
-    uint32_t steps[kSteps];                     // counted scores
-    struct {
-      u64 list[kList];                          // tokens, sorted
-      double upto[kList];                       // weight up to and with each
-      uint32_t count[kBins];                    // up to and with the bin
-      union { u64 sum[kBins]; double mass[kBins]; };  // packed as above; then the weight up to and with the bin
-      uint32_t part_count[kBins + 1];           // of a finer histogram, or where buckets begin
-      union { u64 part_sum[kBins]; double part_mass[kBins]; u64 bucketed[kList]; };
-    };
-  };
-  float peaks[kPeaks];
-  u64 weight[kMostRuns + 1];  // before each run, and of all
-  Mark mark[2 * kMostRuns + 1];
-  double wave_mass[kWaves];
-  uint32_t wave_count[kWaves];
-  u64 wave_best[kWaves];
-  float wave_low[kWaves], wave_high[kWaves];
-  uint32_t place[kPlaces];  // bins of places
+// Scores to steps, the higher ones first: 0 for what is above the first of the others, the last but one for what is below them.  (A
+// difference of halves, which is not beyond the range of float, times the steps of half a unit.)
+struct Steps {
+  float from, half, per;
+  __device__ __forceinline__ float down(float x) const { return fmaf(-0.5f, x, half) * per; }
+  __device__ __forceinline__ float score(int step) const { return 2.f * (half - (float)step / per); }  // at about the end of a step
+  static __device__ __forceinline__ int step(float down) { return down < 0.f ? 0 : 1 + (int)__builtin_amdgcn_fmed3f(down, 0.f, (float)(kSteps - 3)); }
+  // The bounds of `down` from step lo to step hi, both included.
+  static __device__ __forceinline__ float first_of(int lo) { return lo ? (float)(lo - 1) : -INFINITY; }
+  static __device__ __forceinline__ float last_of(int hi) { return hi >= kSteps - 2 ? INFINITY : hi ? __uint_as_float(__float_as_uint((float)hi) - 1) : -FLT_MIN; }
+};
+
+// Tokens of neighbouring steps that lie in the list, one run behind the other.
+struct Run {
+  int b0, b1;                     // steps
+  uint32_t start, count, before;  // where it begins in the list, how many there are, and before them in the row
+  int shift;                      // how far apart its buckets are, for sorting
+  u64 code;                       // about that of the first
+  double mass_before;             // the weight of those before
+
+  // as many buckets as tokens, or half as many, from one code to another
+  __device__ __forceinline__ void span(u64 from, u64 to) {
+    code = from;
+    shift = max(0, __clz((int)count) + 33 - __clzll((long long)(to > from ? to - from : 1)));
+  }
+  __device__ __forceinline__ uint32_t bucket(u64 x) const { return start + (x < code ? 0 : (uint32_t)min((x - code) >> shift, (u64)(count - 1))); }
+};
+
+// What the second pass has to do.
+struct Plan {
+  Run run[kMostRuns];
+  int n;            // runs
+  int near;         // the run up to this step has the last token that min_p keeps; -1: min_p keeps all
+  uint32_t tokens;  // of all runs
+  uint32_t all;     // of the row
+  int weighed;      // it adds up weights
+  int slow;         // too many tokens
+};
+
+// What a row is asked for.
+struct Ask {
+  double factor;   // octaves of weight in a unit of scores
+  double top_p;    // 2: all
+  double far;      // the distance of the last that min_p keeps, or infinity
+  double u;
+  uint32_t top_k;  // 0: all
+};
+
+// What is known of a row before the second pass.
+struct Head {
+  int32_t answered;
+  float top;
+  Steps steps;
+  Ask ask;
+  Plan plan;
+};
+
+// For sums over the wavefronts of a workgroup, and what one of them tells the others.
+struct Waves {
+  double mass[kWaves];
+  uint32_t count[kWaves];
+  u64 best[kWaves];
+  float low[kWaves], high[kWaves];
+  Head head;
+  uint32_t arrived, sure;
+};
+
+// Of a workgroup that counts scores.
+struct Counts {
+  uint32_t steps[kSteps + 64];
+  float peaks[kPeaks];  // scores above the steps
+  float looked[kThreads];
+  float bound;
+  Mark mark[2 * kMostRuns];
+  uint32_t before[2];
   uint32_t listed, all_count;
-  double all_mass;
+  float all_mass;
+};
+
+// Of one that gathers tokens.
+struct Lists {
+  u64 list[kList];                                // tokens, sorted
+  double upto[kList];                             // weight up to and with each
+  uint32_t part_count[kBins + 1];                 // of a finer histogram, or where buckets begin
+  union { u64 part_sum[kBins]; double part_mass[kBins]; u64 bucketed[kList]; };
+  uint32_t count[kBins];                          // of the slow way: up to and with the bin
+  union { u64 sum[kBins]; double mass[kBins]; };  // packed as above; then the weight up to and with the bin
+  u64 weight[kMostRuns + 1];                      // before each run, and of all
+  uint32_t listed, first;
 };
 
 // ---- scores -----------------------------------------------------------------------------------------------
@@ -98,9 +174,9 @@ template <typename T> struct Key {
   }
 };
 
-// f(scores, column of the first) for pieces of `count` scores of a row from column `first` on, by all threads of the workgroup, each in
-// ascending order.  Reads are 16 bytes wide wherever the row begins, 16 scores on their way while 16 are looked at; what sticks out at the ends is read by
-// itself and comes with minus infinity behind it.
+// f(scores, column of the first) for 16 bytes of `count` scores of a row from column `first` on at a time, by all threads of the
+// workgroup, each in ascending order, wherever the row begins; sixteen scores are on their way while sixteen are looked at.  What sticks out at
+// the ends is read by itself and comes with minus infinity behind it.
 template <typename T, typename F> __device__ __forceinline__ void for_pieces(const T* row, int first, int count, F f) {
   typedef const __attribute__((address_space(1))) T* Scores;
   typedef const __attribute__((address_space(1))) u4* Pieces;
@@ -165,26 +241,35 @@ template <typename T, typename F> __device__ __forceinline__ void for_each(const
 struct Scale {
   float top;
   double factor;
-  __device__ double distance(float x) const { return x == top ? 0.0 : ((double)top - (double)x) * factor; }
-  __device__ double weight(float x) const { return exp2(-distance(x)); }
+  __device__ __forceinline__ double distance(float x) const { return x == top ? 0.0 : ((double)top - (double)x) * factor; }
+  // 2^f, f from -1/2 to 1/2, is the polynomial that has its values at nine Chebyshev nodes, off by 2^-39 of it.  A thousand octaves
+  // down nothing is left of a weight.
+  static __device__ __forceinline__ void split(double distance, double& p, double& power) {
+    const double d = fmin(distance, 1000.0), n = rint(d), f = n - d;
+    p = 1.0 + f * (0.6931471805459335 + f * (0.2402265069581299 + f * (0.05550410941205934 + f * (0.009618129159402607 + f * (0.0013333450567999429 +
+        f * (0.00015403455852420792 + f * (1.5310079402541085e-05 + f * 1.3255224885567153e-06)))))));
+    power = __builtin_bit_cast(double, (u64)((uint32_t)(1023 - (int)n) << 20) << 32);
+  }
+  __device__ __forceinline__ double weight(float x) const {
+    double p, power;
+    split(distance(x), p, power);
+    return p * power;
+  }
 };
+__device__ __forceinline__ int bin_of(double distance) { return (int)fmin(distance * kPerOctave, (double)(kBins - 1)); }
 
-// Sums of weights in units of 2^-40 of the highest's, in whole numbers, so that no order of additions matters.  2^f, f from -1/2 to 1/2,
-// is the polynomial that has its values at nine Chebyshev nodes (off by 2^-39 of it); a weight is added to 2^12, where 2^-40 is the last
-// bit, and the bits of that are added up.
+// Sums of weights in units of 2^-40 of the highest's, in whole numbers, so that no order of additions matters: a weight is added to 2^12,
+// where 2^-40 is the last bit, and the bits of that are added up.
 struct Weights {
   double top, factor;
   static constexpr double kAbove = 0x1p12;
   __device__ __forceinline__ u64 of(float x) const {
-    const double d = fmin((top - (double)x) * factor, 1000.0), n = rint(d), f = n - d;  // (nothing is left of the weight there)
-    const double p = 1.0 + f * (0.6931471805459335 + f * (0.2402265069581299 + f * (0.05550410941205934 + f * (0.009618129159402607 + f * (0.0013333450567999429 +
-                     f * (0.00015403455852420792 + f * (1.5310079402541085e-05 + f * 1.3255224885567153e-06)))))));
-    const uint32_t power = (uint32_t)(1023 - (int)n) << 20;
-    return __builtin_bit_cast(u64, fma(p, __builtin_bit_cast(double, (u64)power << 32), kAbove));
+    double p, power;
+    Scale::split((top - (double)x) * factor, p, power);
+    return __builtin_bit_cast(u64, fma(p, power, kAbove));
   }
   static __device__ __forceinline__ u64 none() { return __builtin_bit_cast(u64, kAbove); }
 };
-__device__ __forceinline__ int bin_of(double distance) { return (int)fmin(distance * kPerOctave, (double)(kBins - 1)); }
 
 // 2^34 times 1 - 2^-(f / 32) for f from 0 to 1, as a sum of powers of f ln 2 / 32 (the sixth adds less than 2^-42).  Of the last bin,
 // which has all that is 64 octaves down and more, nothing is weighed.
@@ -233,20 +318,28 @@ template <typename T> __device__ __forceinline__ T of_lane(T x, int lane) {
   }
 }
 
-// Running sums of two entries per thread, in their order, and what is before them.
-struct Sums {
-  uint32_t c[2], c_before;
-  double m[2], m_before;
+// The largest of the lanes of 16, and of all; of what the wavefronts wrote down.
+template <int CTRL, int ROWS> __device__ __forceinline__ float largest_step(float x) {
+  return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float largest_of_16(float x) { return largest_step<0x118, 0xf>(largest_step<0x114, 0xf>(largest_step<0x112, 0xf>(largest_step<0x111, 0xf>(x)))); }
+__device__ __forceinline__ float largest(float x) { return of_lane(largest_step<0x143, 0xc>(largest_step<0x142, 0xa>(largest_of_16(x))), 63); }
+__device__ __forceinline__ float largest_of_waves(const float* x) { return of_lane(largest_of_16(x[threadIdx.x & 15]), 15); }
 
-  __device__ __forceinline__ void scan(Lds& lds, uint32_t c0, double m0) {
+// Running sums of two entries per thread, in their order, and what is before them.
+template <typename M> struct Sums {
+  uint32_t c[2], c_before;
+  M m[2], m_before;
+
+  __device__ __forceinline__ void scan(Waves& waves, uint32_t c0, M m0) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t cs = sum_of_lanes(c[0] + c[1]);
-    const double ms = sum_of_lanes(m[0] + m[1]);
+    const M ms = sum_of_lanes(m[0] + m[1]);
     __syncthreads();
-    if (lane == 63) lds.wave_count[wave] = cs, lds.wave_mass[wave] = ms;
+    if (lane == 63) waves.count[wave] = cs, waves.mass[wave] = ms;
     __syncthreads();
-    const uint32_t cw = sum_of_16(lds.wave_count[lane & 15]);
-    const double mw = sum_of_16(lds.wave_mass[lane & 15]);
+    const uint32_t cw = sum_of_16(waves.count[lane & 15]);
+    const M mw = sum_of_16((M)waves.mass[lane & 15]);
     c_before = c0, m_before = m0;
     if (wave) c_before += of_lane(cw, wave - 1), m_before += of_lane(mw, wave - 1);
     c_before += moved<0x138, 0xf>(cs), m_before += moved<0x138, 0xf>(ms);  // (of the lane before)
@@ -256,17 +349,18 @@ struct Sums {
 
 // ---- places -----------------------------------------------------------------------------------------------
 // The place where a running sum reaches what is asked for.
-struct Place {
+template <typename M> struct Place {
   bool of_count, strict;  // a sum of tokens (at least `count`), or of weights: at least `mass`, or more than that
   uint32_t count;
-  double mass;
-  __device__ bool reached(uint32_t c, double m) const { return of_count ? c >= count : strict ? m > mass : m >= mass; }
-  static __device__ Place tokens(uint32_t n) { return {true, false, n, 0.0}; }
-  static __device__ Place weight(double m, bool more) { return {false, more, 0, m}; }
+  M mass;
+  __device__ __forceinline__ bool reached(uint32_t c, M m) const { return of_count ? c >= count : strict ? m > mass : m >= mass; }
+  static __device__ __forceinline__ Place tokens(uint32_t n) { return {true, false, n, 0}; }
+  static __device__ __forceinline__ Place weight(M m, bool more) { return {false, more, 0, m}; }
 };
+typedef Place<double> At;
 
 // The first of n running sums that reaches the place; the last one if none does.
-__device__ __forceinline__ int first_at(const Place& p, const uint32_t* count, const double* mass, int n) {
+__device__ __forceinline__ int first_at(const At& p, const uint32_t* count, const double* mass, int n) {
   int lo = 0, hi = n - 1;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
@@ -275,37 +369,6 @@ __device__ __forceinline__ int first_at(const Place& p, const uint32_t* count, c
   }
   return lo;
 }
-
-// Tokens of neighbouring steps that lie in the list, one run behind the other.
-struct Run {
-  int b0, b1;                     // steps
-  uint32_t start, count, before;  // where it begins in the list, how many there are, and before them in the row
-  double mass_before;             // and the weight of those
-  u64 code;                       // about that of the first, for sorting
-  int shift;                      // and how far apart its buckets are
-
-  // as many buckets as tokens, or half as many, from one code to another
-  __device__ __forceinline__ void span(u64 from, u64 to) {
-    code = from;
-    shift = max(0, __clz((int)count) + 33 - __clzll((long long)(to > from ? to - from : 1)));
-  }
-  __device__ __forceinline__ uint32_t bucket(u64 x) const { return start + (x < code ? 0 : (uint32_t)min((x - code) >> shift, (u64)(count - 1))); }
-};
-struct Runs {
-  static constexpr int kMost = kMostRuns;
-  Run run[kMost];
-  int n;
-  int near;         // the run up to this step has the last token that min_p keeps; -1: min_p keeps all
-  uint32_t tokens;  // of all runs
-};
-
-// What a row is asked for.
-struct Ask {
-  uint32_t top_k;  // 0: all
-  double top_p;    // 2: all
-  double far;      // the distance of the last that min_p keeps, or infinity
-  double u;
-};
 
 struct Found {
   u64 code;
@@ -324,7 +387,7 @@ template <typename T> struct Row {
   __device__ int column(u64 code) const { return (int)(code & (((u64)1 << log2_columns) - 1)); }
 
   // Tokens that are wanted, into the list in any order; how many there are (they may be more than fit).
-  template <typename W> __device__ __forceinline__ uint32_t gather(Lds& lds, W wanted) const {
+  template <typename W> __device__ __forceinline__ uint32_t gather(Lists& lds, W wanted) const {
     __syncthreads();
     if (threadIdx.x == 0) lds.listed = 0;
     __syncthreads();
@@ -339,9 +402,9 @@ template <typename T> struct Row {
 
   // Sorts the list and adds up its weights.  Codes are dealt into buckets, as many for each run as it has tokens, and each finds its
   // place among those of its bucket.  (What lies outside the bounds of its run lands in a bucket at the end, still in order.)
-  __device__ __forceinline__ void sort(Lds& lds, const Runs& runs) const {
+  __device__ __forceinline__ void sort(Waves& waves, Lists& lds, const Plan& plan) const {
     const int tid = threadIdx.x;
-    const uint32_t n = runs.tokens;
+    const uint32_t n = plan.tokens;
     u64 x[2];
     uint32_t bucket[2], slot[2];
     lds.part_count[2 * tid] = lds.part_count[2 * tid + 1] = 0;
@@ -351,17 +414,17 @@ template <typename T> struct Row {
       const uint32_t i = tid + j * kThreads;
       if (i >= n) continue;
       x[j] = lds.list[i];
-      bucket[j] = runs.run[0].bucket(x[j]);
+      bucket[j] = plan.run[0].bucket(x[j]);
 #pragma unroll
-      for (int k = 1; k < Runs::kMost; ++k)
-        if (k < runs.n && x[j] >= runs.run[k].code) bucket[j] = runs.run[k].bucket(x[j]);
+      for (int k = 1; k < kMostRuns; ++k)
+        if (k < plan.n && x[j] >= plan.run[k].code) bucket[j] = plan.run[k].bucket(x[j]);
       slot[j] = atomicAdd(&lds.part_count[bucket[j]], 1u);
     }
     __syncthreads();
-    Sums s;
+    Sums<double> s;
 #pragma unroll
     for (int j = 0; j < 2; ++j) s.c[j] = lds.part_count[2 * tid + j], s.m[j] = 0.0;
-    s.scan(lds, 0, 0.0);
+    s.scan(waves, 0, 0.0);
     lds.part_count[2 * tid] = s.c_before, lds.part_count[2 * tid + 1] = s.c[0];
     if (tid == kThreads - 1) lds.part_count[kBins] = s.c[1];
     __syncthreads();
@@ -380,52 +443,52 @@ template <typename T> struct Row {
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 2; ++j) s.c[j] = 0, s.m[j] = 2 * tid + j < n ? scale.weight(score(lds.list[2 * tid + j])) : 0.0;
-    s.scan(lds, 0, 0.0);
+    s.scan(waves, 0, 0.0);
     lds.upto[2 * tid] = s.m[0], lds.upto[2 * tid + 1] = s.m[1];
     __syncthreads();
   }
 
   // ---- places in the list
-  static __device__ double mass_at(const Lds& lds, const Run& r, uint32_t i) { return r.mass_before + (lds.upto[i] - (r.start ? lds.upto[r.start - 1] : 0.0)); }
+  static __device__ double mass_at(const Lists& lds, const Run& r, uint32_t i) { return r.mass_before + (lds.upto[i] - (r.start ? lds.upto[r.start - 1] : 0.0)); }
   // The first token of the list at the place, and its run.  (Loops over runs are unrolled: they stay in registers.)
-  static __device__ __forceinline__ uint32_t seek(const Lds& lds, const Runs& runs, Place p, Run& r) {
-    r = runs.run[0];
+  static __device__ __forceinline__ uint32_t seek(const Lists& lds, const Plan& plan, At p, Run& r) {
+    r = plan.run[0];
 #pragma unroll
-    for (int i = 1; i < Runs::kMost; ++i)
-      if (i < runs.n && !p.reached(r.before + r.count, mass_at(lds, r, r.start + r.count - 1))) r = runs.run[i];
+    for (int i = 1; i < kMostRuns; ++i)
+      if (i < plan.n && !p.reached(r.before + r.count, mass_at(lds, r, r.start + r.count - 1))) r = plan.run[i];
     if (p.of_count) return r.start + min(max(p.count, r.before + 1) - r.before, r.count) - 1;
     p.mass -= r.mass_before - (r.start ? lds.upto[r.start - 1] : 0.0);
     return r.start + first_at(p, nullptr, lds.upto + r.start, r.count);
   }
 
   // Whether the place that seek found is where the sum reaches it: not before its run, and not behind.
-  static __device__ bool sure(const Lds& lds, const Place& p, const Run& r, uint32_t all) {
+  static __device__ bool sure(const Lists& lds, const At& p, const Run& r, uint32_t all) {
     return (!r.before || !p.reached(r.before, r.mass_before)) && (r.before + r.count == all || p.reached(r.before + r.count, mass_at(lds, r, r.start + r.count - 1)));
   }
 
   // The answer, where the list has all places.  `kept`, `mass`: all tokens and their weight (if a place or the token needs it).  Nothing
   // is `sure` if a place is in none of the runs.
-  __device__ __forceinline__ Found solve(const Lds& lds, const Ask& ask, const Runs& runs, uint32_t kept, double mass) const {
+  __device__ __forceinline__ Found solve(const Lists& lds, const Ask& ask, const Plan& plan, uint32_t kept, double mass) const {
     Run r;
     bool is_sure = true;
     const uint32_t all = kept;
     if (ask.top_k && ask.top_k < kept) {
-      const Place p = Place::tokens(ask.top_k);
-      const uint32_t at = seek(lds, runs, p, r);
+      const At p = At::tokens(ask.top_k);
+      const uint32_t at = seek(lds, plan, p, r);
       is_sure &= sure(lds, p, r, all);
       kept = ask.top_k, mass = mass_at(lds, r, at);
     }
     if (ask.top_p < 1.0) {
-      const Place p = Place::weight(ask.top_p * mass, false);
-      const uint32_t at = seek(lds, runs, p, r), n = r.before + at - r.start + 1;
+      const At p = At::weight(ask.top_p * mass, false);
+      const uint32_t at = seek(lds, plan, p, r), n = r.before + at - r.start + 1;
       is_sure &= sure(lds, p, r, all);
       if (n < kept) kept = n, mass = mass_at(lds, r, at);
     }
-    if (runs.near >= 0) {
-      r = runs.run[0];
+    if (plan.near >= 0) {
+      r = plan.run[0];
 #pragma unroll
-      for (int i = 1; i < Runs::kMost; ++i)
-        if (i < runs.n && runs.run[i].b0 <= runs.near) r = runs.run[i];
+      for (int i = 1; i < kMostRuns; ++i)
+        if (i < plan.n && plan.run[i].b0 <= plan.near) r = plan.run[i];
       uint32_t lo = 0, hi = r.count;  // how many are near enough
       while (lo < hi) {
         const uint32_t mid = (lo + hi) / 2;
@@ -435,14 +498,14 @@ template <typename T> struct Row {
       is_sure &= lo < r.count || r.before + r.count >= kept;
       if (r.before + lo < kept) kept = r.before + lo, mass = lo ? mass_at(lds, r, r.start + lo - 1) : r.mass_before;
     }
-    const Place p = Place::weight(ask.u * mass, true);
-    const uint32_t at = seek(lds, runs, p, r);
+    const At p = At::weight(ask.u * mass, true);
+    const uint32_t at = seek(lds, plan, p, r);
     return {lds.list[at], scale.weight(score(lds.list[at])) / mass, kept, is_sure && sure(lds, p, r, all)};
   }
 
   // ---- place after place (a list for each), where there are too many tokens for one list
   // The run of tokens in which the place is.
-  __device__ __attribute__((noinline)) Run run_at(Lds& lds, const Place& p) const {
+  __device__ __attribute__((noinline)) Run run_at(Waves& waves, Lists& lds, const At& p) const {
     const int tid = threadIdx.x;
     int b = first_at(p, lds.count, lds.mass, kBins);
     while (b && lds.count[b] == lds.count[b - 1]) --b;  // (what rounding puts behind the last token is the last token's)
@@ -451,7 +514,7 @@ template <typename T> struct Row {
     u64 lo = 0, hi = ((u64)1 << (32 + log2_columns)) - 1;
     while (count > kList) {
       const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 11);
-      Sums s{{0, 0}, 0, {0.0, 0.0}, 0.0};
+      Sums<double> s{{0, 0}, 0, {0.0, 0.0}, 0.0};
       for (int first = 0; first < columns; first += kChunk) {
         __syncthreads();
         lds.part_sum[2 * tid] = lds.part_sum[2 * tid + 1] = 0;
@@ -466,7 +529,7 @@ template <typename T> struct Row {
 #pragma unroll
         for (int j = 0; j < 2; ++j) s.c[j] += count_in(lds.part_sum[2 * tid + j]), s.m[j] += mass_in(lds.part_sum[2 * tid + j], b);
       }
-      s.scan(lds, before, mass_before);
+      s.scan(waves, before, mass_before);
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < 2; ++j) lds.part_count[2 * tid + j] = s.c[j], lds.part_mass[2 * tid + j] = s.m[j];
@@ -483,35 +546,35 @@ template <typename T> struct Row {
       const u64 c = code(x, column);
       return bin_of(scale.distance(x)) == b && c >= lo && c <= hi;
     });
-    Runs runs;
-    runs.n = 1, runs.near = -1, runs.tokens = count;
-    Run& r = runs.run[0];
-    r = {b, b, 0, count, before, mass_before, 0, 0};
+    Plan plan;
+    plan.n = 1, plan.near = -1, plan.tokens = count;
+    Run& r = plan.run[0];
+    r = {b, b, 0, count, before, 0, 0, mass_before};
     if (!lo && scale.top < INFINITY)  // (the bin's ends, or what is left of it)
       lo = code((float)((double)scale.top - b / (kPerOctave * scale.factor)), 0), hi = code((float)((double)scale.top - (b + 1) / (kPerOctave * scale.factor)), 0);
     r.span(lo, hi);
-    sort(lds, runs);
+    sort(waves, lds, plan);
     return r;
   }
 
-  __device__ __attribute__((noinline)) Found solve_slowly(Lds& lds, const Ask& ask) const {
+  __device__ __attribute__((noinline)) Found solve_slowly(Waves& waves, Lists& lds, const Ask& ask) const {
     uint32_t kept = lds.count[kBins - 1];
     double mass = lds.mass[kBins - 1];
-    Runs runs{};
+    Plan plan{};
     Run r;
     uint32_t at;
-    auto find = [&](const Place& p) {
-      const Run& have = runs.run[0];
-      const bool here = runs.n && !p.reached(have.before, have.mass_before) && p.reached(have.before + have.count, mass_at(lds, have, have.count - 1));
-      if (!here) runs.run[0] = run_at(lds, p), runs.n = 1;
-      at = seek(lds, runs, p, r);
+    auto find = [&](const At& p) {
+      const Run& have = plan.run[0];
+      const bool here = plan.n && !p.reached(have.before, have.mass_before) && p.reached(have.before + have.count, mass_at(lds, have, have.count - 1));
+      if (!here) plan.run[0] = run_at(waves, lds, p), plan.n = 1;
+      at = seek(lds, plan, p, r);
     };
     if (ask.top_k && ask.top_k < kept) {
-      find(Place::tokens(ask.top_k));
+      find(At::tokens(ask.top_k));
       kept = ask.top_k, mass = mass_at(lds, r, at);
     }
     if (ask.top_p < 1.0) {
-      find(Place::weight(ask.top_p * mass, false));
+      find(At::weight(ask.top_p * mass, false));
       const uint32_t n = r.before + at + 1;
       if (n < kept) kept = n, mass = mass_at(lds, r, at);
     }
@@ -537,270 +600,324 @@ template <typename T> struct Row {
         if (before + n < kept) kept = before + n, mass = (b ? lds.mass[b - 1] : 0.0) + sum;
       }
     }
-    find(Place::weight(ask.u * mass, true));
+    find(At::weight(ask.u * mass, true));
     return {lds.list[at], scale.weight(score(lds.list[at])) / mass, kept, true};
   }
 };
 
-// ---- steps ------------------------------------------------------------------------------------------------
-// Scores to steps, the higher ones first: 0 for what is above the first of the others, the last but one for what is below them.  (A
-// difference of halves, which is not beyond the range of float, times the steps of half a unit.)
-struct Steps {
-  float from, half, per;
-  __device__ __forceinline__ float down(float x) const { return fmaf(-0.5f, x, half) * per; }
-  __device__ __forceinline__ float score(int step) const { return 2.f * (half - (float)step / per); }  // at about the end of a step
-  static __device__ __forceinline__ int step(float down) { return down < 0.f ? 0 : 1 + (int)min((uint32_t)down, (uint32_t)(kSteps - 3)); }
-  // The bounds of `down` from step lo to step hi, both included.
-  static __device__ __forceinline__ float first_of(int lo) { return lo ? (float)(lo - 1) : -INFINITY; }
-  static __device__ __forceinline__ float last_of(int hi) { return hi >= kSteps - 2 ? INFINITY : hi ? __uint_as_float(__float_as_uint((float)hi) - 1) : -FLT_MIN; }
-};
+// ---- a look at a row --------------------------------------------------------------------------------------
+__device__ __forceinline__ float parameter(const float* p, int64_t r, float without) { return p ? p[r] : without; }
 
-__device__ __forceinline__ void over_lanes_max(float& x) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+__device__ __forceinline__ Ask ask_of(const Args& a, int64_t r, float temperature) {
+  const float top_p = parameter(a.top_p, r, 1.f), min_p = parameter(a.min_p, r, 0.f), uniform = a.uniform[r];
+  const int top_k = a.top_k ? a.top_k[r] : 0;
+  // (0 times infinity is NaN)
+  return {fmax(1.4426950408889634 / (double)temperature, 1e-300), top_p < 1.f ? fmax((double)top_p, 0.0) : 2.0,
+          min_p > 0.f ? min_p >= 1.f ? 0.0 : -log2((double)min_p) : INFINITY, uniform > 0.f ? fmin((double)uniform, 1.0 - 0x1p-24) : 0.0,
+          top_k > 0 && top_k < a.columns ? (uint32_t)top_k : 0u};
 }
 
-// Steps from the highest of some thousand scores of a row down to the lowest, or to the last that has any weight.
-template <typename T> __device__ __forceinline__ Steps look(Lds& lds, const Row<T>& row, double factor) {
+// Steps from the fourth highest or so of some thousand scores of a row down to the lowest, or to the last that has any weight, and a bound
+// above which lie the tokens that can be kept, if they are few (else NaN): where top_k is small, the score of which so many are above
+// among the highest of four to eight that enough of the row's are, and some hundred more; with min_p alone, the least that it may come to.
+template <typename T> __device__ __forceinline__ void look(const Args& a, int64_t r, const T* row, float temperature, Waves& waves, Counts& lds) {
+  constexpr int kWide = 16 / sizeof(T);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(T), pieces = (a.columns - head) / kWide, looked = min(pieces, kThreads);
+  float high = -INFINITY, low = INFINITY;
+  if (tid < looked) {
+    const u4 v = *reinterpret_cast<const u4*>(row + head + (int64_t)((int64_t)tid * pieces / looked) * kWide);
+    T x[kWide];
+    __builtin_memcpy(x, &v, 16);
+#pragma unroll
+    for (int j = 0; j < kWide; ++j) {
+      const float f = (float)x[j];
+      if (f > -INFINITY && f < INFINITY) high = fmaxf(high, f), low = fminf(low, f);
+    }
+  }
+  Ask ask;
+  if (wave == 0) ask = ask_of(a, r, temperature);
+  lds.looked[tid] = high;
+  high = largest(high), low = largest(-low);
+  if (lane == 0) waves.high[wave] = high, waves.low[wave] = low;
+  __syncthreads();
+  if (wave == 0) {
+    low = -largest_of_waves(waves.low);
+    const float mine = waves.high[lane & (kWaves - 1)];
+    high = of_lane(largest_of_16(mine), 15);
+    // above the first step are a hundred scores or so: those above the `rank`-th of the wavefronts' highest
+    const int rank = max(1, min(kWaves / 4, (kWaves / 4 << 17) / a.columns));
+    int higher = 0;
+    for (int w = 0; w < kWaves; ++w) {
+      const float other = of_lane(mine, w);
+      higher += other > mine || (other == mine && w < (lane & (kWaves - 1)));
+    }
+    const float from = of_lane(mine, __builtin_ctzll(__ballot(higher == rank - 1)));
+    Steps steps{-FLT_MAX, -FLT_MAX / 2, 1.f};
+    if (from > -INFINITY) {
+      const double range = fmin((double)from - (double)low, 48.0 / ask.factor);
+      steps = {from, 0.5f * from, (float)fmin(2.0 * (kSteps - 3) / range, (double)FLT_MAX)};
+    }
+    float bound = NAN;
+    if (ask.top_k && ask.top_k <= kBounded) {
+      const float share = (float)ask.top_k * (float)(looked * kWide) / (float)a.columns;
+      const int wanted = (int)(share + 5.f * sqrtf(share) + 8.f);
+      float down[kThreads / 64];
+#pragma unroll
+      for (int j = 0; j < kThreads / 64; ++j) down[j] = steps.down(lds.looked[j * 64 + lane]);
+      int least = 0, most = kSteps;
+      while (most - least > 4) {
+        const int mid = (least + most) / 2;
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < kThreads / 64; ++j) n += __popcll(__ballot(down[j] <= (float)mid));
+        if (n >= wanted) most = mid;
+        else least = mid;
+      }
+      bound = most >= kSteps - 4 ? INFINITY : (float)most;
+    } else if (ask.far < INFINITY && ask.top_p >= 1.0) {
+      const float x = (float)fmax((double)high - ask.far / ask.factor, -(double)FLT_MAX);
+      bound = high > -INFINITY ? fmaxf(steps.down(x), 0.f) + 1.f : NAN;
+    }
+    if (lane == 0) waves.head.ask = ask, waves.head.steps = steps, lds.bound = bound;
+  }
+}
+
+// The first pass: the highest score, whether one is NaN, and the tokens above the bound, or else all scores counted in steps and those above
+// the steps in a list.
+template <typename T> __device__ __forceinline__ float gather_above(Waves& waves, Lists& lds, const Row<T>& row, const Steps& steps, float bound, bool& nan) {
   constexpr int kWide = 16 / sizeof(T);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int head = (int)((16 - (reinterpret_cast<uintptr_t>(row.row) & 15)) & 15) / (int)sizeof(T), pieces = (row.columns - head) / kWide;
-  const u4 v = *reinterpret_cast<const u4*>(row.row + head + (int64_t)((int64_t)tid * pieces / kThreads) * kWide);
-  T x[kWide];
-  __builtin_memcpy(x, &v, 16);
-  float high = -INFINITY, low = INFINITY;
-#pragma unroll
-  for (int j = 0; j < kWide; ++j) {
-    const float f = (float)x[j];
-    if (f > -INFINITY && f < INFINITY) high = fmaxf(high, f), low = fminf(low, f);
-  }
-  low = -low;
-  over_lanes_max(high), over_lanes_max(low);
-  if (lane == 0) lds.wave_high[wave] = high, lds.wave_low[wave] = low;
+  if (tid == 0) lds.listed = 0;
   __syncthreads();
-  // Above the first step are some hundred scores: those above the `rank`-th of the wavefronts' highest.
-  const int rank = max(1, min(kWaves / 4, (kWaves / 4 << 17) / row.columns));
-  const float mine = lds.wave_high[lane & (kWaves - 1)];
-  int higher = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    const float other = lds.wave_high[w];
-    higher += other > mine || (other == mine && w < (lane & (kWaves - 1)));
-    low = fmaxf(low, lds.wave_low[w]);
-  }
-  high = of_lane(mine, __builtin_ctzll(__ballot(higher == rank - 1)));
-  low = -low;
-  if (!(high > -INFINITY)) return {-FLT_MAX, -FLT_MAX / 2, 1.f};
-  const double range = fmin((double)high - (double)low, 48.0 / factor);
-  return {high, 0.5f * high, (float)fmin(2.0 * (kSteps - 3) / range, (double)FLT_MAX)};
+  float high = -INFINITY;
+  for_pieces(row.row, 0, row.columns, [&](const float (&x)[kWide], int column) {
+    bool some = false;
+#pragma unroll
+    for (int j = 0; j < kWide; ++j) {
+      high = __builtin_elementwise_maximum(high, x[j]);  // (NaN stays)
+      some |= steps.down(x[j]) <= bound;
+    }
+    if (some)
+#pragma unroll
+      for (int j = 0; j < kWide; ++j)
+        if (steps.down(x[j]) <= bound && x[j] > -INFINITY) {
+          const uint32_t at = atomicAdd(&lds.listed, 1u);
+          if (at < kList) lds.list[at] = row.code(x[j], column + j);
+        }
+  });
+  nan = __syncthreads_or(high != high);
+  high = largest(high);
+  if (lane == 0) waves.high[wave] = high;
+  __syncthreads();
+  return largest_of_waves(waves.high);
 }
 
-// Counts scores in steps, lists those above them; the highest score, and whether one is NaN.
-template <typename T> __device__ __forceinline__ float count_steps(Lds& lds, const Row<T>& row, const Steps& steps, int first, int count, bool& nan) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+template <typename T> __device__ __forceinline__ float count_steps(Waves& waves, Counts& lds, const Row<T>& row, const Steps& steps, bool& nan) {
+  constexpr int kWide = 16 / sizeof(T);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, aside = kSteps + lane;
   u4* const zero = reinterpret_cast<u4*>(lds.steps);
   for (int i = tid; i < kSteps / 4; i += kThreads) zero[i] = u4{0, 0, 0, 0};
   if (tid == 0) lds.listed = 0;
   __syncthreads();
   float high = -INFINITY;
-  for_pieces(row.row, first, count, [&](const float (&x)[16 / sizeof(T)], int) {
-    bool above = false;
+  for_pieces(row.row, 0, row.columns, [&](const float (&x)[kWide], int) {
+    float least = 0.f;
 #pragma unroll
-    for (int j = 0; j < 16 / (int)sizeof(T); ++j) {
-      high = __builtin_elementwise_maximum(high, x[j]);  // (NaN stays)
+    for (int j = 0; j < kWide; ++j) {
       const float down = steps.down(x[j]);
-      above |= down < 0.f;
-      if (down >= 0.f && x[j] > -INFINITY) atomicAdd(&lds.steps[1 + min((uint32_t)down, (uint32_t)(kSteps - 3))], 1u);
+      high = __builtin_elementwise_maximum(high, x[j]);  // (NaN stays)
+      least = __builtin_elementwise_minimum(least, down);
+      // what is not counted is added somewhere else, so that there is no branch
+      const int step = 1 + (int)__builtin_amdgcn_fmed3f(down, 0.f, (float)(kSteps - 3));
+      atomicAdd(&lds.steps[down >= 0.f && x[j] > -INFINITY ? step : aside], 1u);
     }
-    if (above)  // (seldom)
+    if (!(least >= 0.f))  // (seldom; NaN comes here too, and is none of them)
 #pragma unroll
-      for (int j = 0; j < 16 / (int)sizeof(T); ++j)
+      for (int j = 0; j < kWide; ++j)
         if (steps.down(x[j]) < 0.f) {
           const uint32_t at = atomicAdd(&lds.listed, 1u);
           if (at < kPeaks) lds.peaks[at] = x[j];
         }
   });
   nan = __syncthreads_or(high != high);
-  over_lanes_max(high);
-  if (lane == 0) lds.wave_high[wave] = high;
+  high = largest(high);
+  if (lane == 0) waves.high[wave] = high;
   __syncthreads();
-  for (int w = 0; w < kWaves; ++w) high = fmaxf(high, lds.wave_high[w]);
-  return high;
+  return largest_of_waves(waves.high);
 }
-
-struct Plan {
-  Runs runs;
-  uint32_t all;   // tokens
-  bool weighed;   // the second pass adds up weights
-  bool slow;      // too many tokens
-};
 
 // In which steps the places may be, and so which tokens are gathered.  The scores above the steps are weighed one by one, a step as its
 // count times the weight in its middle.  Where a step's scores lie in it is not known: it is off by its weight times its width (in
 // ln 2 octaves) over the root of 12, as if they all lay at one place of which any is as likely, and the sums of all are off by the root of the
 // squares of that; six times as much is allowed for.  (Whether that was enough is seen in the end.)
-__device__ __forceinline__ Plan plan_of(Lds& lds, const Scale& scale, const Steps& steps, const Ask& ask) {
+__device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale& scale) {
   constexpr int kEach = kSteps / kThreads;
-  constexpr double kRounded = 1e-5;  // of a sum: what weights are rounded by here, and more
+  constexpr float kRounded = 1e-5f;  // of a sum: what weights are rounded by here, and more
+  static_assert(kEach == 8);
+  typedef Place<float> About;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  static_assert(kEach == 16);
+  const Ask& ask = waves.head.ask;
+  const Steps steps = waves.head.steps;
   const uint32_t peaks = lds.listed;
-  Plan plan;
-  plan.slow = peaks > kPeaks || scale.top == INFINITY;
-  if (plan.slow) return plan;
-  double peak = 0.0;
+  if (peaks > kPeaks || scale.top == INFINITY) {
+    if (tid == 0) waves.head.plan.slow = 1;
+    __syncthreads();
+    return;
+  }
+  float peak = 0.f;
 #pragma unroll
   for (int j = 0; j < 2; ++j)
-    if ((uint32_t)(tid + j * kThreads) < peaks) peak += scale.weight(lds.peaks[tid + j * kThreads]);
+    if ((uint32_t)(tid + j * kThreads) < peaks) peak += (float)scale.weight(lds.peaks[tid + j * kThreads]);
   peak = sum_of_lanes(peak);
-  if (lane == 63) lds.wave_mass[wave] = peak;
+  if (lane == 63) waves.low[wave] = peak;
   if (tid == 0) lds.steps[0] = peaks;
   if (tid < 2 * kMostRuns) lds.mark[tid].bin = kSteps;
   __syncthreads();
-  peak = 0.0;
-  for (int w = 0; w < kWaves; ++w) peak += lds.wave_mass[w];
+  peak = of_lane(sum_of_16(waves.low[lane & 15]), 15);
 
   // the sums of each thread's steps
-  const double octaves = 2.0 * scale.factor / steps.per, above = ((double)scale.top - (double)steps.from) * scale.factor - 0.5 * octaves;
-  auto weight_of = [&](uint32_t n, int step) { return step ? n * (double)__builtin_amdgcn_exp2f(-fmaxf((float)(above + step * octaves), 0.f)) : peak; };
+  const double wide = 2.0 * scale.factor / steps.per, above = ((double)scale.top - (double)steps.from) * scale.factor - 0.5 * wide;
+  const float octaves = (float)wide;
+  auto weight_of = [&](uint32_t n, int step) { return step ? (float)n * __builtin_amdgcn_exp2f(-fmaxf((float)(above + step * wide), 0.f)) : peak; };
+  const float first = (float)(above + tid * kEach * wide);
   float squares = 0.f;
-  Sums s{{0, 0}, 0, {0.0, 0.0}, 0.0};
+  Sums<float> s{{0, 0}, 0, {0.f, 0.f}, 0.f};
 #pragma unroll
   for (int j = 0; j < kEach / 4; ++j) {
     const u4 n = reinterpret_cast<const u4*>(lds.steps)[tid * (kEach / 4) + j];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int step = tid * kEach + 4 * j + i;
-      const double w = weight_of(n[i], step);
-      s.c[0] += n[i], s.m[0] += w;
-      squares += step ? (float)(w * w) : 0.f;
+      float w = (float)n[i] * __builtin_amdgcn_exp2f(-fmaxf(fmaf((float)(4 * j + i), octaves, first), 0.f));
+      if (i == 0 && j == 0) w = tid ? w : 0.f;
+      s.c[0] += n[i], s.m[0] += w, squares = fmaf(w, w, squares);
     }
   }
-  s.scan(lds, 0, 0.0);
+  if (tid == 0) s.m[0] += peak;
   squares = sum_of_lanes(squares);
-  if (lane == 63) lds.wave_low[wave] = squares;
+  if (lane == 63) waves.high[wave] = squares;
+  s.scan(waves, 0, 0.f);
   if (tid == kThreads - 1) lds.all_count = s.c[0], lds.all_mass = s.m[0];
   // The step of a place: the wavefront in which a thread's sums reach it adds up the steps of that thread, a lane each.
-  auto mark = [&](int place, auto reached) {
-    const u64 here = __ballot(s.c[0] > s.c_before && reached(s.c[0], s.m[0]) && (!s.c_before || !reached(s.c_before, s.m_before)));
+  auto mark = [&](int place, const About& p) {
+    const u64 here = __ballot(s.c[0] > s.c_before && p.reached(s.c[0], s.m[0]) && (!s.c_before || !p.reached(s.c_before, s.m_before)));
     if (!here) return;
     const int thread = __builtin_ctzll(here), step = ((wave << 6) + thread) * kEach + (lane & (kEach - 1));
-    const uint32_t n = lds.steps[step], c = of_lane(s.c_before, thread) + sum_of_16(n);
-    const double w = weight_of(n, step), m = of_lane(s.m_before, thread) + sum_of_16(w);
-    const u64 some = __ballot(lane < kEach && n), at = __ballot(lane < kEach && n && reached(c, m));
+    const uint32_t n = lane < kEach ? lds.steps[step] : 0, c = of_lane(s.c_before, thread) + sum_of_16(n);
+    const float w = lane < kEach ? weight_of(n, step) : 0.f, m = of_lane(s.m_before, thread) + sum_of_16(w);
+    const u64 some = __ballot(n != 0), at = __ballot(n && p.reached(c, m));
     if (lane == (at ? __builtin_ctzll(at) : 63 - __builtin_clzll(some))) lds.mark[place] = {step, c - n, c, m - w, m};
   };
-  auto up_to = [&](double mass, bool more) { return [=](uint32_t, double m) { return more ? m > mass : m >= mass; }; };
-  auto tokens = [&](uint32_t count) { return [=](uint32_t c, double) { return c >= count; }; };
-
-  __syncthreads();
-  const uint32_t all = lds.all_count;
-  const double total = lds.all_mass;
-  squares = 0.f;
-  for (int w = 0; w < kWaves; ++w) squares += lds.wave_low[w];
-  const double off = 6.0 * 0.6931471805599453 / 3.4641016151377544 * octaves * sqrt((double)squares) + kRounded * total;
-  const bool k = ask.top_k && ask.top_k < all, p = ask.top_p < 1.0;
-  bool m = ask.far < INFINITY;
-  mark(0, tokens(all));
-  if (k) mark(1, tokens(ask.top_k));
-  if (m) {
-    // the first tokens from the step before that of the last score that is kept on, and from the one behind it on
+  const bool far = ask.far < INFINITY;
+  if (far) {
+    // tokens before the step before that of the last score that is kept, and before the one behind it
     const int step = Steps::step(steps.down((float)((double)scale.top - ask.far / scale.factor)));
-    const int at[2] = {max(step - 1, 0), min(step + 1, kSteps - 1)};
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (tid == at[i] / kEach) {
-        uint32_t c = s.c_before;
-        for (int j = 0; j < at[i] % kEach; ++j) c += lds.steps[tid * kEach + j];
-        lds.place[i] = c;
-      }
-    __syncthreads();
-    mark(4, tokens(lds.place[0] + 1)), mark(5, tokens(lds.place[1] + 1));
+    for (int i = 0; i < 2; ++i) {
+      const int at = i ? min(step + 1, kSteps - 1) : max(step - 1, 0);
+      if (tid != at / kEach) continue;
+      uint32_t c = s.c_before;
+      for (int j = 0; j < at % kEach; ++j) c += lds.steps[tid * kEach + j];
+      lds.before[i] = c;
+    }
   }
   __syncthreads();
+  const uint32_t all = lds.all_count;
+  const float total = lds.all_mass;
+  const float off = 1.2005660f * octaves * sqrtf(of_lane(sum_of_16(waves.high[lane & 15]), 15)) + kRounded * total;  // (6 ln 2 / sqrt 12)
+  const bool k = ask.top_k && ask.top_k < all, p = ask.top_p < 1.0;
+  mark(0, About::tokens(all));
+  if (k) mark(1, About::tokens(ask.top_k));
+  if (far) mark(4, About::tokens(lds.before[0] + 1)), mark(5, About::tokens(lds.before[1] + 1));
+  __syncthreads();
+  // What is kept ends at `end` at the latest; its weight is between `least` and `most`.
   auto marked = [&](int place, const Mark& end) { return lds.mark[place].bin < end.bin ? lds.mark[place] : end; };
   Mark end = lds.mark[0];
-  int lo[Runs::kMost], hi[Runs::kMost];             // of top_k, top_p, min_p, and the token
-  uint32_t before[Runs::kMost], upto[Runs::kMost];  // tokens before, and up to and with
+  int lo[kMostRuns], hi[kMostRuns];             // of top_k, top_p, min_p, and the token
+  uint32_t before[kMostRuns], upto[kMostRuns];  // tokens before, and up to and with
 #pragma unroll
-  for (int i = 0; i < Runs::kMost; ++i) lo[i] = hi[i] = kSteps, before[i] = upto[i] = 0;  // none
-  double least = total - off, most = total + off;
+  for (int i = 0; i < kMostRuns; ++i) lo[i] = hi[i] = kSteps, before[i] = upto[i] = 0;  // none
+  float least = total - off, most = total + off;
   if (k) {
     end = lds.mark[1];
     lo[0] = hi[0] = end.bin, before[0] = end.before, upto[0] = end.count;
     least = end.mass_before - off, most = end.mass + off;
   }
   if (p) {
-    mark(2, up_to(ask.top_p * least - off, false)), mark(3, up_to(ask.top_p * most + off, false));
+    mark(2, About::weight((float)ask.top_p * least - off, false)), mark(3, About::weight((float)ask.top_p * most + off, false));
     __syncthreads();
     const Mark a = marked(2, end);
     end = marked(3, end);
     lo[1] = a.bin, before[1] = a.before, hi[1] = end.bin, upto[1] = end.count;
-    least = fmin(least, a.mass_before - off), most = fmin(most, end.mass + off);
+    least = fminf(least, a.mass_before - off), most = fminf(most, end.mass + off);
   }
-  plan.runs.near = -1;
-  m = m && lds.mark[4].bin <= end.bin;
+  const bool m = far && lds.mark[4].bin <= end.bin;
   if (m) {
     const Mark a = lds.mark[4];
     end = marked(5, end);
     lo[2] = a.bin, before[2] = a.before, hi[2] = end.bin, upto[2] = end.count;
-    least = fmin(least, a.mass_before - off), most = fmin(most, end.mass + off);
-    plan.runs.near = end.bin;
+    least = fminf(least, a.mass_before - off), most = fminf(most, end.mass + off);
   }
+  const int near = m ? end.bin : -1;
   const Mark last = all <= kList ? lds.mark[0] : k ? lds.mark[1] : end;  // (the weight of the first top_k is asked for)
-  if (last.count <= kPrefix || all <= kList) {
-    plan.runs.n = 1, plan.runs.tokens = last.count, plan.runs.run[0] = {0, last.bin, 0, last.count, 0, 0.0, 0, 0};
-#pragma unroll
-    for (int i = 1; i < Runs::kMost; ++i) plan.runs.run[i] = {kSteps, kSteps, 0, 0, 0, 0.0, 0, 0};
-    plan.all = all, plan.weighed = last.count < all && !k && (p || !m);
-    __syncthreads();
-    return plan;
-  }
-  mark(6, up_to(ask.u * least - off, true)), mark(7, up_to(ask.u * most + off, true));
+  const bool prefix = last.count <= kPrefix || all <= kList;
+  if (!prefix) mark(6, About::weight((float)ask.u * least - off, true)), mark(7, About::weight((float)ask.u * most + off, true));
   __syncthreads();
-  {
-    const Mark a = marked(6, end), b = marked(7, end);
-    lo[3] = a.bin, before[3] = a.before, hi[3] = b.bin, upto[3] = b.count;
-  }
-  // in order
-  auto order = [&](int i, int j) {
-    if (lo[j] < lo[i]) {
-      const int l = lo[i], h = hi[i];
-      const uint32_t x = before[i], y = upto[i];
-      lo[i] = lo[j], hi[i] = hi[j], before[i] = before[j], upto[i] = upto[j];
-      lo[j] = l, hi[j] = h, before[j] = x, upto[j] = y;
+  if (wave == 0) {
+    Plan plan;
+    plan.near = near, plan.all = all;
+    if (prefix) {
+      lo[0] = 0, hi[0] = last.bin, before[0] = 0, upto[0] = last.count;
+#pragma unroll
+      for (int i = 1; i < kMostRuns; ++i) lo[i] = hi[i] = kSteps;
+      plan.weighed = last.count < all && !k && (p || !m);
+    } else {
+      const Mark a = marked(6, end), b = marked(7, end);
+      lo[3] = a.bin, before[3] = a.before, hi[3] = b.bin, upto[3] = b.count;
+      plan.weighed = true;
+      // in order
+      auto order = [&](int i, int j) {
+        if (lo[j] < lo[i]) {
+          const int l = lo[i], h = hi[i];
+          const uint32_t x = before[i], y = upto[i];
+          lo[i] = lo[j], hi[i] = hi[j], before[i] = before[j], upto[i] = upto[j];
+          lo[j] = l, hi[j] = h, before[j] = x, upto[j] = y;
+        }
+      };
+      order(0, 1), order(2, 3), order(0, 2), order(1, 3), order(1, 2);
+      // What meets is one: those that do are taken into the one before, and the others move up.
+#pragma unroll
+      for (int i = 1; i < kMostRuns; ++i)
+        if (lo[i] < kSteps) hi[i] = max(hi[i], hi[i - 1]), upto[i] = max(upto[i], upto[i - 1]);
+#pragma unroll
+      for (int i = kMostRuns - 1; i; --i)
+        if (lo[i] < kSteps && lo[i] <= hi[i - 1] + 1) {
+          hi[i - 1] = hi[i], upto[i - 1] = upto[i];
+#pragma unroll
+          for (int j = i; j < kMostRuns; ++j) {
+            const bool more = j + 1 < kMostRuns;
+            lo[j] = more ? lo[(j + 1) % kMostRuns] : kSteps, hi[j] = more ? hi[(j + 1) % kMostRuns] : kSteps;
+            before[j] = more ? before[(j + 1) % kMostRuns] : 0, upto[j] = more ? upto[(j + 1) % kMostRuns] : 0;
+          }
+        }
     }
-  };
-  order(0, 1), order(2, 3), order(0, 2), order(1, 3), order(1, 2);
-  // What meets is one: those that do are taken into the one before, and the others move up.
+    plan.n = 0, plan.tokens = 0;
 #pragma unroll
-  for (int i = 1; i < Runs::kMost; ++i)
-    if (lo[i] < kSteps) hi[i] = max(hi[i], hi[i - 1]), upto[i] = max(upto[i], upto[i - 1]);
-#pragma unroll
-  for (int i = Runs::kMost - 1; i; --i)
-    if (lo[i] < kSteps && lo[i] <= hi[i - 1] + 1) {
-      hi[i - 1] = hi[i], upto[i - 1] = upto[i];
-#pragma unroll
-      for (int j = i; j < Runs::kMost; ++j) {
-        const bool more = j + 1 < Runs::kMost;
-        lo[j] = more ? lo[(j + 1) % Runs::kMost] : kSteps, hi[j] = more ? hi[(j + 1) % Runs::kMost] : kSteps;
-        before[j] = more ? before[(j + 1) % Runs::kMost] : 0, upto[j] = more ? upto[(j + 1) % Runs::kMost] : 0;
-      }
+    for (int i = 0; i < kMostRuns; ++i) {
+      const bool there = lo[i] < kSteps;
+      plan.run[i] = {lo[i], hi[i], plan.tokens, there ? upto[i] - before[i] : 0, before[i], 0, 0, 0.0};
+      plan.tokens += plan.run[i].count, plan.n += there;
     }
-  plan.runs.n = 0, plan.runs.tokens = 0;
-#pragma unroll
-  for (int i = 0; i < Runs::kMost; ++i) {
-    plan.runs.run[i] = {lo[i], hi[i], plan.runs.tokens, upto[i] - before[i], before[i], 0.0, 0, 0};
-    plan.runs.tokens += upto[i] - before[i], plan.runs.n += lo[i] < kSteps;
+    plan.slow = plan.tokens > kList;
+    if (lane == 0) waves.head.plan = plan;
   }
-  plan.all = all, plan.weighed = true, plan.slow = plan.runs.tokens > kList;
   __syncthreads();
-  return plan;
 }
 
+// ---- the second pass --------------------------------------------------------------------------------------
 // Gathers the tokens of the plan's runs among `count` scores from `first` on.  RUNS: adds up the weights before each of so many runs too, and
-// of all, in units of 2^-40: a thread's sums of them are exact, and so are those of all threads.  0: there is one run, from the first
-// token on.
-template <int RUNS, typename T> __device__ __forceinline__ void gather_runs(Lds& lds, const Row<T>& row, const Steps& steps, const Runs& runs, int first, int count) {
+// of all.  0: there is one run, from the first token on.
+template <int RUNS, typename T> __device__ __forceinline__ void gather_runs(const Plan& plan, Lists& lds, const Row<T>& row, const Steps& steps, int first, int count) {
   constexpr int kWide = 16 / sizeof(T), kRuns = RUNS ? RUNS : 1;
   if (threadIdx.x == 0) lds.listed = 0;
   if (threadIdx.x <= kMostRuns) lds.weight[threadIdx.x] = 0;
@@ -811,8 +928,8 @@ template <int RUNS, typename T> __device__ __forceinline__ void gather_runs(Lds&
   uint32_t pieces = 0;
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
-    const bool there = i < runs.n;
-    lo[i] = there ? Steps::first_of(runs.run[i].b0) : INFINITY, hi[i] = there ? Steps::last_of(runs.run[i].b1) : -INFINITY, before[i] = 0;
+    const bool there = i < plan.n;
+    lo[i] = there ? Steps::first_of(plan.run[i].b0) : INFINITY, hi[i] = there ? Steps::last_of(plan.run[i].b1) : -INFINITY, before[i] = 0;
   }
   auto wanted = [&](float down) {
     bool in = false;
@@ -834,14 +951,13 @@ template <int RUNS, typename T> __device__ __forceinline__ void gather_runs(Lds&
       }
     }
     ++pieces;
-    if (some) {
+    if (some)
 #pragma unroll
       for (int j = 0; j < kWide; ++j)
         if (wanted(steps.down(x[j])) && x[j] > -INFINITY) {
           const uint32_t at = atomicAdd(&lds.listed, 1u);
           if (at < kList) lds.list[at] = row.code(x[j], column + j);
         }
-    }
   });
   if constexpr (RUNS) {
     const u64 none = (u64)pieces * kWide * Weights::none();
@@ -856,87 +972,93 @@ template <int RUNS, typename T> __device__ __forceinline__ void gather_runs(Lds&
   __syncthreads();
 }
 
-__device__ __forceinline__ float parameter(const float* p, int64_t r, float without) { return p ? p[r] : without; }
+template <typename T> __device__ __forceinline__ void gather_plan(const Plan& plan, Lists& lds, const Row<T>& row, const Steps& steps, int first, int count) {
+  if (!plan.weighed) gather_runs<0>(plan, lds, row, steps, first, count);
+  else if (plan.n == 1) gather_runs<1>(plan, lds, row, steps, first, count);
+  else if (plan.n == 2) gather_runs<2>(plan, lds, row, steps, first, count);
+  else gather_runs<4>(plan, lds, row, steps, first, count);
+}
 
-template <typename T> __global__ void __launch_bounds__(kThreads) sample_kernel(Args a) {
-  __shared__ Lds lds;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t r = blockIdx.x;
-  Row<T> row{static_cast<const T*>(a.logits) + r * a.stride, a.columns, a.log2_columns, {0.f, 0.0}};
-  auto answer = [&](int token, float probability, uint32_t kept) {
-    if (tid) return;
-    a.token[r] = token;
-    if (a.probability) a.probability[r] = probability;
-    if (a.kept) a.kept[r] = (int32_t)kept;
-  };
-  const float temperature = parameter(a.temperature, r, 1.f), top_p = parameter(a.top_p, r, 1.f), min_p = parameter(a.min_p, r, 0.f), uniform = a.uniform[r];
-  const int top_k = a.top_k ? a.top_k[r] : 0;
-  const Ask ask{top_k > 0 && top_k < a.columns ? (uint32_t)top_k : 0u, top_p < 1.f ? fmax((double)top_p, 0.0) : 2.0,
-                min_p > 0.f ? min_p >= 1.f ? 0.0 : -log2((double)min_p) : INFINITY, uniform > 0.f ? fmin((double)uniform, 1.0 - 0x1p-24) : 0.0};
-  row.scale.factor = fmax(1.4426950408889634 / (double)temperature, 1e-300);  // (0 times infinity is NaN)
-  auto give = [&](const Found& f) { answer(row.column(f.code), (float)f.share, f.kept); };
+// ---- answers ----------------------------------------------------------------------------------------------
+__device__ __forceinline__ void answer(const Args& a, int64_t r, int token, float probability, uint32_t kept) {
+  if (threadIdx.x) return;
+  a.token[r] = token;
+  if (a.probability) a.probability[r] = probability;
+  if (a.kept) a.kept[r] = (int32_t)kept;
+}
 
-  if (!(temperature > 0.f) || a.columns <= kList) {
-    // ---- the highest score, and few
-    float high = -INFINITY, low = INFINITY;
-    int at = 0;
-    bool nan = false;
-    for_each(row.row, 0, a.columns, [&](float x, int column) {
-      nan |= x != x;
-      low = x > -INFINITY ? fminf(low, x) : low;
-      const bool more = x > high;
-      high = more ? x : high, at = more ? column : at;
-    });
-    u64 best = high > -INFINITY ? row.code(high, at) : ~(u64)0;
-    low = -low;
+// True if the row is answered with what is known of its highest score.
+template <typename T> __device__ __forceinline__ bool is_answered(const Args& a, int64_t r, const Row<T>& row, u64 best, bool nan, bool greedy) {
+  if (nan) answer(a, r, -1, NAN, 0);
+  else if (best == ~(u64)0) answer(a, r, -1, 0.f, 0);
+  else if (greedy) answer(a, r, row.column(best), 1.f, 1);
+  else return false;
+  return true;
+}
+
+// The first of the highest scores, as a code (all ones: there is none), and the lowest.
+template <typename T> __device__ __forceinline__ u64 best_of(Waves& lds, const Row<T>& row, float& low, bool& nan) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float high = -INFINITY;
+  int at = 0;
+  nan = false, low = INFINITY;
+  for_each(row.row, 0, row.columns, [&](float x, int column) {
+    nan |= x != x;
+    low = x > -INFINITY ? fminf(low, x) : low;
+    const bool more = x > high;
+    high = more ? x : high, at = more ? column : at;
+  });
+  u64 best = high > -INFINITY ? row.code(high, at) : ~(u64)0;
+  low = largest(-low);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) best = min(best, (u64)__shfl_xor((long long)best, d));
-    over_lanes_max(low);
-    if (lane == 0) lds.wave_best[wave] = best, lds.wave_low[wave] = low;
-    nan = __syncthreads_or(nan);
-    for (int w = 0; w < kWaves; ++w) best = min(best, lds.wave_best[w]), low = fmaxf(low, lds.wave_low[w]);
-    if (nan) return answer(-1, NAN, 0);
-    if (best == ~(u64)0) return answer(-1, 0.f, 0);
-    if (!(temperature > 0.f)) return answer(row.column(best), 1.f, 1);
-    row.scale.top = row.score(best);
-    const uint32_t n = row.gather(lds, [&](float, int) { return true; });
-    Runs runs;
-    runs.n = 1, runs.run[0] = {0, kSteps, 0, n, 0, 0.0, 0, 0}, runs.tokens = n, runs.near = ask.far < INFINITY ? 0 : -1;
-    runs.run[0].span(best, row.code(-low, row.columns - 1));
-    row.sort(lds, runs);
-    return give(row.solve(lds, ask, runs, n, lds.upto[n - 1]));
-  }
+  for (int d = 32; d; d >>= 1) best = min(best, (u64)__shfl_xor((long long)best, d));
+  if (lane == 0) lds.best[wave] = best, lds.low[wave] = low;
+  nan = __syncthreads_or(nan);
+  for (int w = 0; w < kWaves; ++w) best = min(best, lds.best[w]);
+  low = -largest_of_waves(lds.low);
+  return best;
+}
 
-  bool nan;
-  const Steps steps = look(lds, row, row.scale.factor);
-  row.scale.top = count_steps(lds, row, steps, 0, a.columns, nan);
-  if (nan) return answer(-1, NAN, 0);
-  if (row.scale.top == -INFINITY) return answer(-1, 0.f, 0);
-  Plan plan = plan_of(lds, row.scale, steps, ask);
-  if (!plan.slow) {
-    const Runs& runs = plan.runs;
-    if (!plan.weighed) gather_runs<0>(lds, row, steps, runs, 0, a.columns);
-    else if (runs.n == 1) gather_runs<1>(lds, row, steps, runs, 0, a.columns);
-    else if (runs.n == 2) gather_runs<2>(lds, row, steps, runs, 0, a.columns);
-    else gather_runs<4>(lds, row, steps, runs, 0, a.columns);
-#pragma unroll
-    for (int i = 0; i < Runs::kMost; ++i) {
-      Run& run = plan.runs.run[i];
-      run.mass_before = plan.weighed ? (double)lds.weight[i] * 0x1p-40 : 0.0;
-      if (i < runs.n) run.span(row.code(run.b0 ? steps.score(run.b0 - 1) : row.scale.top, 0), row.code(steps.score(run.b1), row.columns - 1));
-    }
-    row.sort(lds, runs);
-    const Found f = row.solve(lds, ask, plan.runs, plan.all, plan.weighed ? (double)lds.weight[kMostRuns] * 0x1p-40 : lds.upto[plan.runs.tokens - 1]);
-    if (f.sure && lds.listed == runs.tokens) return give(f);
+// The tokens of the plan are in the list, and the weights before its runs are known: the answer, if it is sure.
+// SPANNED: its run's codes are too.
+template <bool SPANNED, typename T> __device__ __forceinline__ bool find(const Args& a, int64_t r, const Row<T>& row, Waves& waves, Lists& lds) {
+  Plan& plan = waves.head.plan;
+  if (lds.listed != plan.tokens) return false;
+  const Steps steps = waves.head.steps;
+  const int tid = threadIdx.x;
+  if (!SPANNED && tid < kMostRuns) {
+    Run run = plan.run[tid];
+    run.mass_before = plan.weighed ? (double)lds.weight[tid] * 0x1p-40 : 0.0;
+    if (tid < plan.n) run.span(row.code(run.b0 ? steps.score(run.b0 - 1) : row.scale.top, 0), row.code(steps.score(min(run.b1, kSteps - 2)), row.columns - 1));
+    plan.run[tid] = run;
   }
+  __syncthreads();
+  row.sort(waves, lds, plan);
+  if (tid < 64) {
+    const Found f = row.solve(lds, waves.head.ask, plan, plan.all, plan.weighed ? (double)lds.weight[kMostRuns] * 0x1p-40 : lds.upto[plan.tokens - 1]);
+    if (f.sure) answer(a, r, row.column(f.code), (float)f.share, f.kept);
+    if (tid == 0) waves.sure = f.sure;
+  }
+  __syncthreads();
+  return waves.sure;
+}
 
-  // ---- the slow way
-  Sums s{{0, 0}, 0, {0.0, 0.0}, 0.0};
-  for (int first = 0; first < a.columns; first += kChunk) {
+// A plan of one run that has all tokens that matter, `n` of them.
+__device__ __forceinline__ void plan_all(Waves& waves, uint32_t n, int last) {
+  if (threadIdx.x) return;
+  Plan& plan = waves.head.plan;
+  plan.run[0] = {0, last, 0, n, 0, 0, 0, 0.0};
+  plan.n = 1, plan.near = waves.head.ask.far < INFINITY ? 0 : -1, plan.tokens = plan.all = n, plan.weighed = plan.slow = 0;
+}
+
+template <typename T> __device__ __forceinline__ void find_slowly(const Args& a, int64_t r, const Row<T>& row, Waves& waves, Lists& lds) {
+  const int tid = threadIdx.x;
+  Sums<double> s{{0, 0}, 0, {0.0, 0.0}, 0.0};
+  for (int at = 0; at < a.columns; at += kChunk) {
     __syncthreads();
     lds.sum[2 * tid] = lds.sum[2 * tid + 1] = 0;
     __syncthreads();
-    for_each(row.row, first, min(kChunk, a.columns - first), [&](float x, int) {
+    for_each(row.row, at, min(kChunk, a.columns - at), [&](float x, int) {
       if (x == -INFINITY) return;
       const double d = row.scale.distance(x);
       const int bin = bin_of(d);
@@ -946,14 +1068,166 @@ template <typename T> __global__ void __launch_bounds__(kThreads) sample_kernel(
 #pragma unroll
     for (int j = 0; j < 2; ++j) s.c[j] += count_in(lds.sum[2 * tid + j]), s.m[j] += mass_in(lds.sum[2 * tid + j], 2 * tid + j);
   }
-  s.scan(lds, 0, 0.0);
+  s.scan(waves, 0, 0.0);
 #pragma unroll
   for (int j = 0; j < 2; ++j) lds.count[2 * tid + j] = s.c[j], lds.mass[2 * tid + j] = s.m[j];
   __syncthreads();
-  give(row.solve_slowly(lds, ask));
+  const Found f = row.solve_slowly(waves, lds, waves.head.ask);
+  answer(a, r, row.column(f.code), (float)f.share, f.kept);
 }
 
-constexpr int64_t kWorkspace = 256;
+// ---- kernels ----------------------------------------------------------------------------------------------
+// What a row has in the workspace, written anew by each call.
+struct State {
+  Head head;
+  u64 weight[kMostRuns + 1];
+  uint32_t listed, arrived;
+  u64 list[kList];
+};
+constexpr int64_t kStateBytes = (sizeof(State) + 255) / 256 * 256;
+constexpr int kHeadWords = sizeof(Head) / 4;
+static_assert(sizeof(Head) % 4 == 0 && kHeadWords <= kThreads);
+
+template <typename T> __device__ __forceinline__ T read_through(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename T> __device__ __forceinline__ void write_through(T* p, T x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename T> __device__ __forceinline__ T add_through(T* p, T x) { return __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Whether this workgroup is the last of a row's.  What the others have written past the caches is there then: every wavefront waits until
+// its writes are done, then the workgroup counts itself.
+__device__ __forceinline__ bool all_arrived(Waves& waves, uint32_t* counter, uint32_t workgroups) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) waves.arrived = add_through(counter, 1u);
+  __syncthreads();
+  return waves.arrived == workgroups - 1;
+}
+
+// Rows that fit in the list.
+template <typename T> __global__ void __launch_bounds__(kThreads) few_kernel(Args a) {
+  __shared__ Waves waves;
+  __shared__ Lists lds;
+  const int64_t r = blockIdx.x;
+  const float temperature = parameter(a.temperature, r, 1.f);
+  Row<T> row{static_cast<const T*>(a.logits) + r * a.stride, a.columns, a.log2_columns, {0.f, 0.0}};
+  if (threadIdx.x < 64) waves.head.ask = ask_of(a, r, temperature);  // (all lanes write the same)
+  bool nan;
+  float low;
+  const u64 best = best_of(waves, row, low, nan);
+  if (is_answered(a, r, row, best, nan, !(temperature > 0.f))) return;
+  row.scale = {row.score(best), waves.head.ask.factor};
+  const uint32_t n = row.gather(lds, [&](float, int) { return true; });
+  plan_all(waves, n, kSteps);
+  if (threadIdx.x == 0) waves.head.plan.run[0].span(best, row.code(low, a.columns - 1));
+  __syncthreads();
+  find<true>(a, r, row, waves, lds);
+}
+
+// The first pass over a longer row; SECOND: and all the rest.
+template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) row_kernel(Args a, int64_t row0, State* states, int64_t state_bytes) {
+  __shared__ Waves waves;
+  __shared__ Lists lists;
+  __shared__ Counts counts;
+  const int tid = threadIdx.x;
+  const int64_t r = row0 + blockIdx.x;
+  State* const state = reinterpret_cast<State*>(reinterpret_cast<char*>(states) + blockIdx.x * state_bytes);
+  const float temperature = parameter(a.temperature, r, 1.f);
+  Row<T> row{static_cast<const T*>(a.logits) + r * a.stride, a.columns, a.log2_columns, {0.f, 0.0}};
+  bool nan;
+  if (!SECOND && tid == 0) state->head.answered = 1;
+  if (!(temperature > 0.f)) {
+    float low;
+    const u64 best = best_of(waves, row, low, nan);
+    is_answered(a, r, row, best, nan, true);
+    return;
+  }
+  look(a, r, row.row, temperature, waves, counts);
+  __syncthreads();
+  const Steps steps = waves.head.steps;
+  const float bound = counts.bound;
+  row.scale.factor = waves.head.ask.factor;
+  if (bound == bound) {
+    const float high = gather_above(waves, lists, row, steps, bound, nan);
+    if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
+    const uint32_t n = lists.listed, top_k = waves.head.ask.top_k;
+    if (n && n <= kList && (n >= top_k || bound == INFINITY)) {
+      row.scale.top = high;
+      plan_all(waves, n, bound < kSteps - 4 ? (int)bound : kSteps - 2);
+      __syncthreads();
+      if (find<false>(a, r, row, waves, lists)) return;
+    }
+    __syncthreads();
+  }
+  const float high = count_steps(waves, counts, row, steps, nan);
+  if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
+  row.scale.top = high;
+  plan_row(waves, counts, row.scale);
+  if constexpr (SECOND) {
+    if (!waves.head.plan.slow) {
+      gather_plan(waves.head.plan, lists, row, steps, 0, a.columns);
+      if (find<false>(a, r, row, waves, lists)) return;
+    }
+    find_slowly(a, r, row, waves, lists);
+  } else {
+    if (tid == 0) waves.head.answered = 0, waves.head.top = high, state->listed = state->arrived = 0;
+    if (tid <= kMostRuns) state->weight[tid] = 0;
+    __syncthreads();
+    if (tid < kHeadWords) reinterpret_cast<uint32_t*>(&state->head)[tid] = reinterpret_cast<const uint32_t*>(&waves.head)[tid];
+  }
+}
+
+// The scores of a row's piece.
+__device__ __forceinline__ void piece_of(int columns, int pieces, int piece, int& first, int& count) {
+  const int each = ((columns + pieces - 1) / pieces + 15) / 16 * 16;
+  first = min(each * piece, columns), count = min(each, columns - first);
+}
+
+// The second pass over a row, by several workgroups; the last of them does the rest.
+template <typename T> __global__ void __launch_bounds__(kThreads) gather_kernel(Args a, int64_t row0, State* states, int64_t state_bytes, int pieces) {
+  __shared__ Waves waves;
+  __shared__ Lists lds;
+  const int tid = threadIdx.x, slot = blockIdx.x / pieces, piece = blockIdx.x % pieces;
+  const int64_t r = row0 + slot;
+  State* const state = reinterpret_cast<State*>(reinterpret_cast<char*>(states) + slot * state_bytes);
+  if (state->head.answered) return;
+  if (tid < kHeadWords) reinterpret_cast<uint32_t*>(&waves.head)[tid] = reinterpret_cast<const uint32_t*>(&state->head)[tid];
+  __syncthreads();
+  const Row<T> row{static_cast<const T*>(a.logits) + r * a.stride, a.columns, a.log2_columns, {waves.head.top, waves.head.ask.factor}};
+  if (waves.head.plan.slow) {
+    if (piece) return;
+  } else {
+    int first, count;
+    piece_of(a.columns, pieces, piece, first, count);
+    gather_plan(waves.head.plan, lds, row, waves.head.steps, first, count);
+    const uint32_t listed = lds.listed;
+    if (tid == 0) lds.first = listed ? add_through(&state->listed, listed) : 0;
+    if (tid <= kMostRuns && lds.weight[tid]) add_through(&state->weight[tid], lds.weight[tid]);
+    __syncthreads();
+    for (uint32_t i = tid; i < min(listed, (uint32_t)kList) && lds.first + i < kList; i += kThreads) write_through(&state->list[lds.first + i], lds.list[i]);
+    if (!all_arrived(waves, &state->arrived, pieces)) return;
+    for (uint32_t i = tid; i < waves.head.plan.tokens; i += kThreads) lds.list[i] = read_through(&state->list[i]);
+    if (tid == 0) lds.listed = read_through(&state->listed);
+    if (tid <= kMostRuns) lds.weight[tid] = read_through(&state->weight[tid]);
+    __syncthreads();
+    if (find<false>(a, r, row, waves, lds)) return;
+  }
+  find_slowly(a, r, row, waves, lds);
+}
+
+template <typename T> void launch(const Args& a, int64_t rows, State* states, hipStream_t stream) {
+  if (a.columns <= kList) {
+    hipLaunchKernelGGL(few_kernel<T>, dim3((unsigned)rows), dim3(kThreads), 0, stream, a);
+    return;
+  }
+  for (int64_t row0 = 0; row0 < rows; row0 += kMostRows) {
+    const int n = (int)std::min<int64_t>(rows - row0, kMostRows), pieces = std::min(std::max(kGroups / n, kLeastGathering), a.columns / kLeastPiece);
+    if (pieces < 2) {
+      hipLaunchKernelGGL((row_kernel<T, true>), dim3((unsigned)n), dim3(kThreads), 0, stream, a, row0, states, kStateBytes);
+    } else {
+      hipLaunchKernelGGL((row_kernel<T, false>), dim3((unsigned)n), dim3(kThreads), 0, stream, a, row0, states, kStateBytes);
+      hipLaunchKernelGGL(gather_kernel<T>, dim3((unsigned)(n * pieces)), dim3(kThreads), 0, stream, a, row0, states, kStateBytes, pieces);
+    }
+  }
+}
 
 }  // namespace
 
@@ -962,7 +1236,7 @@ extern "C" {
 int64_t rsr_sample_workspace(int64_t rows, int64_t columns) {
   if (rows < 0 || rows > 1 << 24) return set_error(RSR_ERR_INVALID_ARGUMENT, "rows must be in 0..2^24");
   if (columns < 1 || columns > 1 << 22) return set_error(RSR_ERR_INVALID_ARGUMENT, "columns must be in 1..2^22");
-  return kWorkspace;
+  return std::max<int64_t>(1, std::min<int64_t>(rows, kMostRows)) * kStateBytes;
 }
 
 int rsr_sample(const void* logits, int64_t rows, int64_t columns, int64_t stride, int dtype, const float* temperature, const int32_t* top_k,
@@ -979,8 +1253,7 @@ int rsr_sample(const void* logits, int64_t rows, int64_t columns, int64_t stride
     return set_error(RSR_ERR_INVALID_ARGUMENT, "the workspace is missing, too small or not 256-byte aligned");
   Args a{logits, temperature, top_p, min_p, uniform, top_k, token, probability, kept, stride, (int32_t)columns, 1};
   while ((int64_t)1 << a.log2_columns < columns) ++a.log2_columns;
-  auto kern = dtype == RSR_F32 ? sample_kernel<float> : dtype == RSR_F16 ? sample_kernel<_Float16> : sample_kernel<__bf16>;
-  hipLaunchKernelGGL(kern, dim3((unsigned)rows), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+  (dtype == RSR_F32 ? launch<float> : dtype == RSR_F16 ? launch<_Float16> : launch<__bf16>)(a, rows, static_cast<State*>(workspace), static_cast<hipStream_t>(stream));
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(RSR_ERR_HIP, std::string("rsr_sample: ") + hipGetErrorString(e));
   return RSR_OK;
