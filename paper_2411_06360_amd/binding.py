@@ -461,12 +461,20 @@ class RsrRotary(ctypes.Structure):
     ]
 
 
+_REAL: dict = {"torch.float32": set(), "torch.float64": set()}  # names, and the types themselves once they were seen
+
+
 def _numbers(x, kind: str, count: int) -> Optional[int]:
     """Address of a contiguous tensor of floating-point numbers of that type, with at least `count` elements (None stays None)."""
     if x is None:
         return None
-    if str(x.dtype) != kind or x.numel() < count or not x.is_contiguous():
-        raise ValueError(f"a contiguous tensor of {count} numbers of {kind} is wanted")
+    dtype, known = x.dtype, _REAL[kind]
+    if dtype not in known:
+        if str(dtype) != kind:
+            raise ValueError(f"a contiguous tensor of {count} numbers of {kind} is wanted, not {dtype}")
+        known.add(dtype)
+    if x.numel() < count or not x.is_contiguous():
+        raise ValueError(f"a contiguous tensor of {count} numbers is wanted")
     return x.data_ptr()
 
 

@@ -38,7 +38,6 @@ constexpr int kPeaks = 2 * kThreads;  // scores above the steps
 constexpr int kBounded = 512;         // top_k up to here is looked up in one pass
 constexpr int kGroups = 256;          // workgroups of a launch: one for each CU
 constexpr int kLeastPiece = 8192;     // scores of a workgroup, where several have a row
-constexpr int kLeastGathering = 2;    // workgroups of a row in the second pass
 constexpr int kMostRows = 1024;       // of a launch
 constexpr int kPrefix = 1024;        // tokens that are rather gathered from the first one on than counted
 
@@ -175,12 +174,12 @@ template <typename T> struct Key {
 };
 
 // f(scores, column of the first) for 16 bytes of `count` scores of a row from column `first` on at a time, by all threads of the
-// workgroup, each in ascending order, wherever the row begins; sixteen scores are on their way while sixteen are looked at.  What sticks out at
+// workgroup, each in ascending order, wherever the row begins; SCORES of a thread are on their way while as many are looked at.  What sticks out at
 // the ends is read by itself and comes with minus infinity behind it.
-template <typename T, typename F> __device__ __forceinline__ void for_pieces(const T* row, int first, int count, F f) {
+template <int SCORES = 16, typename T, typename F> __device__ __forceinline__ void for_pieces(const T* row, int first, int count, F f) {
   typedef const __attribute__((address_space(1))) T* Scores;
   typedef const __attribute__((address_space(1))) u4* Pieces;
-  constexpr int kWide = 16 / sizeof(T), kAtOnce = sizeof(T) == 4 ? 4 : 2;
+  constexpr int kWide = 16 / sizeof(T), kAtOnce = SCORES / kWide;
   const Scores from = (Scores)(row + first);
   const int head = min(count, (int)((16 - (reinterpret_cast<uintptr_t>(row + first) & 15)) & 15) / (int)sizeof(T));
   const int pieces = (count - head) / kWide, tail = head + pieces * kWide, tid = threadIdx.x;
@@ -617,7 +616,7 @@ __device__ __forceinline__ Ask ask_of(const Args& a, int64_t r, float temperatur
           top_k > 0 && top_k < a.columns ? (uint32_t)top_k : 0u};
 }
 
-// Steps from the fourth highest or so of some thousand scores of a row down to the lowest, or to the last that has any weight, and a bound
+// Steps from one of the highest of some thousand scores of a row down to the lowest, or to the last that has any weight, and a bound
 // above which lie the tokens that can be kept, if they are few (else NaN): where top_k is small, the score of which so many are above
 // among the highest of four to eight that enough of the row's are, and some hundred more; with min_p alone, the least that it may come to.
 template <typename T> __device__ __forceinline__ void look(const Args& a, int64_t r, const T* row, float temperature, Waves& waves, Counts& lds) {
@@ -645,8 +644,8 @@ template <typename T> __device__ __forceinline__ void look(const Args& a, int64_
     low = -largest_of_waves(waves.low);
     const float mine = waves.high[lane & (kWaves - 1)];
     high = of_lane(largest_of_16(mine), 15);
-    // above the first step are a hundred scores or so: those above the `rank`-th of the wavefronts' highest
-    const int rank = max(1, min(kWaves / 4, (kWaves / 4 << 17) / a.columns));
+    // above the first step are some hundred scores: those above the `rank`-th of the wavefronts' highest
+    const int rank = max(1, min(kWaves / 2, (kWaves / 2 << 17) / a.columns));
     int higher = 0;
     for (int w = 0; w < kWaves; ++w) {
       const float other = of_lane(mine, w);
@@ -691,7 +690,7 @@ template <typename T> __device__ __forceinline__ float gather_above(Waves& waves
   if (tid == 0) lds.listed = 0;
   __syncthreads();
   float high = -INFINITY;
-  for_pieces(row.row, 0, row.columns, [&](const float (&x)[kWide], int column) {
+  for_pieces<32>(row.row, 0, row.columns, [&](const float (&x)[kWide], int column) {
     bool some = false;
 #pragma unroll
     for (int j = 0; j < kWide; ++j) {
@@ -750,7 +749,7 @@ template <typename T> __device__ __forceinline__ float count_steps(Waves& waves,
 // In which steps the places may be, and so which tokens are gathered.  The scores above the steps are weighed one by one, a step as its
 // count times the weight in its middle.  Where a step's scores lie in it is not known: it is off by its weight times its width (in
 // ln 2 octaves) over the root of 12, as if they all lay at one place of which any is as likely, and the sums of all are off by the root of the
-// squares of that; six times as much is allowed for.  (Whether that was enough is seen in the end.)
+// squares of that; four and a half times as much is allowed for.  (Whether that was enough is seen in the end.)
 __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale& scale) {
   constexpr int kEach = kSteps / kThreads;
   constexpr float kRounded = 1e-5f;  // of a sum: what weights are rounded by here, and more
@@ -824,7 +823,7 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
   __syncthreads();
   const uint32_t all = lds.all_count;
   const float total = lds.all_mass;
-  const float off = 1.2005660f * octaves * sqrtf(of_lane(sum_of_16(waves.high[lane & 15]), 15)) + kRounded * total;  // (6 ln 2 / sqrt 12)
+  const float off = 0.9004245f * octaves * sqrtf(of_lane(sum_of_16(waves.high[lane & 15]), 15)) + kRounded * total;  // (4.5 ln 2 / sqrt 12)
   const bool k = ask.top_k && ask.top_k < all, p = ask.top_p < 1.0;
   mark(0, About::tokens(all));
   if (k) mark(1, About::tokens(ask.top_k));
@@ -1143,12 +1142,18 @@ template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) r
   look(a, r, row.row, temperature, waves, counts);
   __syncthreads();
   const Steps steps = waves.head.steps;
-  const float bound = counts.bound;
+  float bound = counts.bound;
   row.scale.factor = waves.head.ask.factor;
   if (bound == bound) {
-    const float high = gather_above(waves, lists, row, steps, bound, nan);
+    float high = gather_above(waves, lists, row, steps, bound, nan);
     if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
-    const uint32_t n = lists.listed, top_k = waves.head.ask.top_k;
+    const uint32_t top_k = waves.head.ask.top_k;
+    if (lists.listed > kList && !(top_k && top_k <= kBounded)) {  // (min_p alone: with the highest score known the bound is what it has to be)
+      bound = fmaxf(steps.down((float)fmax((double)high - waves.head.ask.far / row.scale.factor, -(double)FLT_MAX)), 0.f) + 1.f;
+      __syncthreads();
+      high = gather_above(waves, lists, row, steps, bound, nan);
+    }
+    const uint32_t n = lists.listed;
     if (n && n <= kList && (n >= top_k || bound == INFINITY)) {
       row.scale.top = high;
       plan_all(waves, n, bound < kSteps - 4 ? (int)bound : kSteps - 2);
@@ -1219,7 +1224,7 @@ template <typename T> void launch(const Args& a, int64_t rows, State* states, hi
     return;
   }
   for (int64_t row0 = 0; row0 < rows; row0 += kMostRows) {
-    const int n = (int)std::min<int64_t>(rows - row0, kMostRows), pieces = std::min(std::max(kGroups / n, kLeastGathering), a.columns / kLeastPiece);
+    const int n = (int)std::min<int64_t>(rows - row0, kMostRows), pieces = std::min(kGroups / n, a.columns / kLeastPiece);
     if (pieces < 2) {
       hipLaunchKernelGGL((row_kernel<T, true>), dim3((unsigned)n), dim3(kThreads), 0, stream, a, row0, states, kStateBytes);
     } else {
