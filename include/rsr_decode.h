@@ -49,8 +49,8 @@ typedef struct rsr_rotary_t {
  * rsr_head_rotate - for every head x of every row of q and k
  *   y = x * weight / sqrt(mean(x^2) + eps)     (or y = x)
  *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),   t = position[row] * frequency[j], for pair j = (a, b)
- * with one rounding, to the type of the result.  The mean is taken in 64 bits, the angle's whole turns are taken off in 64
- * bits (and what those lose): a far position is rotated as exactly as a near one.  A value that is not finite touches its own
+ * in 32 bits, with one rounding at the end to the type of the result.  (Where squares leave the range of float their mean is taken in 64
+ * bits.)  The angle's whole turns are taken off in 64 bits, with what those lose: a far position is rotated as exactly as a near one.  A value that is not finite touches its own
  * head alone (its pair, without a norm).  A head of zeros with eps 0 is not finite.
  *
  *   q, k         DEVICE, row t at q + t * q_stride elements: [heads][head_dim], k: [kv_heads][head_dim]

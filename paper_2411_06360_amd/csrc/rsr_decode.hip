@@ -25,7 +25,6 @@ int launched(const char* what) {
 // (or of the rest's), so that with either pairing both of a pair are its own.  As many lanes as the next power of two above
 // head_dim / 8 make a head, and a wavefront turns from head to head of one token, whose angles it works out once.
 constexpr int kRotateThreads = 256;
-constexpr int kHeadsAtOnce = 4;  // of a lane
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 
@@ -40,23 +39,19 @@ struct RotateArgs {
   int32_t log2_lanes;  // lanes of a head
   int32_t share;       // wavefronts of a token
   float eps;
+  float share_of_one;  // 1 / dim
   bool norm, pairs;
 };
 
-template <typename T> __device__ inline f4 load4(const void* p, int64_t at) {
-  if constexpr (sizeof(T) == 4) {
-    return *reinterpret_cast<const f4*>(static_cast<const float*>(p) + at);
-  } else {
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    const t4 x = *reinterpret_cast<const t4*>(static_cast<const T*>(p) + at);
-    return f4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
-  }
-}
+template <typename T> struct Four {
+  typedef T type __attribute__((ext_vector_type(4)));
+  static __device__ inline type load(const T* p) { return *reinterpret_cast<const type*>(p); }
+  static __device__ inline f4 wide(type x) { return f4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]}; }
+  static __device__ inline void store(T* p, f4 x) { *reinterpret_cast<type*>(p) = type{(T)x[0], (T)x[1], (T)x[2], (T)x[3]}; }
+};
 
-template <typename T> __device__ inline void store4(void* p, int64_t at, f4 x) {
-  typedef T t4 __attribute__((ext_vector_type(4)));
-  *reinterpret_cast<t4*>(static_cast<T*>(p) + at) = t4{(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
-}
+// (the norm's weights may lie anywhere)
+__device__ inline f4 load4_anywhere(const float* p) { return f4{p[0], p[1], p[2], p[3]}; }
 
 // position * frequency in whole turns, less the whole ones: the product in two doubles, and the quotient by 2 pi as a product with two.
 __device__ inline float turn_of(int position, double frequency) {
@@ -66,14 +61,43 @@ __device__ inline float turn_of(int position, double frequency) {
   return (float)((turns - rint(turns)) + rest);
 }
 
+// The sum over the lanes of a head, in each of them.
+template <int CTRL> __device__ inline float and_moved(float x) {
+  return x + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+__device__ inline float over_head(float x, int log2_lanes) {
+  if (log2_lanes >= 1) x = and_moved<0xb1>(x);   // the neighbour
+  if (log2_lanes >= 2) x = and_moved<0x4e>(x);   // the other two of four
+  if (log2_lanes >= 3) x = and_moved<0x141>(x);  // of eight, backwards
+  if (log2_lanes >= 4) x = and_moved<0x140>(x);  // of sixteen, backwards
+  return log2_lanes >= 5 ? x + __shfl_xor(x, 16) : x;
+}
+
 template <typename IN, typename OUT> __global__ void __launch_bounds__(kRotateThreads) rotate_kernel(RotateArgs a) {
-  const int lane = threadIdx.x & 63, lanes = 1 << a.log2_lanes, in_head = lane & (lanes - 1);
-  const int64_t wave = (int64_t)blockIdx.x * (kRotateThreads / 64) + (threadIdx.x >> 6), token = wave / a.share;
+  const int lane = threadIdx.x & 63, lanes = 1 << a.log2_lanes, in_head = lane & (lanes - 1), part = lane >> a.log2_lanes;
+  const int64_t wave = (int64_t)blockIdx.x * (kRotateThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), token = wave / a.share;
   if (token >= a.tokens) return;
-  const int all = a.heads + a.kv_heads, each = 64 >> a.log2_lanes, step = a.share * each * kHeadsAtOnce;
+  const int all = a.heads + a.kv_heads, each = 64 >> a.log2_lanes, step = a.share * each;
   const bool there = in_head < a.dim / 8, turns = in_head < a.rotated / 8;
   const int rest = in_head - a.rotated / 8;
   const int lo = there ? turns ? 4 * in_head : a.rotated + 4 * rest : 0, hi = there ? turns ? a.rotated / 2 + lo : (a.dim - a.rotated) / 2 + lo : 0;
+  const IN* const q = static_cast<const IN*>(a.q) + token * a.q_stride;
+  const IN* const k = static_cast<const IN*>(a.k) + token * a.k_stride;
+  OUT* const q_out = static_cast<OUT*>(a.q_out) + token * a.q_out_stride;
+  OUT* const k_out = static_cast<OUT*>(a.k_out) + token * a.k_out_stride;
+  const int first = (int)(wave - token * a.share) * each;
+  // The heads that are next are on their way while some are worked on, the first ones while the angles are.
+  typedef typename Four<IN>::type Raw;
+  Raw next[2];
+  auto load = [&](int head0) {
+    const int head = min(head0 + part, all - 1);  // (the last one again instead of none)
+    const IN* const from = head < a.heads ? q + head * a.dim : k + (head - a.heads) * a.dim;
+    next[0] = Four<IN>::load(from + lo), next[1] = Four<IN>::load(from + hi);
+  };
+  load(first);
+  f4 q_weight[2]{{1, 1, 1, 1}, {1, 1, 1, 1}}, k_weight[2]{{1, 1, 1, 1}, {1, 1, 1, 1}};
+  if (a.norm && a.q_weight) q_weight[0] = load4_anywhere(a.q_weight + lo), q_weight[1] = load4_anywhere(a.q_weight + hi);
+  if (a.norm && a.k_weight) k_weight[0] = load4_anywhere(a.k_weight + lo), k_weight[1] = load4_anywhere(a.k_weight + hi);
   f4 sin{0, 0, 0, 0}, cos{1, 1, 1, 1};
   if (there && turns) {
     const int position = a.position[token];
@@ -85,50 +109,50 @@ template <typename IN, typename OUT> __global__ void __launch_bounds__(kRotateTh
       sin[j] = s, cos[j] = c;
     }
   }
-  for (int head0 = (int)(wave - token * a.share) * each * kHeadsAtOnce + (lane >> a.log2_lanes); head0 - (lane >> a.log2_lanes) < all; head0 += step) {
-    f4 x[kHeadsAtOnce][2];
+  for (int head0 = first; head0 < all; head0 += step) {
+    f4 x[2] = {Four<IN>::wide(next[0]), Four<IN>::wide(next[1])};
+    if (head0 + step < all) load(head0 + step);  // (in place too: another turn's heads are others)
+    const int head = head0 + part;
+    const bool is_there = there && head < all;
+    if (a.norm) {
+      if (!there) x[0] = x[1] = f4{0, 0, 0, 0};
+      f4 s = x[0] * x[0];
+      s = x[1] * x[1] + s;
+      const float mean = over_head((s[0] + s[1]) + (s[2] + s[3]), a.log2_lanes) * a.share_of_one;
+      const float m = mean + a.eps, near = __builtin_amdgcn_rsqf(m), by = fmaf(0.5f * near, fmaf(-m * near, near, 1.f), near);
+      const bool odd = is_there && !(mean < 1e30f && m > 1e-30f);
+      f4 w[2];
 #pragma unroll
-    for (int i = 0; i < kHeadsAtOnce; ++i) {
-      const int head = head0 + i * each;
-      x[i][0] = x[i][1] = f4{0, 0, 0, 0};
-      if (!there || head >= all) continue;
-      const void* const from = head < a.heads ? a.q : a.k;
-      const int64_t at = head < a.heads ? token * a.q_stride + (int64_t)head * a.dim : token * a.k_stride + (int64_t)(head - a.heads) * a.dim;
-      x[i][0] = load4<IN>(from, at + lo), x[i][1] = load4<IN>(from, at + hi);
-    }
-#pragma unroll
-    for (int i = 0; i < kHeadsAtOnce; ++i) {
-      const int head = head0 + i * each;
-      if (a.norm) {
+      for (int j = 0; j < 2; ++j) w[j] = head < a.heads ? q_weight[j] : k_weight[j];
+      if (!__ballot(odd)) {
+        x[0] = x[0] * by * w[0], x[1] = x[1] * by * w[1];
+      } else {
+        // (seldom: squares beyond the range of float, or what does not count in it; of these heads alone)
         double sum = 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) sum = fma((double)x[i][h][j], (double)x[i][h][j], sum);
+          for (int e = 0; e < 4; ++e) sum = fma((double)x[j][e], (double)x[j][e], sum);
         for (int d = lanes / 2; d; d >>= 1) sum += __shfl_xor(sum, d);
-        const double by = 1.0 / sqrt(sum / a.dim + (double)a.eps);
-        const float* const weight = head < a.heads ? a.q_weight : a.k_weight;
+        const double exact = 1.0 / sqrt(sum / a.dim + (double)a.eps);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f4 w = weight && there ? f4{weight[(h ? hi : lo)], weight[(h ? hi : lo) + 1], weight[(h ? hi : lo) + 2], weight[(h ? hi : lo) + 3]} : f4{1, 1, 1, 1};
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[i][h][j] = (float)((double)x[i][h][j] * by) * w[j];
-        }
+          for (int e = 0; e < 4; ++e) x[j][e] = (odd ? (float)((double)x[j][e] * exact) : x[j][e] * by) * w[j][e];
       }
-      if (!there || head >= all) continue;
-      if (turns) {
-        const f4 u = x[i][0], v = x[i][1];
-        if (!a.pairs) {
-          x[i][0] = u * cos - v * sin, x[i][1] = u * sin + v * cos;
-        } else {
-          x[i][0] = f4{u[0] * cos[0] - u[1] * sin[0], u[0] * sin[0] + u[1] * cos[0], u[2] * cos[1] - u[3] * sin[1], u[2] * sin[1] + u[3] * cos[1]};
-          x[i][1] = f4{v[0] * cos[2] - v[1] * sin[2], v[0] * sin[2] + v[1] * cos[2], v[2] * cos[3] - v[3] * sin[3], v[2] * sin[3] + v[3] * cos[3]};
-        }
-      }
-      void* const to = head < a.heads ? a.q_out : a.k_out;
-      const int64_t at = head < a.heads ? token * a.q_out_stride + (int64_t)head * a.dim : token * a.k_out_stride + (int64_t)(head - a.heads) * a.dim;
-      store4<OUT>(to, at + lo, x[i][0]), store4<OUT>(to, at + hi, x[i][1]);
     }
+    if (!is_there) continue;
+    if (turns) {
+      const f4 u = x[0], v = x[1];
+      if (!a.pairs) {
+        x[0] = u * cos - v * sin, x[1] = u * sin + v * cos;
+      } else {
+        x[0] = f4{u[0] * cos[0] - u[1] * sin[0], u[0] * sin[0] + u[1] * cos[0], u[2] * cos[1] - u[3] * sin[1], u[2] * sin[1] + u[3] * cos[1]};
+        x[1] = f4{v[0] * cos[2] - v[1] * sin[2], v[0] * sin[2] + v[1] * cos[2], v[2] * cos[3] - v[3] * sin[3], v[2] * sin[3] + v[3] * cos[3]};
+      }
+    }
+    OUT* const to = head < a.heads ? q_out + head * a.dim : k_out + (head - a.heads) * a.dim;
+    Four<OUT>::store(to + lo, x[0]), Four<OUT>::store(to + hi, x[1]);
   }
 }
 
@@ -183,34 +207,65 @@ __global__ void __launch_bounds__(kKeepThreads) count_kernel(KeepArgs a) {
   if (lane == 0) a.add[r] = __popcll(p.on);
 }
 
-// The paths, one behind the other: a workgroup adds up what all requests before its own add.
-__global__ void __launch_bounds__(kKeepThreads) paths_kernel(KeepArgs a, int each) {
+__device__ inline void write_path(const KeepArgs& a, int r, int lane, const Path& p, int64_t at) {
+  if (lane == 0) a.first[r] = (int32_t)min(at, (int64_t)a.tokens);
+  at += __popcll(p.on & ((1ull << lane) - 1));
+  if (p.on >> lane & 1 && at < a.tokens) a.rows[at] = (int32_t)(p.first + lane), a.found[at] = p.chosen;
+}
+
+// The paths, one behind the other, with what is behind the last.  ALONE: of at most kAlone requests, which one workgroup walks, some for
+// each wavefront.  Else `add` is known, a workgroup has `each` requests, adds up what all before them add, and walks its own again (a
+// place to keep the paths in between would be as long as all trees).
+constexpr int kRounds = 4, kAlone = kRounds * kKeepWaves;
+
+template <bool ALONE> __global__ void __launch_bounds__(kKeepThreads) paths_kernel(KeepArgs a, int each) {
   __shared__ int64_t before_sum[kKeepWaves], all_sum[kKeepWaves];
+  __shared__ int32_t adds[kAlone];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int r0 = blockIdx.x * each, r1 = min(r0 + each, a.requests);
   int64_t before = 0, all = 0;
-  for (int r = tid; r < a.requests; r += kKeepThreads) {
-    const int add = a.add[r];
-    all += add, before += r < r0 ? add : 0;
-  }
-  for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d), all += __shfl_xor(all, d);
-  if (lane == 0) before_sum[wave] = before, all_sum[wave] = all;
-  __syncthreads();
-  before = all = 0;
-  for (int w = 0; w < kKeepWaves; ++w) before += before_sum[w], all += all_sum[w];
-  for (int r = r0 + wave; r < r1; r += kKeepWaves) {
-    const Path p = path_of(a, r, lane);
-    int64_t at = 0;
-    for (int s = r0 + lane; s < r; s += 64) at += a.add[s];
-    for (int d = 32; d; d >>= 1) at += __shfl_xor(at, d);
-    at += before;
-    if (lane == 0) a.first[r] = (int32_t)min(at, (int64_t)a.tokens);
-    at += __popcll(p.on & ((1ull << lane) - 1));
-    if (p.on >> lane & 1 && at < a.tokens) a.rows[at] = (int32_t)(p.first + lane), a.found[at] = p.chosen;
+  if constexpr (ALONE) {
+    Path p[kRounds];
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      const int r = i * kKeepWaves + wave;
+      if (r >= a.requests) continue;
+      p[i] = path_of(a, r, lane);
+      if (lane == 0) a.add[r] = adds[r] = __popcll(p[i].on);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      const int r = i * kKeepWaves + wave;
+      if (r >= a.requests) continue;
+      int64_t at = lane < r ? adds[lane] : 0;
+      for (int d = 32; d; d >>= 1) at += __shfl_xor(at, d);
+      write_path(a, r, lane, p[i], at);
+    }
+    all = lane < a.requests ? adds[lane] : 0;
+    for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d);
+  } else {
+    const int r0 = blockIdx.x * each, r1 = min(r0 + each, a.requests);
+    for (int r = tid; r < a.requests; r += kKeepThreads) {
+      const int add = a.add[r];
+      all += add, before += r < r0 ? add : 0;
+    }
+    for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d), all += __shfl_xor(all, d);
+    if (lane == 0) before_sum[wave] = before, all_sum[wave] = all;
+    __syncthreads();
+    before = all = 0;
+    for (int w = 0; w < kKeepWaves; ++w) before += before_sum[w], all += all_sum[w];
+    for (int r = r0 + wave; r < r1; r += kKeepWaves) {
+      const Path p = path_of(a, r, lane);
+      int64_t at = 0;
+      for (int s = r0 + lane; s < r; s += 64) at += a.add[s];
+      for (int d = 32; d; d >>= 1) at += __shfl_xor(at, d);
+      write_path(a, r, lane, p, before + at);
+    }
   }
   if (blockIdx.x == 0 && tid == 0) a.first[a.requests] = (int32_t)min(all, (int64_t)a.tokens);
   for (int64_t i = all + (int64_t)blockIdx.x * kKeepThreads + tid; i < a.tokens; i += (int64_t)gridDim.x * kKeepThreads) a.rows[i] = a.found[i] = -1;
 }
+static_assert(kAlone <= 64);
 
 }  // namespace
 
@@ -241,10 +296,10 @@ int rsr_head_rotate(const rsr_rotary_t* rotary, const void* q, int64_t q_stride,
   if (!fault && ((heads && kv_heads && q_out == k_out) || (heads && kv_heads && (q_out == k || k_out == q)))) fault = "an output must not be another input or output";
   if (fault) return set_error(RSR_ERR_INVALID_ARGUMENT, fault);
   RotateArgs a{q, k, q_out, k_out, rotary->frequency, rotary->q_weight, rotary->k_weight, position, q_stride, k_stride, q_out_stride, k_out_stride, tokens,
-               heads, kv_heads, rotary->head_dim, rotary->rotated, 0, 1, rotary->eps, rotary->norm != 0, rotary->pairs != 0};
+               heads, kv_heads, rotary->head_dim, rotary->rotated, 0, 1, rotary->eps, 1.f / (float)rotary->head_dim, rotary->norm != 0, rotary->pairs != 0};
   while (8 << a.log2_lanes < a.dim) ++a.log2_lanes;
   // a wavefront for each token, or as many as its heads keep busy where that leaves the chip idle
-  const int each = (64 >> a.log2_lanes) * kHeadsAtOnce;
+  const int each = 64 >> a.log2_lanes;
   const int64_t most = (heads + kv_heads + each - 1) / each;
   a.share = (int32_t)std::min(most, std::max<int64_t>(1, 4096 / tokens));
   const int64_t groups = (tokens * a.share + kRotateThreads / 64 - 1) / (kRotateThreads / 64);
@@ -267,11 +322,13 @@ int rsr_tree_keep(const int32_t* drafted, const int32_t* chosen, const int32_t* 
       if (outputs[i] && (outputs[i] == inputs[j] || (j < i && outputs[i] == outputs[j]))) return set_error(RSR_ERR_INVALID_ARGUMENT, "an output must not be an input or another output");
   }
   const KeepArgs a{drafted, chosen, parent, start, rows, found, add, first, requests, tokens};
-  if (requests) {
-    hipLaunchKernelGGL(count_kernel, dim3((requests + kKeepWaves - 1) / kKeepWaves), dim3(kKeepThreads), 0, static_cast<hipStream_t>(stream), a);
+  if (requests <= kAlone) {
+    hipLaunchKernelGGL(paths_kernel<true>, dim3(1), dim3(kKeepThreads), 0, static_cast<hipStream_t>(stream), a, 0);
+    return launched("rsr_tree_keep");
   }
   const int each = std::max(kKeepWaves, (requests + 255) / 256);
-  hipLaunchKernelGGL(paths_kernel, dim3(std::max(1, (requests + each - 1) / each)), dim3(kKeepThreads), 0, static_cast<hipStream_t>(stream), a, each);
+  hipLaunchKernelGGL(count_kernel, dim3((requests + kKeepWaves - 1) / kKeepWaves), dim3(kKeepThreads), 0, static_cast<hipStream_t>(stream), a);
+  hipLaunchKernelGGL(paths_kernel<false>, dim3((requests + each - 1) / each), dim3(kKeepThreads), 0, static_cast<hipStream_t>(stream), a, each);
   return launched("rsr_tree_keep");
 }
 

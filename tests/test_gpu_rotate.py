@@ -20,12 +20,13 @@ def frequencies(rotated, base=10000.0):
 
 
 def close(got, x, position, frequency, dim, eps, weight, pairs, out):
-    """Every value by the definition.  A normed value is rounded twice (2^-24 each), its sine and cosine are off by 2 pi times the
-    rounding of the turn (half a turn at most: 2^-26) and by two units in the last place of a value up to 1 (2^-23 together with that: 7
-    times 2^-24 at most), and the two products and their sum are rounded once each: 12 times 2^-24 of |y_a| + |y_b|; then the rounding to
-    the result's type, whose smallest numbers are 2^-24 apart (float16) or less."""
+    """Every value by the definition, in units of 2^-24 of |y_a| + |y_b|.  The sum of a head's squares is a tree of at most nine roundings, all of
+    one sign, its mean and eps three more, of which a root passes on half; the reciprocal root, refined, is off by 1.5: 7.5 together; twice
+    rounded, with the weight: 9.5.  (A head of 64 bits: less.)  Sine and cosine are off by 2 pi times the rounding of the turn (half a turn at most:
+    1.6) and by two units in the last place of a value up to 1 (4): 5.6.  The two products and their sum are rounded once each: 18.1 in all.
+    Then the rounding to the result's type, whose smallest numbers are 2^-24 apart (float16) or less."""
     want, size = oracle.rotate(plain(x), position.cpu().numpy(), None if frequency is None else frequency.cpu().numpy(), dim, eps, plain(weight), pairs)
-    error, bound = np.abs(plain(got) - want), 12 * 2.0**-24 * size + np.abs(want) * ROUND[out] + 2.0**-25
+    error, bound = np.abs(plain(got) - want), 18.1 * 2.0**-24 * size + np.abs(want) * ROUND[out] + 2.0**-25
     assert np.isfinite(plain(got)).all()
     assert (error <= bound).all(), f"off by {float((error / bound).max()):.3g} times the bound"
 
