@@ -39,6 +39,7 @@ constexpr int kBounded = 512;         // top_k up to here is looked up in one pa
 constexpr int kGroups = 256;          // workgroups of a launch: one for each CU
 constexpr int kLeastPiece = 8192;     // scores of a workgroup, where several have a row
 constexpr int kMostRows = 1024;       // of a launch
+constexpr int kLeastCounted = 1 << 14, kFewestCounts = 4, kMostCounts = 8;  // the first pass: scores of a piece, and pieces of a row (or one)
 constexpr int kPrefix = 1024;        // tokens that are rather gathered from the first one on than counted
 
 // What a bin adds up in one word: for each token a one above, and below how much less than the bin's most its weight is, in units of
@@ -684,13 +685,13 @@ template <typename T> __device__ __forceinline__ void look(const Args& a, int64_
 
 // The first pass: the highest score, whether one is NaN, and the tokens above the bound, or else all scores counted in steps and those above
 // the steps in a list.
-template <typename T> __device__ __forceinline__ float gather_above(Waves& waves, Lists& lds, const Row<T>& row, const Steps& steps, float bound, bool& nan) {
+template <typename T> __device__ __forceinline__ float gather_above(Waves& waves, Lists& lds, const Row<T>& row, const Steps& steps, int first, int count, float bound, bool& nan) {
   constexpr int kWide = 16 / sizeof(T);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (tid == 0) lds.listed = 0;
   __syncthreads();
   float high = -INFINITY;
-  for_pieces<32>(row.row, 0, row.columns, [&](const float (&x)[kWide], int column) {
+  for_pieces<32>(row.row, first, count, [&](const float (&x)[kWide], int column) {
     bool some = false;
 #pragma unroll
     for (int j = 0; j < kWide; ++j) {
@@ -712,7 +713,7 @@ template <typename T> __device__ __forceinline__ float gather_above(Waves& waves
   return largest_of_waves(waves.high);
 }
 
-template <typename T> __device__ __forceinline__ float count_steps(Waves& waves, Counts& lds, const Row<T>& row, const Steps& steps, bool& nan) {
+template <typename T> __device__ __forceinline__ float count_steps(Waves& waves, Counts& lds, const Row<T>& row, const Steps& steps, int first, int count, bool& nan) {
   constexpr int kWide = 16 / sizeof(T);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, aside = kSteps + lane;
   u4* const zero = reinterpret_cast<u4*>(lds.steps);
@@ -720,7 +721,7 @@ template <typename T> __device__ __forceinline__ float count_steps(Waves& waves,
   if (tid == 0) lds.listed = 0;
   __syncthreads();
   float high = -INFINITY;
-  for_pieces(row.row, 0, row.columns, [&](const float (&x)[kWide], int) {
+  for_pieces(row.row, first, count, [&](const float (&x)[kWide], int) {
     float least = 0.f;
 #pragma unroll
     for (int j = 0; j < kWide; ++j) {
@@ -764,16 +765,17 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
     __syncthreads();
     return;
   }
-  float peak = 0.f;
+  const Weights weights{scale.top, scale.factor};
+  u64 high = 0;  // (they lie in any order, so their sum is one of whole numbers)
 #pragma unroll
   for (int j = 0; j < 2; ++j)
-    if ((uint32_t)(tid + j * kThreads) < peaks) peak += (float)scale.weight(lds.peaks[tid + j * kThreads]);
-  peak = sum_of_lanes(peak);
-  if (lane == 63) waves.low[wave] = peak;
+    if ((uint32_t)(tid + j * kThreads) < peaks) high += weights.of(lds.peaks[tid + j * kThreads]) - Weights::none();
+  high = sum_of_lanes(high);
+  if (lane == 63) waves.best[wave] = high;
   if (tid == 0) lds.steps[0] = peaks;
   if (tid < 2 * kMostRuns) lds.mark[tid].bin = kSteps;
   __syncthreads();
-  peak = of_lane(sum_of_16(waves.low[lane & 15]), 15);
+  const float peak = (float)((double)of_lane(sum_of_16(waves.best[lane & 15]), 15) * 0x1p-40);
 
   // the sums of each thread's steps
   const double wide = 2.0 * scale.factor / steps.per, above = ((double)scale.top - (double)steps.from) * scale.factor - 0.5 * wide;
@@ -996,12 +998,12 @@ template <typename T> __device__ __forceinline__ bool is_answered(const Args& a,
 }
 
 // The first of the highest scores, as a code (all ones: there is none), and the lowest.
-template <typename T> __device__ __forceinline__ u64 best_of(Waves& lds, const Row<T>& row, float& low, bool& nan) {
+template <typename T> __device__ __forceinline__ u64 best_of(Waves& lds, const Row<T>& row, int first, int count, float& low, bool& nan) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float high = -INFINITY;
   int at = 0;
   nan = false, low = INFINITY;
-  for_each(row.row, 0, row.columns, [&](float x, int column) {
+  for_each(row.row, first, count, [&](float x, int column) {
     nan |= x != x;
     low = x > -INFINITY ? fminf(low, x) : low;
     const bool more = x > high;
@@ -1076,14 +1078,28 @@ template <typename T> __device__ __forceinline__ void find_slowly(const Args& a,
 }
 
 // ---- kernels ----------------------------------------------------------------------------------------------
-// What a row has in the workspace, written anew by each call.
-struct State {
+// The workspace: of a launch's first rows, which several workgroups share, the only words that have to be zero before a call, and are
+// behind it; what the second pass has to know of each row, and what each piece of a row has given the first.
+struct Counter {
+  uint32_t arrived, listed;
+};
+constexpr int kSharedRows = kGroups / 2, kCounterBytes = kSharedRows * sizeof(Counter);
+static_assert(kCounterBytes % 256 == 0);
+struct alignas(256) State {
   Head head;
   u64 weight[kMostRuns + 1];
   uint32_t listed, arrived;
   u64 list[kList];
 };
-constexpr int64_t kStateBytes = (sizeof(State) + 255) / 256 * 256;
+struct alignas(256) Part {
+  u64 best, high;  // `high` with flags above: a NaN, too many of a step
+  u64 steps[kSteps / 4];
+};
+struct Workspace {
+  Counter* counters;
+  State* states;
+  Part* parts;
+};
 constexpr int kHeadWords = sizeof(Head) / 4;
 static_assert(sizeof(Head) % 4 == 0 && kHeadWords <= kThreads);
 
@@ -1111,7 +1127,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) few_kernel(Arg
   if (threadIdx.x < 64) waves.head.ask = ask_of(a, r, temperature);  // (all lanes write the same)
   bool nan;
   float low;
-  const u64 best = best_of(waves, row, low, nan);
+  const u64 best = best_of(waves, row, 0, a.columns, low, nan);
   if (is_answered(a, r, row, best, nan, !(temperature > 0.f))) return;
   row.scale = {row.score(best), waves.head.ask.factor};
   const uint32_t n = row.gather(lds, [&](float, int) { return true; });
@@ -1121,50 +1137,147 @@ template <typename T> __global__ void __launch_bounds__(kThreads) few_kernel(Arg
   find<true>(a, r, row, waves, lds);
 }
 
-// The first pass over a longer row; SECOND: and all the rest.
-template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) row_kernel(Args a, int64_t row0, State* states, int64_t state_bytes) {
+// The scores of a row's piece.
+__device__ __forceinline__ void piece_of(int columns, int pieces, int piece, int& first, int& count) {
+  const int each = ((columns + pieces - 1) / pieces + 15) / 16 * 16;
+  first = min(each * piece, columns), count = min(each, columns - first);
+}
+
+// What a workgroup has found in its piece goes past the caches: counts, and the list behind what others have listed.
+__device__ __forceinline__ void give(Lists& lists, const Counts& counts, bool counted, u64 best, float high, bool nan, int count, State* state, Counter* counter,
+                                     Part* part) {
+  const int tid = threadIdx.x;
+  bool too_many = false;
+  if (counted) {
+    u64 packed[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t n = counts.steps[tid * 8 + j];
+      too_many |= n > 0xffff;
+      packed[j / 4] |= (u64)(n & 0xffff) << 16 * (j % 4);
+    }
+    write_through(&part->steps[2 * tid], packed[0]), write_through(&part->steps[2 * tid + 1], packed[1]);
+    if (count > 0xffff) too_many = __syncthreads_or(too_many);
+  }
+  if (tid == 0) {
+    write_through(&part->best, best);
+    write_through(&part->high, (u64)(nan ? 1 : 0) << 32 | (u64)(too_many ? 2 : 0) << 32 | __float_as_uint(high));
+  }
+  const uint32_t listed = counted ? counts.listed : lists.listed;
+  if (listed) {
+    if (tid == 0) lists.first = add_through(&counter->listed, listed);
+    __syncthreads();
+    const uint32_t first = lists.first;
+    for (uint32_t i = tid; i < min(listed, (uint32_t)kList) && first + i < kList; i += kThreads)
+      write_through(&state->list[first + i], counted ? (u64)__float_as_uint(counts.peaks[i]) : lists.list[i]);
+  }
+}
+// All that others have found, by the last of them.  The row's counters are zero then.
+__device__ __forceinline__ void take(Waves& waves, Lists& lists, Counts& counts, bool counted, u64& best, float& high, bool& nan, bool& too_many, State* state, Counter* counter, const Part* part, int pieces) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (tid < 64) {
+    u64 b = ~(u64)0;
+    uint32_t flags = 0;
+    float h = -INFINITY;
+    for (int i = lane; i < pieces; i += 64) {
+      const u64 x = read_through(&part[i].high);
+      b = min(b, read_through(&part[i].best)), flags |= (uint32_t)(x >> 32), h = fmaxf(h, __uint_as_float((uint32_t)x));
+    }
+    const u64 any_nan = __ballot(flags & 1), any_many = __ballot(flags & 2);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) b = min(b, (u64)__shfl_xor((long long)b, d));
+    h = largest(h);
+    if (tid == 0) waves.best[0] = b, waves.high[0] = h, waves.sure = (any_nan ? 1 : 0) | (any_many ? 2 : 0);
+  }
+  const uint32_t listed = read_through(&counter->listed);
+  if (counted) {
+    uint32_t n[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int i0 = 0; i0 < pieces; i0 += 8) {
+      u64 x[8][2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) x[i][j] = read_through(&part[min(i0 + i, pieces - 1)].steps[2 * tid + j]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i0 + i < pieces)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) n[j] += (uint32_t)(x[i][j / 4] >> 16 * (j % 4)) & 0xffff;
+    }
+    for (int j = 0; j < 8; ++j) counts.steps[8 * tid + j] = n[j];
+    for (uint32_t i = tid; i < min(listed, (uint32_t)kPeaks); i += kThreads) counts.peaks[i] = __uint_as_float((uint32_t)read_through(&state->list[i]));
+  } else {
+    for (uint32_t i = tid; i < min(listed, (uint32_t)kList); i += kThreads) lists.list[i] = read_through(&state->list[i]);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    lists.listed = counts.listed = listed;
+    write_through(&counter->arrived, 0u), write_through(&counter->listed, 0u);
+  }
+  best = waves.best[0], high = waves.high[0], nan = waves.sure & 1, too_many = waves.sure & 2;
+  __syncthreads();
+}
+
+// The first pass over a longer row; SECOND: and all the rest, by one workgroup.  Else several share it, and the last of them goes on.
+template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) row_kernel(Args a, int64_t row0, Workspace w, int pieces) {
   __shared__ Waves waves;
   __shared__ Lists lists;
   __shared__ Counts counts;
-  const int tid = threadIdx.x;
-  const int64_t r = row0 + blockIdx.x;
-  State* const state = reinterpret_cast<State*>(reinterpret_cast<char*>(states) + blockIdx.x * state_bytes);
+  const int tid = threadIdx.x, slot = SECOND ? blockIdx.x : blockIdx.x / pieces, piece = SECOND ? 0 : blockIdx.x % pieces;
+  const int64_t r = row0 + slot;
+  State* const state = w.states + slot;
+  Counter* const counter = w.counters + slot;
+  Part* const parts = w.parts + (int64_t)slot * pieces;
   const float temperature = parameter(a.temperature, r, 1.f);
+  const bool greedy = !(temperature > 0.f);
   Row<T> row{static_cast<const T*>(a.logits) + r * a.stride, a.columns, a.log2_columns, {0.f, 0.0}};
-  bool nan;
+  bool nan = false, too_many = false;
+  int first = 0, count = a.columns;
+  if (!SECOND) piece_of(a.columns, pieces, piece, first, count);
+  u64 best = ~(u64)0;
+  float high = -INFINITY, bound = NAN;
+  if (greedy) {
+    best = best_of(waves, row, first, count, high, nan);
+    if (tid == 0) lists.listed = 0;
+    __syncthreads();
+  } else {
+    look(a, r, row.row, temperature, waves, counts);
+    __syncthreads();
+    bound = counts.bound;
+    row.scale.factor = waves.head.ask.factor;
+  }
+  const Steps steps = waves.head.steps;
+  const bool bounded = bound == bound, counted = !greedy && !bounded;
+  if (bounded) high = gather_above(waves, lists, row, steps, first, count, bound, nan);
+  else if (counted) high = count_steps(waves, counts, row, steps, first, count, nan);
+  if (!SECOND && pieces > 1) {
+    give(lists, counts, counted, best, high, nan, count, state, counter, parts + piece);
+    if (!all_arrived(waves, &counter->arrived, pieces)) return;
+    take(waves, lists, counts, counted, best, high, nan, too_many, state, counter, parts, pieces);
+  }
   if (!SECOND && tid == 0) state->head.answered = 1;
-  if (!(temperature > 0.f)) {
-    float low;
-    const u64 best = best_of(waves, row, low, nan);
+  if (greedy) {
     is_answered(a, r, row, best, nan, true);
     return;
   }
-  look(a, r, row.row, temperature, waves, counts);
-  __syncthreads();
-  const Steps steps = waves.head.steps;
-  float bound = counts.bound;
-  row.scale.factor = waves.head.ask.factor;
-  if (bound == bound) {
-    float high = gather_above(waves, lists, row, steps, bound, nan);
-    if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
+  if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
+  row.scale.top = high;
+  if (bounded) {
     const uint32_t top_k = waves.head.ask.top_k;
     if (lists.listed > kList && !(top_k && top_k <= kBounded)) {  // (min_p alone: with the highest score known the bound is what it has to be)
       bound = fmaxf(steps.down((float)fmax((double)high - waves.head.ask.far / row.scale.factor, -(double)FLT_MAX)), 0.f) + 1.f;
       __syncthreads();
-      high = gather_above(waves, lists, row, steps, bound, nan);
+      gather_above(waves, lists, row, steps, 0, a.columns, bound, nan);
     }
     const uint32_t n = lists.listed;
     if (n && n <= kList && (n >= top_k || bound == INFINITY)) {
-      row.scale.top = high;
       plan_all(waves, n, bound < kSteps - 4 ? (int)bound : kSteps - 2);
       __syncthreads();
       if (find<false>(a, r, row, waves, lists)) return;
     }
     __syncthreads();
   }
-  const float high = count_steps(waves, counts, row, steps, nan);
-  if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
-  row.scale.top = high;
+  if (bounded || too_many) count_steps(waves, counts, row, steps, 0, a.columns, nan);
   plan_row(waves, counts, row.scale);
   if constexpr (SECOND) {
     if (!waves.head.plan.slow) {
@@ -1180,19 +1293,13 @@ template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) r
   }
 }
 
-// The scores of a row's piece.
-__device__ __forceinline__ void piece_of(int columns, int pieces, int piece, int& first, int& count) {
-  const int each = ((columns + pieces - 1) / pieces + 15) / 16 * 16;
-  first = min(each * piece, columns), count = min(each, columns - first);
-}
-
 // The second pass over a row, by several workgroups; the last of them does the rest.
-template <typename T> __global__ void __launch_bounds__(kThreads) gather_kernel(Args a, int64_t row0, State* states, int64_t state_bytes, int pieces) {
+template <typename T> __global__ void __launch_bounds__(kThreads) gather_kernel(Args a, int64_t row0, Workspace w, int pieces) {
   __shared__ Waves waves;
   __shared__ Lists lds;
   const int tid = threadIdx.x, slot = blockIdx.x / pieces, piece = blockIdx.x % pieces;
   const int64_t r = row0 + slot;
-  State* const state = reinterpret_cast<State*>(reinterpret_cast<char*>(states) + slot * state_bytes);
+  State* const state = w.states + slot;
   if (state->head.answered) return;
   if (tid < kHeadWords) reinterpret_cast<uint32_t*>(&waves.head)[tid] = reinterpret_cast<const uint32_t*>(&state->head)[tid];
   __syncthreads();
@@ -1218,18 +1325,24 @@ template <typename T> __global__ void __launch_bounds__(kThreads) gather_kernel(
   find_slowly(a, r, row, waves, lds);
 }
 
-template <typename T> void launch(const Args& a, int64_t rows, State* states, hipStream_t stream) {
+int64_t states_of(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(rows, kMostRows)); }
+
+template <typename T> void launch(const Args& a, int64_t rows, void* workspace, hipStream_t stream) {
   if (a.columns <= kList) {
     hipLaunchKernelGGL(few_kernel<T>, dim3((unsigned)rows), dim3(kThreads), 0, stream, a);
     return;
   }
+  Workspace w{static_cast<Counter*>(workspace), reinterpret_cast<State*>(static_cast<char*>(workspace) + kCounterBytes), nullptr};
+  w.parts = reinterpret_cast<Part*>(w.states + states_of(rows));
   for (int64_t row0 = 0; row0 < rows; row0 += kMostRows) {
     const int n = (int)std::min<int64_t>(rows - row0, kMostRows), pieces = std::min(kGroups / n, a.columns / kLeastPiece);
     if (pieces < 2) {
-      hipLaunchKernelGGL((row_kernel<T, true>), dim3((unsigned)n), dim3(kThreads), 0, stream, a, row0, states, kStateBytes);
+      hipLaunchKernelGGL((row_kernel<T, true>), dim3((unsigned)n), dim3(kThreads), 0, stream, a, row0, w, 1);
     } else {
-      hipLaunchKernelGGL((row_kernel<T, false>), dim3((unsigned)n), dim3(kThreads), 0, stream, a, row0, states, kStateBytes);
-      hipLaunchKernelGGL(gather_kernel<T>, dim3((unsigned)(n * pieces)), dim3(kThreads), 0, stream, a, row0, states, kStateBytes, pieces);
+      int counted = std::min({kGroups / n, a.columns / kLeastCounted, kMostCounts});
+      if (counted < kFewestCounts) counted = 1;
+      hipLaunchKernelGGL((row_kernel<T, false>), dim3((unsigned)(n * counted)), dim3(kThreads), 0, stream, a, row0, w, counted);
+      hipLaunchKernelGGL(gather_kernel<T>, dim3((unsigned)(n * pieces)), dim3(kThreads), 0, stream, a, row0, w, pieces);
     }
   }
 }
@@ -1241,7 +1354,8 @@ extern "C" {
 int64_t rsr_sample_workspace(int64_t rows, int64_t columns) {
   if (rows < 0 || rows > 1 << 24) return set_error(RSR_ERR_INVALID_ARGUMENT, "rows must be in 0..2^24");
   if (columns < 1 || columns > 1 << 22) return set_error(RSR_ERR_INVALID_ARGUMENT, "columns must be in 1..2^22");
-  return std::max<int64_t>(1, std::min<int64_t>(rows, kMostRows)) * kStateBytes;
+  const int64_t parts = std::min<int64_t>(kGroups, std::min<int64_t>(rows, kMostRows) * (columns / kLeastCounted));
+  return kCounterBytes + states_of(rows) * (int64_t)sizeof(State) + parts * (int64_t)sizeof(Part);
 }
 
 int rsr_sample(const void* logits, int64_t rows, int64_t columns, int64_t stride, int dtype, const float* temperature, const int32_t* top_k,
@@ -1258,7 +1372,7 @@ int rsr_sample(const void* logits, int64_t rows, int64_t columns, int64_t stride
     return set_error(RSR_ERR_INVALID_ARGUMENT, "the workspace is missing, too small or not 256-byte aligned");
   Args a{logits, temperature, top_p, min_p, uniform, top_k, token, probability, kept, stride, (int32_t)columns, 1};
   while ((int64_t)1 << a.log2_columns < columns) ++a.log2_columns;
-  (dtype == RSR_F32 ? launch<float> : dtype == RSR_F16 ? launch<_Float16> : launch<__bf16>)(a, rows, static_cast<State*>(workspace), static_cast<hipStream_t>(stream));
+  (dtype == RSR_F32 ? launch<float> : dtype == RSR_F16 ? launch<_Float16> : launch<__bf16>)(a, rows, workspace, static_cast<hipStream_t>(stream));
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(RSR_ERR_HIP, std::string("rsr_sample: ") + hipGetErrorString(e));
   return RSR_OK;
