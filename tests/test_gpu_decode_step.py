@@ -1,0 +1,295 @@
+"""A decoder's step as it is used: rsr_head_rotate, rsr_tree_attention, rsr_sample, rsr_tree_keep, rsr_cache_slots and rsr_cache_append, one
+behind the other, in graphs and on streams of their own."""
+import numpy as np
+import pytest
+
+from examples.tree_decode import Config, Weights, run
+from oracle import decode as oracle
+from tests.cache_util import draft
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+import paper_2411_06360_amd as R  # noqa: E402
+
+
+def bf16(x):
+    return torch.from_numpy(np.asarray(x, np.float32)).bfloat16().double().numpy()
+
+
+def plain_decode(c: Config, w: Weights, request: int, uniform, prompt, length):
+    """The tokens one by one in 64 bits (keys and values rounded as the cache rounds them)."""
+    m = {n: a.astype(np.float64) * w.scale for n, a in w.matrices.items()}
+    group, d = c.heads // c.kv_heads, c.head_dim
+    frequency = 1e4 ** -(np.arange(d // 2) / (d // 2))
+    keys, values, tokens = [], [], list(prompt)
+    for at in range(len(prompt) + length - 1):
+        x = w.tokens[tokens[at]].astype(np.float64)
+        turned = {n: oracle.rotate((x @ m[n])[None], [at], frequency, d, eps=np.float32(1e-6))[0][0] for n in ("q", "k")}
+        keys.append(bf16(turned["k"]).reshape(c.kv_heads, d))
+        values.append(bf16(x @ m["v"]).reshape(c.kv_heads, d))
+        if at < len(prompt) - 1:
+            continue
+        q, K, V = turned["q"].reshape(c.heads, d), np.array(keys), np.array(values)
+        mixed = np.empty((c.heads, d))
+        for a in range(c.heads):
+            s = K[:, a // group] @ q[a] * d ** -0.5
+            e = np.exp(s - s.max())
+            mixed[a] = e @ V[:, a // group] / e.sum()
+        scores = (x + w.attention * (mixed.reshape(-1) @ m["o"])) @ m["head"]
+        tokens.append(oracle.sample(scores, temperature=np.float32(c.temperature), top_p=np.float32(c.top_p), uniform=uniform[request, at])[0])
+    return tokens[len(prompt):]
+
+
+@pytest.mark.parametrize("temperature,top_p", [(0.0, 1.0), (0.7, 0.9), (1.0, 1.0)])
+def test_trees_decode_what_single_tokens_do(temperature, top_p):
+    """With rotated heads, and drawn: a token is drawn with its request's number of its position, so that trees change nothing."""
+    print("example", temperature, top_p, flush=True)
+    c = Config(hidden=256, heads=4, kv_heads=2, vocabulary=64, k=6, page_size=16, pages=48, pages_per_request=8, seed=5, rotary=True, temperature=temperature, top_p=top_p)
+    results = run(c, requests=3, prompt=5, length=30, widths=(3, 2, 1))
+    assert results["plain"]["tokens"] == results["drafted"]["tokens"]
+    rng, w = np.random.default_rng(c.seed + 1), Weights(c)
+    uniform = np.random.default_rng(c.seed + 2).random((3, len(w.positions)), dtype=np.float32)
+    for r in range(3):
+        prompt = rng.integers(0, c.vocabulary, 5 + 7 * r).tolist()
+        assert results["drafted"]["tokens"][r] == plain_decode(c, w, r, uniform, prompt, 30)
+
+
+HEADS, KV, DIM, PAGE, PAGES, WORDS = 8, 2, 64, 16, 64, 5000
+
+
+class Step:
+    """Everything that a step of three requests with drafted trees has, in buffers that stay where they are."""
+
+    def __init__(self, new=(9, 1, 20)):
+        ints = {"dtype": torch.int32, "device": "cuda"}
+        self.new, self.n = new, sum(new)
+        self.start = torch.tensor(np.concatenate([[0], np.cumsum(new)]), **ints)
+        self.owner = torch.repeat_interleave(torch.arange(len(new)), torch.tensor(new)).cuda()
+        wide = (HEADS + 2 * KV) * DIM
+        self.qkv = torch.empty((self.n, wide), device="cuda")
+        self.q, self.k, self.v = self.qkv.split([HEADS * DIM, KV * DIM, KV * DIM], dim=1)
+        self.mixed = torch.empty((self.n, HEADS * DIM), device="cuda")
+        self.matrix = torch.randn((HEADS * DIM, WORDS), generator=torch.Generator().manual_seed(1)).cuda()
+        self.logits = torch.empty((self.n, WORDS), device="cuda")
+        self.parent, self.drafted, self.depth, self.chosen, self.kept, self.rows, self.found, self.slots, self.position = (torch.zeros(self.n, **ints) for _ in range(9))
+        self.mask = torch.zeros(self.n, dtype=torch.int64, device="cuda")
+        self.add, self.first = torch.zeros(3, **ints), torch.zeros(4, **ints)
+        self.uniform, self.probability = (torch.zeros(self.n, device="cuda") for _ in range(2))
+        self.how = dict(temperature=torch.full((self.n,), 8.0, device="cuda"), top_k=torch.full((self.n,), 40, **ints), top_p=torch.full((self.n,), 0.9, device="cuda"))
+        self.keys, self.values = (torch.zeros((PAGES, KV, PAGE, DIM), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        self.cache = R.make_cache(self.keys, self.values)
+        self.table = torch.zeros((3, 12), **ints)
+        self.free, self.count, self.left = torch.arange(PAGES, **ints), torch.zeros(1, **ints), torch.zeros(1, **ints)
+        self.held, self.now, self.begin = torch.zeros(3, **ints), torch.zeros(3, **ints), torch.zeros(4, **ints)
+        weight = torch.linspace(0.5, 1.5, DIM).cuda()
+        self.rotary = R.make_rotary(1e4 ** -(torch.arange(DIM // 2, dtype=torch.float64) / (DIM // 2)).cuda(), DIM, eps=1e-6, q_weight=weight, k_weight=weight.flip(0).contiguous())
+        self.step = R.make_step(self.table, self.held, self.start, self.n, max(new), self.mask)
+        self.workspace = torch.zeros(R.rsr_tree_attention_workspace(self.cache, self.step, HEADS), dtype=torch.uint8, device="cuda")
+        self.space = torch.zeros(R.rsr_sample_workspace(self.n, WORDS), dtype=torch.uint8, device="cuda")
+
+    def fill(self, seed):
+        """Other inputs, and the cache as it was at first; each guess is what will be chosen, where `guess` knows."""
+        rng, g = np.random.default_rng(seed), torch.Generator().manual_seed(seed)
+        self.qkv.copy_(torch.randn(self.qkv.shape, generator=g))
+        self.parent.copy_(torch.tensor([p for n in self.new for p in draft(rng, n)], dtype=torch.int32))
+        self.drafted.copy_(torch.from_numpy(rng.integers(0, WORDS, self.n).astype(np.int32)))
+        self.uniform.copy_(torch.rand(self.n, generator=g))
+        for x in (self.keys, self.values):
+            x.copy_(torch.randn(x.shape, generator=g))
+        held = torch.tensor([37, 16, 0], dtype=torch.int32)
+        self.held.copy_(held), self.count.fill_(PAGES - 4), self.free.copy_(torch.arange(PAGES))
+        table = torch.full((3, 12), -1, dtype=torch.int32)
+        table[0, :3], table[1, :1] = torch.tensor([60, 61, 62], dtype=torch.int32), 63
+        self.table.copy_(table)
+        for x in (self.chosen, self.rows, self.found, self.slots):
+            x.fill_(-7)
+        self.begin_values = self.qkv.double().cpu().numpy()
+
+    def guess(self, chosen):
+        """Half of the guesses are what was chosen behind the tokens on which they hang."""
+        parent, start = self.parent.tolist(), self.start.tolist()
+        for r in range(3):
+            for i in range(start[r] + 1, start[r + 1], 2):
+                if parent[i] >= 0:
+                    self.drafted[i] = chosen[start[r] + parent[i]]
+
+    def go(self, stream=None):
+        s = (stream or torch.cuda.current_stream()).cuda_stream
+        R.rsr_tree_masks(self.parent, self.start, self.mask, self.depth, s)
+        torch.add(self.depth, self.held[self.owner], out=self.position)
+        R.rsr_head_rotate(self.rotary, self.q, self.k, self.position, self.q, self.k, s)
+        R.rsr_tree_attention(self.cache, self.step, self.q, self.k, self.v, self.mixed, HEADS, DIM ** -0.5, self.workspace, s)
+        torch.mm(self.mixed, self.matrix, out=self.logits)
+        R.rsr_sample(self.logits, self.uniform, self.chosen, self.space, probability=self.probability, kept=self.kept, stream=s, **self.how)
+        R.rsr_tree_keep(self.drafted, self.chosen, self.parent, self.start, self.rows, self.found, self.add, self.first, s)
+        R.rsr_cache_slots(self.held, self.add, self.table, PAGE, self.free, self.count, self.slots, self.begin, self.now, self.left, s)
+        R.rsr_cache_append(self.cache, self.k, self.v, self.slots, self.rows, s)
+
+    def results(self):
+        torch.cuda.synchronize()
+        return [x.clone() for x in (self.chosen, self.kept, self.probability, self.rows, self.found, self.add, self.first, self.slots, self.now, self.table, self.keys, self.values, self.qkv)]
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def eager(step, seed):
+    step.fill(seed)
+    step.go()
+    chosen = step.chosen.tolist()
+    step.fill(seed)
+    step.guess(chosen)
+    step.go()
+    return step.results()
+
+
+def test_a_step_by_its_parts():
+    """Each part against its definition, with what the parts before it have left."""
+    step = Step()
+    for seed in range(3):
+        eager(step, seed)
+        before = step.begin_values
+        frequency, weight = 1e4 ** -(np.arange(DIM // 2) / (DIM // 2)), torch.linspace(0.5, 1.5, DIM).numpy()
+        for x, at, by in ((step.q, 0, weight), (step.k, HEADS * DIM, weight[::-1])):
+            want, size = oracle.rotate(before[:, at:at + x.shape[1]], step.position.cpu().numpy(), frequency, DIM, eps=np.float32(1e-6), weight=by)
+            # 18.1 units of 2^-24, as for the operator alone, and the frequencies' 2^-53 at angles below 2^7
+            assert (np.abs(x.double().cpu().numpy() - want) <= 18.2 * 2.0**-24 * size).all()
+        rows = step.logits.double().cpu().numpy()
+        drawn = [oracle.sample(rows[i], 8.0, 40, float(np.float32(0.9)), 0.0, float(step.uniform[i])) for i in range(step.n)]
+        assert step.chosen.tolist() == [t for t, _, _ in drawn] and step.kept.tolist() == [n for _, _, n in drawn]
+        want = oracle.keep(step.drafted.tolist(), step.chosen.tolist(), step.parent.tolist(), step.start.tolist(), step.n)
+        assert (step.rows.tolist(), step.found.tolist(), step.add.tolist(), step.first.tolist()) == want
+        assert sum(want[2]) > 3  # (some guesses were right)
+        # the kept tokens' keys and values are in the cache, behind what was there
+        for r, at in enumerate(want[3][:3]):
+            for i in range(want[2][r]):
+                place, row = int(step.held[r]) + i, want[0][at + i]
+                page = int(step.table[r, place // PAGE])
+                for pages, x in ((step.keys, step.k), (step.values, step.v)):
+                    assert torch.equal(pages[page, :, place % PAGE].flatten(), x[row].bfloat16())
+
+
+def test_a_step_in_a_graph():
+    """Replayed with other inputs in the same buffers, with eager work between the replays."""
+    step = Step()
+    wanted = [eager(step, seed) for seed in range(4)]
+    guesses = []
+    for seed in range(4):
+        step.fill(seed)
+        step.guess(wanted[seed][0].tolist())
+        guesses.append(step.drafted.clone())
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step.go()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step.go()
+    for seed in (0, 1, 2, 3, 2, 0):
+        step.fill(seed)
+        step.drafted.copy_(guesses[seed])
+        graph.replay()
+        assert same(step.results(), wanted[seed]), f"replay {seed}"
+        other = eager(step, 1)
+        assert same(other, wanted[1])
+
+
+def sampling(rows, columns, seed, space):
+    g = torch.Generator().manual_seed(seed)
+    x, u = 2 * torch.randn((rows, columns), generator=g).cuda(), torch.rand(rows, generator=g).cuda()
+    x[:, 17] += 9
+    token, kept = (torch.full((rows,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    kind = torch.arange(rows) % 4
+    how = dict(temperature=torch.tensor([1.0, 0.0, 0.8, 1.5])[kind].cuda(), top_k=torch.tensor([0, 0, 50, 0], dtype=torch.int32)[kind].cuda(), top_p=torch.tensor([0.9, 1.0, 1.0, 1.0])[kind].cuda(),
+               min_p=torch.tensor([0.0, 0.0, 0.0, 0.05])[kind].cuda())
+    return x, u, token, kept, how, lambda: R.rsr_sample(x, u, token, space, kept=kept, stream=torch.cuda.current_stream().cuda_stream, **how)
+
+
+def test_graphs_that_share_a_workspace():
+    """Calls of different shapes, one behind the other, captured into two graphs and between them eager ones, all with one workspace."""
+    shapes = [(5, 131072), (64, 66000), (300, 9000), (3, 1000)]
+    space = torch.zeros(max(R.rsr_sample_workspace(*s) for s in shapes), dtype=torch.uint8, device="cuda")
+    calls = [sampling(*s, seed, space) for seed, s in enumerate(shapes)]
+    wanted = []
+    for x, u, token, kept, how, call in calls:
+        call()
+        torch.cuda.synchronize()
+        wanted.append((token.clone(), kept.clone()))
+        rows = x.double().cpu().numpy()
+        given = [(float(how["temperature"][r]), int(how["top_k"][r]), float(how["top_p"][r]), float(how["min_p"][r]), float(u[r])) for r in range(min(8, len(rows)))]
+        assert [(int(token[r]), int(kept[r])) for r in range(len(given))] == [oracle.sample(rows[r], *g)[::2] for r, g in enumerate(given)]
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for graph, some in zip(graphs, ((0, 2, 1), (1, 3, 0))):
+        with torch.cuda.graph(graph):
+            for i in some:
+                calls[i][-1]()
+    for turn in range(4):
+        for c in calls:
+            c[2].fill_(-7), c[3].fill_(-7)
+        graphs[turn % 2].replay()
+        calls[2 if turn % 2 else 3][-1]()
+        graphs[1 - turn % 2].replay()
+        torch.cuda.synchronize()
+        for (_, _, token, kept, _, _), want in zip(calls, wanted):
+            assert torch.equal(token, want[0]) and torch.equal(kept, want[1]), turn
+
+
+def test_streams_at_once():
+    """Calls on streams of their own, with workspaces of their own, none of which waits for another."""
+    calls = []
+    for i in range(3):
+        shape = ((40, 131072), (16, 70000), (256, 20000))[i]
+        calls.append(sampling(*shape, 10 + i, torch.zeros(R.rsr_sample_workspace(*shape), dtype=torch.uint8, device="cuda")))
+    wanted = []
+    for c in calls:
+        c[-1]()
+        torch.cuda.synchronize()
+        wanted.append((c[2].clone(), c[3].clone()))
+        c[2].fill_(-7), c[3].fill_(-7)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(10):
+        for c, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                c[-1]()
+    torch.cuda.synchronize()
+    for c, want in zip(calls, wanted):
+        assert torch.equal(c[2], want[0]) and torch.equal(c[3], want[1])
+
+
+@pytest.mark.parametrize("shape", [(1, 1 << 22), (2, 1 << 20), (1, 131072), (63, 70000), (65, 66000)])
+def test_a_row_by_many_workgroups(shape):
+    """Rows that several workgroups share: whole rows of one score, of two, a NaN or the only number in any piece."""
+    print("shared rows", shape, flush=True)
+    rows, columns = shape
+    space = torch.zeros(R.rsr_sample_workspace(rows, columns), dtype=torch.uint8, device="cuda")
+    token, kept = (torch.full((rows,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    u = torch.full((rows,), 0.75, device="cuda")
+    x = torch.zeros((rows, columns), dtype=torch.bfloat16, device="cuda")
+    half = torch.full((rows,), 0.5, device="cuda")
+
+    def call(**how):
+        R.rsr_sample(x, u, token, space, kept=kept, stream=torch.cuda.current_stream().cuda_stream, **how)
+        torch.cuda.synchronize()
+        return token.tolist(), kept.tolist()
+
+    # (running sums of equal weights: the first of which the sum is above u times all is the token with the number of u times all)
+    assert call() == ([columns * 3 // 4] * rows, [columns] * rows)
+    assert call(top_p=half) == ([-(-columns // 2) * 3 // 4] * rows, [-(-columns // 2)] * rows)
+    assert call(temperature=0 * half) == ([0] * rows, [1] * rows)
+    assert call(min_p=half) == ([columns * 3 // 4] * rows, [columns] * rows)
+    assert call(top_k=torch.full((rows,), 7, dtype=torch.int32, device="cuda")) == ([5] * rows, [7] * rows)
+    for at in (0, columns // 3, columns - 1):
+        x.fill_(-float("inf"))
+        x[:, at] = -3
+        assert call() == ([at] * rows, [1] * rows)
+        assert call(temperature=0 * half) == ([at] * rows, [1] * rows)
+        assert call(min_p=half) == ([at] * rows, [1] * rows)
+        x[:, at] = float("nan")
+        assert call() == ([-1] * rows, [0] * rows)
+        assert call(temperature=0 * half) == ([-1] * rows, [0] * rows)
+        assert call(top_k=torch.full((rows,), 7, dtype=torch.int32, device="cuda")) == ([-1] * rows, [0] * rows)
+    x.fill_(-float("inf"))
+    assert call() == ([-1] * rows, [0] * rows)
