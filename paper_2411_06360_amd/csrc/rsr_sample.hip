@@ -105,8 +105,9 @@ struct Plan {
   uint32_t tokens;  // of all runs
   uint32_t all;     // of the row
   int weighed;      // it adds up weights
-  int slow;         // too many tokens
+  int slow;         // kMany: too many tokens for the list; kSlow: too many above the steps, or no steps
 };
+constexpr int kMany = 1, kSlow = 2;
 
 // What a row is asked for.
 struct Ask {
@@ -155,7 +156,11 @@ struct Lists {
   uint32_t part_count[kBins + 1];                 // of a finer histogram, or where buckets begin
   union { u64 part_sum[kBins]; double part_mass[kBins]; u64 bucketed[kList]; };
   uint32_t count[kBins];                          // of the slow way: up to and with the bin
-  union { u64 sum[kBins]; double mass[kBins]; };  // packed as above; then the weight up to and with the bin
+  union {
+    u64 sum[kBins];  // packed as above; then
+    double mass[kBins];  // the weight up to and with the bin
+    struct { uint32_t least[kBins], most[kBins]; };  // keys, where equal scores are counted
+  };
   u64 weight[kMostRuns + 1];                      // before each run, and of all
   uint32_t listed, first;
 };
@@ -761,7 +766,7 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
   const Steps steps = waves.head.steps;
   const uint32_t peaks = lds.listed;
   if (peaks > kPeaks || scale.top == INFINITY) {
-    if (tid == 0) waves.head.plan.slow = 1;
+    if (tid == 0) waves.head.plan.slow = kSlow;
     __syncthreads();
     return;
   }
@@ -909,7 +914,7 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
       plan.run[i] = {lo[i], hi[i], plan.tokens, there ? upto[i] - before[i] : 0, before[i], 0, 0, 0.0};
       plan.tokens += plan.run[i].count, plan.n += there;
     }
-    plan.slow = plan.tokens > kList;
+    plan.slow = plan.tokens > kList ? kMany : 0;
     if (lane == 0) waves.head.plan = plan;
   }
   __syncthreads();
@@ -917,20 +922,25 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
 
 // ---- the second pass --------------------------------------------------------------------------------------
 // Gathers the tokens of the plan's runs among `count` scores from `first` on.  RUNS: adds up the weights before each of so many runs too, and
-// of all.  0: there is one run, from the first token on.
-template <int RUNS, typename T> __device__ __forceinline__ void gather_runs(const Plan& plan, Lists& lds, const Row<T>& row, const Steps& steps, int first, int count) {
+// of all.  0: there is one run, from the first token on.  EQUAL: does not list tokens, but counts them, each run's in kEach parts, with the least and
+// the most of their keys.
+constexpr int kEach = kBins / kMostRuns;
+template <int RUNS, bool EQUAL, typename T> __device__ __forceinline__ void gather_runs(const Plan& plan, Lists& lds, const Row<T>& row, const Steps& steps, int first, int count) {
   constexpr int kWide = 16 / sizeof(T), kRuns = RUNS ? RUNS : 1;
   if (threadIdx.x == 0) lds.listed = 0;
   if (threadIdx.x <= kMostRuns) lds.weight[threadIdx.x] = 0;
+  if constexpr (EQUAL)
+    for (int i = threadIdx.x; i < kBins; i += kThreads) lds.count[i] = lds.most[i] = 0, lds.least[i] = ~0u;
   __syncthreads();
   const Weights weights{row.scale.top, row.scale.factor};
-  float lo[kRuns], hi[kRuns];
+  float lo[kRuns], hi[kRuns], from[kRuns], per[kRuns];
   u64 before[kRuns], all = 0;
   uint32_t pieces = 0;
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
     const bool there = i < plan.n;
     lo[i] = there ? Steps::first_of(plan.run[i].b0) : INFINITY, hi[i] = there ? Steps::last_of(plan.run[i].b1) : -INFINITY, before[i] = 0;
+    if constexpr (EQUAL) from[i] = there && plan.run[i].b0 ? lo[i] : steps.down(row.scale.top), per[i] = kEach / ((float)plan.run[i].b1 - from[i]);
   }
   auto wanted = [&](float down) {
     bool in = false;
@@ -956,6 +966,16 @@ template <int RUNS, typename T> __device__ __forceinline__ void gather_runs(cons
 #pragma unroll
       for (int j = 0; j < kWide; ++j)
         if (wanted(steps.down(x[j])) && x[j] > -INFINITY) {
+          if constexpr (EQUAL) {
+            const float down = steps.down(x[j]);
+            int part = 0;
+#pragma unroll
+            for (int i = 0; i < kRuns; ++i)
+              if (down >= lo[i] && down <= hi[i]) part = i * kEach + (int)__builtin_amdgcn_fmed3f((down - from[i]) * per[i], 0.f, (float)(kEach - 1));
+            const uint32_t key = Key<T>::of(x[j]);
+            atomicAdd(&lds.count[part], 1u), atomicMin(&lds.least[part], key), atomicMax(&lds.most[part], key);
+            continue;
+          }
           const uint32_t at = atomicAdd(&lds.listed, 1u);
           if (at < kList) lds.list[at] = row.code(x[j], column + j);
         }
@@ -974,10 +994,11 @@ template <int RUNS, typename T> __device__ __forceinline__ void gather_runs(cons
 }
 
 template <typename T> __device__ __forceinline__ void gather_plan(const Plan& plan, Lists& lds, const Row<T>& row, const Steps& steps, int first, int count) {
-  if (!plan.weighed) gather_runs<0>(plan, lds, row, steps, first, count);
-  else if (plan.n == 1) gather_runs<1>(plan, lds, row, steps, first, count);
-  else if (plan.n == 2) gather_runs<2>(plan, lds, row, steps, first, count);
-  else gather_runs<4>(plan, lds, row, steps, first, count);
+  if (plan.slow) plan.n <= 2 ? gather_runs<2, true>(plan, lds, row, steps, first, count) : gather_runs<4, true>(plan, lds, row, steps, first, count);
+  else if (!plan.weighed) gather_runs<0, false>(plan, lds, row, steps, first, count);
+  else if (plan.n == 1) gather_runs<1, false>(plan, lds, row, steps, first, count);
+  else if (plan.n == 2) gather_runs<2, false>(plan, lds, row, steps, first, count);
+  else gather_runs<4, false>(plan, lds, row, steps, first, count);
 }
 
 // ---- answers ----------------------------------------------------------------------------------------------
@@ -1044,6 +1065,123 @@ template <bool SPANNED, typename T> __device__ __forceinline__ bool find(const A
   return waves.sure;
 }
 
+// The runs have more tokens than the list, but they are counted, and in every part all are equal: the answer, if that holds and it is sure.
+// Among equal tokens a place is a number, and the token itself is looked for.
+template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, int64_t r, const Row<T>& row, Waves& waves, Lists& lds) {
+  const Plan& plan = waves.head.plan;
+  const Ask& ask = waves.head.ask;
+  const int tid = threadIdx.x;
+  int near = 0;
+  for (int i = 1; i < kMostRuns; ++i)
+    if (i < plan.n && plan.run[i].b0 <= plan.near) near = i;
+  if (tid == 0) lds.first = 0;
+  Sums<double> s;
+  bool mixed = false, is_near[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int part = 2 * tid + j;
+    const uint32_t n = lds.count[part];
+    const float x = Key<T>::score(n ? lds.least[part] : 0);
+    mixed |= n && lds.least[part] != lds.most[part];
+    is_near[j] = n && plan.near >= 0 && part / kEach == near && row.scale.distance(x) <= ask.far;
+    s.c[j] = n, s.m[j] = n ? n * row.scale.weight(x) : 0.0;
+  }
+  if (__syncthreads_or(mixed)) return false;
+  s.scan(waves, 0, 0.0);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    lds.part_count[2 * tid + j] = s.c[j], lds.upto[2 * tid + j] = s.m[j];
+    if (is_near[j]) atomicMax(&lds.first, (uint32_t)(2 * tid + j + 1));
+  }
+  __syncthreads();
+  if (lds.part_count[kBins - 1] != plan.tokens) return false;
+
+  if (tid < 64) {
+    uint32_t kept = plan.all, before, count, nth;
+    double mass = (double)lds.weight[kMostRuns] * 0x1p-40, mass_before, upto;
+    int part;
+    bool is_sure = true;
+    // a run's sums up to and with a part
+    auto counted = [&](int i, int at) { return plan.run[i].before + lds.part_count[at] - (i ? lds.part_count[i * kEach - 1] : 0); };
+    auto weighed = [&](int i, int at) { return (double)lds.weight[i] * 0x1p-40 + (lds.upto[at] - (i ? lds.upto[i * kEach - 1] : 0.0)); };
+    auto seek = [&](const At& p) {
+      int i = 0;
+      while (i + 1 < plan.n && !p.reached(counted(i, i * kEach + kEach - 1), weighed(i, i * kEach + kEach - 1))) ++i;
+      int lo = i * kEach, hi = lo + kEach - 1;
+      const bool behind = p.reached(counted(i, hi), weighed(i, hi));
+      is_sure &= (!plan.run[i].before || !p.reached(plan.run[i].before, (double)lds.weight[i] * 0x1p-40)) && (behind || counted(i, hi) == plan.all);
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (p.reached(counted(i, mid), weighed(i, mid))) hi = mid;
+        else lo = mid + 1;
+      }
+      auto size = [&](int at) { return lds.part_count[at] - (at ? lds.part_count[at - 1] : 0); };
+      while (!size(lo) && lo < i * kEach + kEach - 1) ++lo;  // (what is reached before the first one is the first one's)
+      while (!size(lo)) --lo;                                // (and what rounding puts behind the last is the last one's)
+      part = lo;
+      const uint32_t n = size(part);
+      const double weight = row.scale.weight(Key<T>::score(lds.least[part]));
+      before = counted(i, part) - n, mass_before = weighed(i, part) - n * weight;
+      const double of = fmin(fmax((p.mass - mass_before) / weight, 0.0), (double)n);
+      nth = min(max(p.of_count ? p.count - before : p.strict ? (uint32_t)floor(of) + 1 : (uint32_t)ceil(of), 1u), n);
+      count = before + nth, upto = mass_before + nth * weight;
+    };
+    if (ask.top_k && ask.top_k < kept) {
+      seek(At::tokens(ask.top_k));
+      kept = ask.top_k, mass = upto;
+    }
+    if (ask.top_p < 1.0) {
+      seek(At::weight(ask.top_p * mass, false));
+      if (count < kept) kept = count, mass = upto;
+    }
+    if (plan.near >= 0) {
+      const int last = (int)lds.first - 1;
+      const uint32_t n = last < 0 ? plan.run[near].before : counted(near, last), end = plan.run[near].before + plan.run[near].count;
+      is_sure &= n < end || end >= kept;
+      if (n < kept) kept = n, mass = last < 0 ? (double)lds.weight[near] * 0x1p-40 : weighed(near, last);
+    }
+    seek(At::weight(ask.u * mass, true));
+    if (tid == 0) waves.sure = is_sure, waves.count[0] = lds.least[part], waves.count[1] = nth, waves.count[2] = kept, waves.mass[0] = mass;
+  }
+  __syncthreads();
+  if (!waves.sure) return false;
+  const float x = Key<T>::score(waves.count[0]);
+  const uint32_t number = waves.count[1], kept = waves.count[2];
+  const double mass = waves.mass[0];
+
+  // the token: a count of the equal ones in 2048 parts of the row, then one part
+  const int shift = max(0, row.log2_columns - 11);
+  __syncthreads();
+  lds.part_count[2 * tid] = lds.part_count[2 * tid + 1] = 0;
+  __syncthreads();
+  for_each(row.row, 0, row.columns, [&](float y, int column) {
+    if (y == x) atomicAdd(&lds.part_count[column >> shift], 1u);
+  });
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 2; ++j) s.c[j] = lds.part_count[2 * tid + j], s.m[j] = 0.0;
+  s.scan(waves, 0, 0.0);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t c = j ? s.c[0] : s.c_before;
+    if (c < number && s.c[j] >= number) lds.first = 2 * tid + j, lds.listed = number - c;
+  }
+  __syncthreads();
+  const int column = ((int)lds.first << shift) + 2 * tid, end = min(((int)lds.first + 1) << shift, row.columns);
+  const uint32_t wanted = lds.listed;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) s.c[j] = column + j < end && (float)row.row[min(column + j, row.columns - 1)] == x, s.m[j] = 0.0;
+  s.scan(waves, 0, 0.0);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t c = j ? s.c[0] : s.c_before;
+    if (c < wanted && s.c[j] >= wanted) lds.first = column + j;
+  }
+  __syncthreads();
+  answer(a, r, (int)lds.first, (float)(row.scale.weight(x) / mass), kept);
+  return true;
+}
+
 // A plan of one run that has all tokens that matter, `n` of them.
 __device__ __forceinline__ void plan_all(Waves& waves, uint32_t n, int last) {
   if (threadIdx.x) return;
@@ -1089,7 +1227,11 @@ struct alignas(256) State {
   Head head;
   u64 weight[kMostRuns + 1];
   uint32_t listed, arrived;
-  u64 list[kList];
+  union {
+    u64 list[kList];
+    struct { uint32_t count[kBins], least[kBins]; };
+  };
+  uint32_t most[kBins];
 };
 struct alignas(256) Part {
   u64 best, high;  // `high` with flags above: a NaN, too many of a step
@@ -1280,14 +1422,16 @@ template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) r
   if (bounded || too_many) count_steps(waves, counts, row, steps, 0, a.columns, nan);
   plan_row(waves, counts, row.scale);
   if constexpr (SECOND) {
-    if (!waves.head.plan.slow) {
+    if (waves.head.plan.slow != kSlow) {
       gather_plan(waves.head.plan, lists, row, steps, 0, a.columns);
-      if (find<false>(a, r, row, waves, lists)) return;
+      if (waves.head.plan.slow ? find_equal(a, r, row, waves, lists) : find<false>(a, r, row, waves, lists)) return;
     }
     find_slowly(a, r, row, waves, lists);
   } else {
     if (tid == 0) waves.head.answered = 0, waves.head.top = high, state->listed = state->arrived = 0;
     if (tid <= kMostRuns) state->weight[tid] = 0;
+    if (waves.head.plan.slow)
+      for (int i = tid; i < kBins; i += kThreads) state->count[i] = state->most[i] = 0, state->least[i] = ~0u;
     __syncthreads();
     if (tid < kHeadWords) reinterpret_cast<uint32_t*>(&state->head)[tid] = reinterpret_cast<const uint32_t*>(&waves.head)[tid];
   }
@@ -1304,28 +1448,42 @@ template <typename T> __global__ void __launch_bounds__(kThreads) gather_kernel(
   if (tid < kHeadWords) reinterpret_cast<uint32_t*>(&waves.head)[tid] = reinterpret_cast<const uint32_t*>(&state->head)[tid];
   __syncthreads();
   const Row<T> row{static_cast<const T*>(a.logits) + r * a.stride, a.columns, a.log2_columns, {waves.head.top, waves.head.ask.factor}};
-  if (waves.head.plan.slow) {
+  const int slow = waves.head.plan.slow;
+  if (slow == kSlow) {
     if (piece) return;
   } else {
     int first, count;
     piece_of(a.columns, pieces, piece, first, count);
     gather_plan(waves.head.plan, lds, row, waves.head.steps, first, count);
-    const uint32_t listed = lds.listed;
-    if (tid == 0) lds.first = listed ? add_through(&state->listed, listed) : 0;
     if (tid <= kMostRuns && lds.weight[tid]) add_through(&state->weight[tid], lds.weight[tid]);
-    __syncthreads();
-    for (uint32_t i = tid; i < min(listed, (uint32_t)kList) && lds.first + i < kList; i += kThreads) write_through(&state->list[lds.first + i], lds.list[i]);
+    if (slow) {
+      for (int i = tid; i < kBins; i += kThreads) {
+        if (!lds.count[i]) continue;
+        add_through(&state->count[i], lds.count[i]);
+        __hip_atomic_fetch_min(&state->least[i], lds.least[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_fetch_max(&state->most[i], lds.most[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    } else {
+      const uint32_t listed = lds.listed;
+      if (tid == 0) lds.first = listed ? add_through(&state->listed, listed) : 0;
+      __syncthreads();
+      for (uint32_t i = tid; i < min(listed, (uint32_t)kList) && lds.first + i < kList; i += kThreads) write_through(&state->list[lds.first + i], lds.list[i]);
+    }
     if (!all_arrived(waves, &state->arrived, pieces)) return;
-    for (uint32_t i = tid; i < waves.head.plan.tokens; i += kThreads) lds.list[i] = read_through(&state->list[i]);
-    if (tid == 0) lds.listed = read_through(&state->listed);
     if (tid <= kMostRuns) lds.weight[tid] = read_through(&state->weight[tid]);
+    if (slow) {
+      for (int i = tid; i < kBins; i += kThreads) lds.count[i] = read_through(&state->count[i]), lds.least[i] = read_through(&state->least[i]), lds.most[i] = read_through(&state->most[i]);
+    } else {
+      for (uint32_t i = tid; i < waves.head.plan.tokens; i += kThreads) lds.list[i] = read_through(&state->list[i]);
+      if (tid == 0) lds.listed = read_through(&state->listed);
+    }
     __syncthreads();
-    if (find<false>(a, r, row, waves, lds)) return;
+    if (slow ? find_equal(a, r, row, waves, lds) : find<false>(a, r, row, waves, lds)) return;
   }
   find_slowly(a, r, row, waves, lds);
 }
 
-int64_t states_of(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(rows, kMostRows)); }
+int64_t states_of(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(rows, kSharedRows)); }
 
 template <typename T> void launch(const Args& a, int64_t rows, void* workspace, hipStream_t stream) {
   if (a.columns <= kList) {

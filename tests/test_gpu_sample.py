@@ -46,7 +46,7 @@ class Call:
         token, kept, probability = self.results()
         for r, (t, p, n) in enumerate(self.expected()):
             assert (token[r], kept[r]) == (t, n), f"row {r}: token {token[r]} of {kept[r]}, not {t} of {n}"
-            # one rounding to float, and weights off by 2^-40 of their size
+            # one rounding to float, and weights off by 2^-39 of their size
             assert probability[r] == pytest.approx(p, rel=2.0**-23, abs=1e-38, nan_ok=True), r
         return self
 
@@ -119,6 +119,42 @@ def test_few_different_scores(dtype):
     x = torch.randint(-3, 2, (16, 30000), generator=g).to(DTYPES[dtype]).cuda()
     Call(x, numbers(12, 16), temperature=[1.0, 0.5] * 8, top_k=[0, 8000, 0, 12345] * 4, top_p=[0.7, 0.9, 1.0, 0.37] * 4, min_p=[0.0, 0.0, 0.1, 0.0] * 4).check()
     Call(torch.where(x == 0, -0.0, x.float()).to(DTYPES[dtype]).contiguous(), numbers(13, 16), top_k=[9000] * 16).check()  # (zeros of both signs are equal)
+
+
+@pytest.mark.parametrize("rows", [1, 12, 150])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mean", [10.0, -20.0, 0.0])
+def test_rounded_scores(mean, dtype, rows):
+    """Scores of bfloat16, some thousand of each (float32: the same numbers), far from zero and not; each place in the middle of equal ones."""
+    print("rounded", mean, dtype, rows, flush=True)
+    few = (torch.arange(rows) % 12).tolist()
+    how = dict(temperature=[1.0, 0.7, 1.0, 1.0, 2.0, 1.0], top_k=[0, 0, 20000, 0, 9000, 3000], top_p=[0.9, 0.95, 1.0, 1.0, 0.9, 0.99], min_p=[0.0, 0.0, 0.0, 0.01, 0.001, 0.0])
+    x = (scores(6, 12, 131072, peak=0.0) + mean).bfloat16().to(DTYPES[dtype])[few].contiguous()
+    c = Call(x, [numbers(8, 12)[i] for i in few], **{name: [v[i % 6] for i in few] for name, v in how.items()})
+    if rows <= 12:
+        c.check()
+        return
+    c.call()
+    token, kept, _ = c.results()
+    want = Call(x[:12], numbers(8, 12), **{name: v * 2 for name, v in how.items()}).expected()
+    assert list(zip(token, kept)) == [(want[i][0], want[i][2]) for i in few]
+
+
+@pytest.mark.parametrize("rows", [1, 12, 130])
+def test_thousands_next_to_each_other(rows):
+    """More tokens than are sorted at once within a step, all different: a long row's scores from 1 to 1.012, and one far away."""
+    print("next to each other", rows, flush=True)
+    columns = 70000
+    x = 1 + torch.randperm(columns, generator=torch.Generator().manual_seed(3)).float() * 2.0**-23
+    x[777] = -40.0
+    few = (torch.arange(rows) % 12).tolist()
+    how = dict(top_k=[0, 0, 33333, 0], top_p=[0.9, 0.3, 1.0, 1.0], min_p=[0.0, 0.0, 0.0, 0.995])
+    given = {name: [v[i % 4] for i in few] for name, v in how.items()}
+    c = Call(x.cuda().expand(rows, columns).contiguous(), [numbers(4, 12)[i] for i in few], **given)
+    c.call()
+    token, kept, _ = c.results()
+    want = Call(x.cuda().expand(12, columns).contiguous(), numbers(4, 12), **{name: v * 3 for name, v in how.items()}).expected()
+    assert list(zip(token, kept)) == [(want[i][0], want[i][2]) for i in few]
 
 
 def test_masked_scores():
