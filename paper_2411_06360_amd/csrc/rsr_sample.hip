@@ -37,7 +37,8 @@ constexpr int kSteps = 8 * kThreads;  // of counted scores; the first has what i
 constexpr int kPeaks = 2 * kThreads;  // scores above the steps
 constexpr int kBounded = 512;         // top_k up to here is looked up in one pass
 constexpr int kGroups = 256;          // workgroups of a launch: one for each CU
-constexpr int kLeastPiece = 8192;     // scores of a workgroup, where several have a row
+constexpr int kLeastPiece = 4096;     // scores of a workgroup, where several have a row
+constexpr int kFew = 1024;            // columns up to here are sorted whole
 constexpr int kMostRows = 1024;       // of a launch
 constexpr int kLeastCounted = 1 << 14, kFewestCounts = 4, kMostCounts = 8;  // the first pass: scores of a piece, and pieces of a row (or one)
 constexpr int kPrefix = 1024;        // tokens that are rather gathered from the first one on than counted
@@ -85,16 +86,25 @@ struct Steps {
 struct Run {
   int b0, b1;                     // steps
   uint32_t start, count, before;  // where it begins in the list, how many there are, and before them in the row
-  int shift;                      // how far apart its buckets are, for sorting
+  int shift;                      // how far apart its buckets are, for sorting; kEven: as many for each step
+  float from, each;               // for kEven: where it begins, and buckets of a step
   u64 code;                       // about that of the first
   double mass_before;             // the weight of those before
 
-  // as many buckets as tokens, or half as many, from one code to another
+  // As many buckets as tokens, or half as many, from one code to another.  Codes are dense where scores are near zero: if these lie on both
+  // sides of it, the buckets are even in the scores.
+  static constexpr int kEven = -1;
   __device__ __forceinline__ void span(u64 from, u64 to) {
     code = from;
     shift = max(0, __clz((int)count) + 33 - __clzll((long long)(to > from ? to - from : 1)));
   }
-  __device__ __forceinline__ uint32_t bucket(u64 x) const { return start + (x < code ? 0 : (uint32_t)min((x - code) >> shift, (u64)(count - 1))); }
+  __device__ __forceinline__ void span_even(float down_first, float down_last) {
+    shift = kEven, from = down_first, each = (float)count / (down_last - down_first);
+  }
+  __device__ __forceinline__ uint32_t bucket(u64 x, float down) const {
+    if (shift == kEven) return start + (uint32_t)__builtin_amdgcn_fmed3f((down - from) * each, 0.f, (float)(count - 1));
+    return start + (x < code ? 0 : (uint32_t)min((x - code) >> shift, (u64)(count - 1)));
+  }
 };
 
 // What the second pass has to do.
@@ -105,6 +115,7 @@ struct Plan {
   uint32_t tokens;  // of all runs
   uint32_t all;     // of the row
   int weighed;      // it adds up weights
+  int behind;       // the place of top_p is behind what min_p keeps
   int slow;         // kMany: too many tokens for the list; kSlow: too many above the steps, or no steps
 };
 constexpr int kMany = 1, kSlow = 2;
@@ -407,7 +418,7 @@ template <typename T> struct Row {
 
   // Sorts the list and adds up its weights.  Codes are dealt into buckets, as many for each run as it has tokens, and each finds its
   // place among those of its bucket.  (What lies outside the bounds of its run lands in a bucket at the end, still in order.)
-  __device__ __forceinline__ void sort(Waves& waves, Lists& lds, const Plan& plan) const {
+  __device__ __forceinline__ void sort(Waves& waves, Lists& lds, const Plan& plan, const Steps& steps) const {
     const int tid = threadIdx.x;
     const uint32_t n = plan.tokens;
     u64 x[2];
@@ -419,10 +430,11 @@ template <typename T> struct Row {
       const uint32_t i = tid + j * kThreads;
       if (i >= n) continue;
       x[j] = lds.list[i];
-      bucket[j] = plan.run[0].bucket(x[j]);
+      const float down = steps.down(score(x[j]));
+      bucket[j] = plan.run[0].bucket(x[j], down);
 #pragma unroll
       for (int k = 1; k < kMostRuns; ++k)
-        if (k < plan.n && x[j] >= plan.run[k].code) bucket[j] = plan.run[k].bucket(x[j]);
+        if (k < plan.n && x[j] >= plan.run[k].code) bucket[j] = plan.run[k].bucket(x[j], down);
       slot[j] = atomicAdd(&lds.part_count[bucket[j]], 1u);
     }
     __syncthreads();
@@ -483,7 +495,7 @@ template <typename T> struct Row {
       is_sure &= sure(lds, p, r, all);
       kept = ask.top_k, mass = mass_at(lds, r, at);
     }
-    if (ask.top_p < 1.0) {
+    if (ask.top_p < 1.0 && !plan.behind) {
       const At p = At::weight(ask.top_p * mass, false);
       const uint32_t at = seek(lds, plan, p, r), n = r.before + at - r.start + 1;
       is_sure &= sure(lds, p, r, all);
@@ -554,11 +566,11 @@ template <typename T> struct Row {
     Plan plan;
     plan.n = 1, plan.near = -1, plan.tokens = count;
     Run& r = plan.run[0];
-    r = {b, b, 0, count, before, 0, 0, mass_before};
+    r = {b, b, 0, count, before, 0, 0.f, 0.f, 0, mass_before};
     if (!lo && scale.top < INFINITY)  // (the bin's ends, or what is left of it)
       lo = code((float)((double)scale.top - b / (kPerOctave * scale.factor)), 0), hi = code((float)((double)scale.top - (b + 1) / (kPerOctave * scale.factor)), 0);
     r.span(lo, hi);
-    sort(waves, lds, plan);
+    sort(waves, lds, plan, waves.head.steps);
     return r;
   }
 
@@ -651,7 +663,7 @@ template <typename T> __device__ __forceinline__ void look(const Args& a, int64_
     const float mine = waves.high[lane & (kWaves - 1)];
     high = of_lane(largest_of_16(mine), 15);
     // above the first step are some hundred scores: those above the `rank`-th of the wavefronts' highest
-    const int rank = max(1, min(kWaves / 2, (kWaves / 2 << 17) / a.columns));
+    const int with = __popcll(__ballot(mine > -INFINITY) & 0xffff), rank = max(1, min(with / 2, (kWaves / 2 << 17) / a.columns));
     int higher = 0;
     for (int w = 0; w < kWaves; ++w) {
       const float other = of_lane(mine, w);
@@ -660,7 +672,8 @@ template <typename T> __device__ __forceinline__ void look(const Args& a, int64_
     const float from = of_lane(mine, __builtin_ctzll(__ballot(higher == rank - 1)));
     Steps steps{-FLT_MAX, -FLT_MAX / 2, 1.f};
     if (from > -INFINITY) {
-      const double range = fmin((double)from - (double)low, 48.0 / ask.factor);
+      // (but no finer than 2^-33 of the scores, so that those above are some steps away and not infinitely many)
+      const double range = fmax(fmin((double)from - (double)low, 48.0 / ask.factor), fmax(fabs((double)from) * 0x1p-20, 1e-20));
       steps = {from, 0.5f * from, (float)fmin(2.0 * (kSteps - 3) / range, (double)FLT_MAX)};
     }
     float bound = NAN;
@@ -683,6 +696,11 @@ template <typename T> __device__ __forceinline__ void look(const Args& a, int64_
     } else if (ask.far < INFINITY && ask.top_p >= 1.0) {
       const float x = (float)fmax((double)high - ask.far / ask.factor, -(double)FLT_MAX);
       bound = high > -INFINITY ? fmaxf(steps.down(x), 0.f) + 1.f : NAN;
+      // Not if it leaves sixteen thousand tokens or more, as the share of the looked at pieces with such a score says.
+      const float share = (float)(8 * kList) / (float)a.columns;
+      int n = 0;
+      for (int j = 0; j < kThreads / 64; ++j) n += __popcll(__ballot(steps.down(lds.looked[j * 64 + lane]) <= bound));
+      if (share < 1.f && (float)n > (float)looked * (1.f - __builtin_amdgcn_exp2f(kWide * __builtin_amdgcn_logf(1.f - share)))) bound = NAN;
     }
     if (lane == 0) waves.head.ask = ask, waves.head.steps = steps, lds.bound = bound;
   }
@@ -758,7 +776,7 @@ template <typename T> __device__ __forceinline__ float count_steps(Waves& waves,
 // squares of that; four and a half times as much is allowed for.  (Whether that was enough is seen in the end.)
 __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale& scale) {
   constexpr int kEach = kSteps / kThreads;
-  constexpr float kRounded = 1e-5f;  // of a sum: what weights are rounded by here, and more
+  constexpr float kRounded = 2e-6f;  // of a sum: what some twenty roundings come to, and more
   static_assert(kEach == 8);
   typedef Place<float> About;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -830,7 +848,8 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
   __syncthreads();
   const uint32_t all = lds.all_count;
   const float total = lds.all_mass;
-  const float off = 0.9004245f * octaves * sqrtf(of_lane(sum_of_16(waves.high[lane & 15]), 15)) + kRounded * total;  // (4.5 ln 2 / sqrt 12)
+  const float off = 0.9004245f * octaves * sqrtf(of_lane(sum_of_16(waves.high[lane & 15]), 15)) + kRounded * total +  // (4.5 ln 2 / sqrt 12)
+                    weight_of(lds.steps[kSteps - 2], kSteps - 2);  // (what is below all that were looked at may have no weight at all)
   const bool k = ask.top_k && ask.top_k < all, p = ask.top_p < 1.0;
   mark(0, About::tokens(all));
   if (k) mark(1, About::tokens(ask.top_k));
@@ -857,6 +876,7 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
     lo[1] = a.bin, before[1] = a.before, hi[1] = end.bin, upto[1] = end.count;
     least = fminf(least, a.mass_before - off), most = fminf(most, end.mass + off);
   }
+  const Mark weight_end = end;
   const bool m = far && lds.mark[4].bin <= end.bin;
   if (m) {
     const Mark a = lds.mark[4];
@@ -865,13 +885,15 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
     least = fminf(least, a.mass_before - off), most = fminf(most, end.mass + off);
   }
   const int near = m ? end.bin : -1;
-  const Mark last = all <= kList ? lds.mark[0] : k ? lds.mark[1] : end;  // (the weight of the first top_k is asked for)
-  const bool prefix = last.count <= kPrefix || all <= kList;
+  const bool behind = m && p && end.bin < lo[1];
+  if (behind) lo[1] = hi[1] = kSteps, before[1] = upto[1] = 0;
+  const Mark last = k ? lds.mark[1] : p && !behind ? weight_end : end;  // (the weight of the first top_k is asked for, and top_p's place looked up)
+  const bool prefix = last.count <= kPrefix;
   if (!prefix) mark(6, About::weight((float)ask.u * least - off, true)), mark(7, About::weight((float)ask.u * most + off, true));
   __syncthreads();
   if (wave == 0) {
     Plan plan;
-    plan.near = near, plan.all = all;
+    plan.near = near, plan.all = all, plan.behind = behind;
     if (prefix) {
       lo[0] = 0, hi[0] = last.bin, before[0] = 0, upto[0] = last.count;
 #pragma unroll
@@ -911,7 +933,7 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
 #pragma unroll
     for (int i = 0; i < kMostRuns; ++i) {
       const bool there = lo[i] < kSteps;
-      plan.run[i] = {lo[i], hi[i], plan.tokens, there ? upto[i] - before[i] : 0, before[i], 0, 0, 0.0};
+      plan.run[i] = {lo[i], hi[i], plan.tokens, there ? upto[i] - before[i] : 0, before[i], 0, 0.f, 0.f, 0, 0.0};
       plan.tokens += plan.run[i].count, plan.n += there;
     }
     plan.slow = plan.tokens > kList ? kMany : 0;
@@ -1051,11 +1073,15 @@ template <bool SPANNED, typename T> __device__ __forceinline__ bool find(const A
   if (!SPANNED && tid < kMostRuns) {
     Run run = plan.run[tid];
     run.mass_before = plan.weighed ? (double)lds.weight[tid] * 0x1p-40 : 0.0;
-    if (tid < plan.n) run.span(row.code(run.b0 ? steps.score(run.b0 - 1) : row.scale.top, 0), row.code(steps.score(min(run.b1, kSteps - 2)), row.columns - 1));
+    if (tid < plan.n) {
+      const float first = run.b0 ? steps.score(run.b0 - 1) : row.scale.top, last = steps.score(min(run.b1, kSteps - 2));
+      run.span(row.code(first, 0), row.code(last, row.columns - 1));
+      if (first > 0.f && last < 0.f) run.span_even(steps.down(first), steps.down(last));
+    }
     plan.run[tid] = run;
   }
   __syncthreads();
-  row.sort(waves, lds, plan);
+  row.sort(waves, lds, plan, steps);
   if (tid < 64) {
     const Found f = row.solve(lds, waves.head.ask, plan, plan.all, plan.weighed ? (double)lds.weight[kMostRuns] * 0x1p-40 : lds.upto[plan.tokens - 1]);
     if (f.sure) answer(a, r, row.column(f.code), (float)f.share, f.kept);
@@ -1130,7 +1156,7 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
       seek(At::tokens(ask.top_k));
       kept = ask.top_k, mass = upto;
     }
-    if (ask.top_p < 1.0) {
+    if (ask.top_p < 1.0 && !plan.behind) {
       seek(At::weight(ask.top_p * mass, false));
       if (count < kept) kept = count, mass = upto;
     }
@@ -1186,8 +1212,8 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
 __device__ __forceinline__ void plan_all(Waves& waves, uint32_t n, int last) {
   if (threadIdx.x) return;
   Plan& plan = waves.head.plan;
-  plan.run[0] = {0, last, 0, n, 0, 0, 0, 0.0};
-  plan.n = 1, plan.near = waves.head.ask.far < INFINITY ? 0 : -1, plan.tokens = plan.all = n, plan.weighed = plan.slow = 0;
+  plan.run[0] = {0, last, 0, n, 0, 0, 0.f, 0.f, 0, 0.0};
+  plan.n = 1, plan.near = waves.head.ask.far < INFINITY ? 0 : -1, plan.tokens = plan.all = n, plan.weighed = plan.behind = plan.slow = 0;
 }
 
 template <typename T> __device__ __forceinline__ void find_slowly(const Args& a, int64_t r, const Row<T>& row, Waves& waves, Lists& lds) {
@@ -1274,7 +1300,11 @@ template <typename T> __global__ void __launch_bounds__(kThreads) few_kernel(Arg
   row.scale = {row.score(best), waves.head.ask.factor};
   const uint32_t n = row.gather(lds, [&](float, int) { return true; });
   plan_all(waves, n, kSteps);
-  if (threadIdx.x == 0) waves.head.plan.run[0].span(best, row.code(low, a.columns - 1));
+  if (threadIdx.x == 0) {
+    const float top = row.scale.top;
+    waves.head.plan.run[0].span(best, row.code(low, a.columns - 1)), waves.head.steps = {top, 0.5f * top, 1.f};
+    if (top > 0.f && low < 0.f && top < INFINITY) waves.head.plan.run[0].span_even(0.f, waves.head.steps.down(low));
+  }
   __syncthreads();
   find<true>(a, r, row, waves, lds);
 }
@@ -1486,7 +1516,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) gather_kernel(
 int64_t states_of(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(rows, kSharedRows)); }
 
 template <typename T> void launch(const Args& a, int64_t rows, void* workspace, hipStream_t stream) {
-  if (a.columns <= kList) {
+  if (a.columns <= kFew) {
     hipLaunchKernelGGL(few_kernel<T>, dim3((unsigned)rows), dim3(kThreads), 0, stream, a);
     return;
   }

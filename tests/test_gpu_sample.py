@@ -157,6 +157,20 @@ def test_thousands_next_to_each_other(rows):
     assert list(zip(token, kept)) == [(want[i][0], want[i][2]) for i in few]
 
 
+@pytest.mark.parametrize("seed", range(32))
+def test_parameters_together(seed):
+    """Whatever comes together: narrow and wide scores around zero and not, peaks, masks, with every parameter."""
+    rng = np.random.default_rng(seed)
+    columns, rows = int(rng.choice([1025, 1500, 5000, 50021, 131072, 152064])), int(rng.choice([1, 3, 9]))
+    dtype, mean, spread, peak = rng.choice(["f32", "f32", "f16", "bf16"]), rng.choice([0, 0, 5, -10, 20]), rng.choice([0.01, 0.3, 2, 4]), rng.choice([0, 4, 12])
+    print("together", seed, columns, rows, dtype, mean, spread, peak, flush=True)
+    x = (scores(seed, rows, columns, spread=float(spread), peak=float(peak), few=64) + float(mean)).to(DTYPES[dtype])
+    if seed % 4 == 0:
+        x[:, rng.random(columns) < 0.5] = -math.inf
+    how = dict(temperature=[0.3, 0.7, 1.0, 1.5, 3.0], top_k=[0, 0, 20, 1000, 5000], top_p=[1.0, 0.5, 0.9, 0.99, 0.999], min_p=[0.0, 0.0, 0.001, 0.05, 0.2])
+    Call(x, numbers(seed, rows), **{name: rng.choice(v, rows).tolist() for name, v in how.items()}).check()
+
+
 def test_masked_scores():
     x = scores(21, 12, 5000)
     x[0:8, ::2] = -math.inf
