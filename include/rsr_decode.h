@@ -50,8 +50,8 @@ typedef struct rsr_rotary_t {
  *   y = x * weight / sqrt(mean(x^2) + eps)     (or y = x)
  *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),   t = position[row] * frequency[j], for pair j = (a, b)
  * in 32 bits, with one rounding at the end to the type of the result.  (Where squares leave the range of float their mean is taken in 64
- * bits.)  The angle's whole turns are taken off in 64 bits, with what those lose: a far position is rotated as exactly as a near one.  A value that is not finite touches its own
- * head alone (its pair, without a norm).  A head of zeros with eps 0 is not finite.
+ * bits.)  The angle's whole turns are taken off in 64 bits, with what those lose: a far position is rotated as exactly as a near one.
+ * A value that is not finite touches its own head alone (its pair, without a norm).  A head of zeros with eps 0 is not finite.
  *
  *   q, k         DEVICE, row t at q + t * q_stride elements: [heads][head_dim], k: [kv_heads][head_dim]
  *   dtype        of q and k: RSR_F32, RSR_F16 or RSR_BF16
@@ -94,8 +94,9 @@ int rsr_head_rotate(const rsr_rotary_t *rotary, const void *q, int64_t q_stride,
  * A score of minus infinity is no token's: it is never chosen and not counted.  A row without another score has token -1,
  * probability 0 and kept 0; a row with NaN has token -1, probability NaN and kept 0.  With scores of plus infinity only these
  * tokens have weight, all the same.
- * Weights and sums are held in 64 bits, off by some 2^-40: a border of a sum falls between the tokens between which it falls exactly unless it is that
- * near to one.  A row's results depend on its own scores and parameters alone, bit for bit.
+ * Weights and sums are held in 64 bits, off by some 2^-39 (2^-34 of each weight where thousands of different scores lie next to each other): a border of
+ * a sum falls between the tokens between which it falls exactly unless it is that near to one.  A row's results depend on nothing but its own scores and
+ * parameters, and in their last bits on where in 16 bytes it begins; not on other rows, nor on the order in which workgroups come.
  * Errors: RSR_ERR_INVALID_ARGUMENT, RSR_ERR_HIP (launch failure).
  */
 int64_t rsr_sample_workspace(int64_t rows, int64_t columns); /* bytes, or a negative status; HOST only */

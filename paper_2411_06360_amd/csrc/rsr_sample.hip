@@ -8,11 +8,20 @@
 // times the weights of the steps' middles tell every sum of weights to some hundredths of a percent, and so in which steps the places are.  A
 // second pass adds up what lies before these, in 64 bits, and gathers what is in them.  It computes a weight for every score, which
 // takes longer than reading it, and several workgroups share it.
-//   If too many tokens are there (thousands of equal scores, say) the slow way is taken: a histogram with count and weight of each bin, 2048
+//   If too many tokens are there, they are most often equal (16-bit scores far from zero): then the second pass counts them in parts of the steps, and
+// a place is a number among equal ones.  If that does not hold either the slow way is taken: a histogram with count and weight of each bin, 2048
 // bins of 1/32 of an octave of weight, and place after place with finer ones of what is left.
 //
-// A row is one workgroup's, of sixteen wavefronts: what all of them compute alike costs four times what one of them takes, so one
-// alone plans and finds, and the others wait.
+// Where there are as many rows as CUs a row is one workgroup's, of sixteen wavefronts; few long rows are shared by several, in either pass, and
+// the last one that comes goes on.  What all sixteen compute alike costs four times what one of them takes, so one alone plans and finds, and the
+// others wait.  Every function is part of its kernel: a single call anywhere gives every launch a stack, which takes 1 to 8 us more (256 rows of 131072 with
+// top_k 50 52 us, and 46 so).
+//
+// What bounds it: with few rows the steps behind each other.  16 rows of 131072 with top_p 0.9, 39 us from call to call: a look 2.4, counts of 16384 scores 4.1,
+// handing them on and adding them up 7.5, the plan 4.9, until the second launch is at work 2.7, weights of 8192 scores 5.3, handing on 5, sorting 2.8, finding 1.4.
+// With many rows the second pass, some 14 operations in 64 bits for a score: 256 rows, 98 us, of which 22 are for counting and 40 for weighing, where
+// reading all scores twice from memory takes 53.  Other figures: one row of 131072 33 us; with top_k 50 one row takes 20, 16 rows 23, 256 rows 52; the highest
+// score of each of 256 rows 32; 256 rows that all ask for something else 88.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -35,13 +44,20 @@ constexpr int kPerOctave = 32;       // bins
 constexpr int kList = 2 * kThreads;  // tokens that are sorted at once
 constexpr int kSteps = 8 * kThreads;  // of counted scores; the first has what is above all others
 constexpr int kPeaks = 2 * kThreads;  // scores above the steps
-constexpr int kBounded = 512;         // top_k up to here is looked up in one pass
+// top_k up to here is looked up in one pass: 16 rows of 131072 take 23 us with top_k 50 (counted in steps: 34), 25 with 512 (34), 55 with 900 (35); 256
+// rows 52 (72), 73 (72), 102 (73).
+constexpr int kBounded = 512;
 constexpr int kGroups = 256;          // workgroups of a launch: one for each CU
-constexpr int kLeastPiece = 4096;     // scores of a workgroup, where several have a row
-constexpr int kFew = 1024;            // columns up to here are sorted whole
+// Scores of a workgroup at least, where several have a row.  The second pass: one row of 131072 takes 32.7 us, with 8192 33.6, with 16384 36.1.
+constexpr int kLeastPiece = 4096;
+// Columns up to here are sorted whole: 1000 take 10 us.  (2048 would take 22, and 18 with steps.)
+constexpr int kFew = 1024;
 constexpr int kMostRows = 1024;       // of a launch
-constexpr int kLeastCounted = 1 << 14, kFewestCounts = 4, kMostCounts = 8;  // the first pass: scores of a piece, and pieces of a row (or one)
-constexpr int kPrefix = 1024;        // tokens that are rather gathered from the first one on than counted
+// The first pass hands 16 KB of counts on for each piece: four to eight pieces or one.  16 rows of 131072 take 39 us (in one piece 46; one row in 8, 16 or 64
+// 33.2, 34.8, 34.9), 32768 scores in two pieces 29.7 us (in one 27.3), 128 rows of 131072 in two 72.3 (70.7).
+constexpr int kLeastCounted = 1 << 14, kFewestCounts = 4, kMostCounts = 8;
+// Tokens that are rather gathered from the first one on than counted: 256 rows of 131072 with top_k 900 take 73 us (with a prefix of 64: 98).
+constexpr int kPrefix = 1024;
 
 // What a bin adds up in one word: for each token a one above, and below how much less than the bin's most its weight is, in units of
 // 2^-34 of that.  A bin is 1/46 of its most wide at least (2^(1/32)): below 2^29 of them, and 2^17 tokens fit.
@@ -522,7 +538,7 @@ template <typename T> struct Row {
 
   // ---- place after place (a list for each), where there are too many tokens for one list
   // The run of tokens in which the place is.
-  __device__ __attribute__((noinline)) Run run_at(Waves& waves, Lists& lds, const At& p) const {
+  __device__ __forceinline__ Run run_at(Waves& waves, Lists& lds, const At& p) const {
     const int tid = threadIdx.x;
     int b = first_at(p, lds.count, lds.mass, kBins);
     while (b && lds.count[b] == lds.count[b - 1]) --b;  // (what rounding puts behind the last token is the last token's)
@@ -574,7 +590,7 @@ template <typename T> struct Row {
     return r;
   }
 
-  __device__ __attribute__((noinline)) Found solve_slowly(Waves& waves, Lists& lds, const Ask& ask) const {
+  __device__ __forceinline__ Found solve_slowly(Waves& waves, Lists& lds, const Ask& ask) const {
     uint32_t kept = lds.count[kBins - 1];
     double mass = lds.mass[kBins - 1];
     Plan plan{};
@@ -970,7 +986,8 @@ template <int RUNS, bool EQUAL, typename T> __device__ __forceinline__ void gath
     for (int i = 0; i < kRuns; ++i) in |= down >= lo[i] && down <= hi[i];
     return in;
   };
-  for_pieces(row.row, first, count, [&](const float (&x)[kWide], int column) {
+  // (8 at once where registers would not do for 16)
+  for_pieces<EQUAL || (RUNS == 4 && sizeof(T) == 2) ? 8 : 16>(row.row, first, count, [&](const float (&x)[kWide], int column) {
     bool some = false;
 #pragma unroll
     for (int j = 0; j < kWide; ++j) {
