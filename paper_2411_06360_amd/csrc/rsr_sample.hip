@@ -260,10 +260,24 @@ template <int SCORES = 16, typename T, typename F> __device__ __forceinline__ vo
 }
 // f(score, column) for each score.
 template <typename T, typename F> __device__ __forceinline__ void for_each(const T* row, int first, int count, F f) {
-  for_pieces(row, first, count, [&](const float (&x)[16 / sizeof(T)], int column) {
+  for_pieces<8>(row, first, count, [&](const float (&x)[16 / sizeof(T)], int column) {
 #pragma unroll
     for (int j = 0; j < 16 / (int)sizeof(T); ++j) f(x[j], column + j);
   });
+}
+
+// The same in any order, score by score, with little code: for what is seldom or little to do.
+template <int AT_ONCE = 2, typename T, typename F> __device__ __forceinline__ void for_each_seldom(const T* row, int first, int count, F f) {
+  typedef const __attribute__((address_space(1))) T* Scores;
+  const Scores from = (Scores)(row + first);
+  for (int i0 = threadIdx.x; i0 < count; i0 += AT_ONCE * kThreads) {
+    T x[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) x[j] = from[min(i0 + j * kThreads, count - 1)];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j)
+      if (i0 + j * kThreads < count) f((float)x[j], first + i0 + j * kThreads);
+  }
 }
 
 // ---- weights ----------------------------------------------------------------------------------------------
@@ -421,7 +435,7 @@ template <typename T> struct Row {
     __syncthreads();
     if (threadIdx.x == 0) lds.listed = 0;
     __syncthreads();
-    for_each(row, 0, columns, [&](float x, int column) {
+    for_each_seldom(row, 0, columns, [&](float x, int column) {
       if (x == -INFINITY || !wanted(x, column)) return;
       const uint32_t at = atomicAdd(&lds.listed, 1u);
       if (at < kList) lds.list[at] = code(x, column);
@@ -550,7 +564,7 @@ template <typename T> struct Row {
         __syncthreads();
         lds.part_sum[2 * tid] = lds.part_sum[2 * tid + 1] = 0;
         __syncthreads();
-        for_each(row, first, min(kChunk, columns - first), [&](float x, int column) {
+        for_each_seldom(row, first, min(kChunk, columns - first), [&](float x, int column) {
           if (x == -INFINITY) return;
           const double d = scale.distance(x);
           const u64 c = code(x, column);
@@ -593,45 +607,43 @@ template <typename T> struct Row {
     double mass = lds.mass[kBins - 1];
     Plan plan{};
     Run r;
-    uint32_t at;
-    auto find = [&](const At& p) {
+    uint32_t at = 0;
+    // top_k's place, top_p's, and the token's: a loop, for one copy of the code
+#pragma unroll 1
+    for (int place = 0; place < 3; ++place) {
+      if (place == 0 && !(ask.top_k && ask.top_k < kept)) continue;
+      if (place == 1 && !(ask.top_p < 1.0)) continue;
+      if (place == 2 && ask.far < INFINITY) {
+        const int b = bin_of(ask.far);
+        const uint32_t before = b ? lds.count[b - 1] : 0;
+        if (before < kept) {
+          // (a count and a sum over all that is near enough in its bin)
+          double sum = 0.0;
+          uint32_t n = 0;
+          for (int first = 0; first < columns; first += kChunk) {
+            __syncthreads();
+            if (threadIdx.x == 0) lds.part_sum[0] = 0;
+            __syncthreads();
+            for_each_seldom(row, first, min(kChunk, columns - first), [&](float x, int) {
+              if (x == -INFINITY) return;
+              const double d = scale.distance(x);
+              if (d <= ask.far && bin_of(d) == b) atomicAdd(&lds.part_sum[0], packed(d, b));
+            });
+            __syncthreads();
+            n += count_in(lds.part_sum[0]), sum += mass_in(lds.part_sum[0], b);
+          }
+          if (before + n < kept) kept = before + n, mass = (b ? lds.mass[b - 1] : 0.0) + sum;
+        }
+      }
+      const At p = place == 0 ? At::tokens(ask.top_k) : place == 1 ? At::weight(ask.top_p * mass, false) : At::weight(ask.u * mass, true);
       const Run& have = plan.run[0];
       const bool here = plan.n && !p.reached(have.before, have.mass_before) && p.reached(have.before + have.count, mass_at(lds, have, have.count - 1));
       if (!here) plan.run[0] = run_at(waves, lds, p), plan.n = 1;
       at = seek(lds, plan, p, r);
-    };
-    if (ask.top_k && ask.top_k < kept) {
-      find(At::tokens(ask.top_k));
-      kept = ask.top_k, mass = mass_at(lds, r, at);
-    }
-    if (ask.top_p < 1.0) {
-      find(At::weight(ask.top_p * mass, false));
+      if (place == 0) kept = ask.top_k, mass = mass_at(lds, r, at);
       const uint32_t n = r.before + at + 1;
-      if (n < kept) kept = n, mass = mass_at(lds, r, at);
+      if (place == 1 && n < kept) kept = n, mass = mass_at(lds, r, at);
     }
-    if (ask.far < INFINITY) {
-      const int b = bin_of(ask.far);
-      const uint32_t before = b ? lds.count[b - 1] : 0;
-      if (before < kept) {
-        // (a count and a sum over all that is near enough in its bin)
-        double sum = 0.0;
-        uint32_t n = 0;
-        for (int first = 0; first < columns; first += kChunk) {
-          __syncthreads();
-          if (threadIdx.x == 0) lds.part_sum[0] = 0;
-          __syncthreads();
-          for_each(row, first, min(kChunk, columns - first), [&](float x, int) {
-            if (x == -INFINITY) return;
-            const double d = scale.distance(x);
-            if (d <= ask.far && bin_of(d) == b) atomicAdd(&lds.part_sum[0], packed(d, b));
-          });
-          __syncthreads();
-          n += count_in(lds.part_sum[0]), sum += mass_in(lds.part_sum[0], b);
-        }
-        if (before + n < kept) kept = before + n, mass = (b ? lds.mass[b - 1] : 0.0) + sum;
-      }
-    }
-    find(At::weight(ask.u * mass, true));
     return {lds.list[at], scale.weight(score(lds.list[at])) / mass, kept, true};
   }
 };
@@ -728,7 +740,7 @@ template <typename T> __device__ __forceinline__ float gather_above(Waves& waves
   if (tid == 0) lds.listed = 0;
   __syncthreads();
   float high = -INFINITY;
-  for_pieces<32>(row.row, first, count, [&](const float (&x)[kWide], int column) {
+  for_pieces<sizeof(T) == 2 ? 8 : 16>(row.row, first, count, [&](const float (&x)[kWide], int column) {
     bool some = false;
 #pragma unroll
     for (int j = 0; j < kWide; ++j) {
@@ -758,7 +770,7 @@ template <typename T> __device__ __forceinline__ float count_steps(Waves& waves,
   if (tid == 0) lds.listed = 0;
   __syncthreads();
   float high = -INFINITY;
-  for_pieces(row.row, first, count, [&](const float (&x)[kWide], int) {
+  for_pieces<8>(row.row, first, count, [&](const float (&x)[kWide], int) {
     float least = 0.f;
 #pragma unroll
     for (int j = 0; j < kWide; ++j) {
@@ -984,8 +996,8 @@ template <int RUNS, bool EQUAL, typename T> __device__ __forceinline__ void gath
     for (int i = 0; i < kRuns; ++i) in |= down >= lo[i] && down <= hi[i];
     return in;
   };
-  // (8 at once where registers would not do for 16)
-  for_pieces<EQUAL || (RUNS == 4 && sizeof(T) == 2) ? 8 : 16>(row.row, first, count, [&](const float (&x)[kWide], int column) {
+  // (Few on their way are enough where each is weighed; more would take more registers, and code than a kernel may have.)
+  for_pieces<RUNS == 4 ? kWide : RUNS || sizeof(T) == 2 ? 8 : 16>(row.row, first, count, [&](const float (&x)[kWide], int column) {
     bool some = false;
 #pragma unroll
     for (int j = 0; j < kWide; ++j) {
@@ -1031,10 +1043,10 @@ template <int RUNS, bool EQUAL, typename T> __device__ __forceinline__ void gath
 }
 
 template <typename T> __device__ __forceinline__ void gather_plan(const Plan& plan, Lists& lds, const Row<T>& row, const Steps& steps, int first, int count) {
-  if (plan.slow) plan.n <= 2 ? gather_runs<2, true>(plan, lds, row, steps, first, count) : gather_runs<4, true>(plan, lds, row, steps, first, count);
+  if (plan.slow) gather_runs<4, true>(plan, lds, row, steps, first, count);
   else if (!plan.weighed) gather_runs<0, false>(plan, lds, row, steps, first, count);
-  else if (plan.n == 1) gather_runs<1, false>(plan, lds, row, steps, first, count);
-  else if (plan.n == 2) gather_runs<2, false>(plan, lds, row, steps, first, count);
+  else if (plan.n == 1 && sizeof(T) == 4) gather_runs<sizeof(T) == 4 ? 1 : 2, false>(plan, lds, row, steps, first, count);  // (16-bit scores: no room for its code)
+  else if (plan.n <= 2) gather_runs<2, false>(plan, lds, row, steps, first, count);
   else gather_runs<4, false>(plan, lds, row, steps, first, count);
 }
 
@@ -1167,21 +1179,21 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
       nth = min(max(p.of_count ? p.count - before : p.strict ? (uint32_t)floor(of) + 1 : (uint32_t)ceil(of), 1u), n);
       count = before + nth, upto = mass_before + nth * weight;
     };
-    if (ask.top_k && ask.top_k < kept) {
-      seek(At::tokens(ask.top_k));
-      kept = ask.top_k, mass = upto;
+    // top_k's place, top_p's, and the token's: a loop, for one copy of the code
+#pragma unroll 1
+    for (int place = 0; place < 3; ++place) {
+      if (place == 0 && !(ask.top_k && ask.top_k < kept)) continue;
+      if (place == 1 && !(ask.top_p < 1.0 && !plan.behind)) continue;
+      if (place == 2 && plan.near >= 0) {
+        const int last = (int)lds.first - 1;
+        const uint32_t n = last < 0 ? plan.run[near].before : counted(near, last), end = plan.run[near].before + plan.run[near].count;
+        is_sure &= n < end || end >= kept;
+        if (n < kept) kept = n, mass = last < 0 ? (double)lds.weight[near] * 0x1p-40 : weighed(near, last);
+      }
+      seek(place == 0 ? At::tokens(ask.top_k) : place == 1 ? At::weight(ask.top_p * mass, false) : At::weight(ask.u * mass, true));
+      if (place == 0) kept = ask.top_k, mass = upto;
+      if (place == 1 && count < kept) kept = count, mass = upto;
     }
-    if (ask.top_p < 1.0 && !plan.behind) {
-      seek(At::weight(ask.top_p * mass, false));
-      if (count < kept) kept = count, mass = upto;
-    }
-    if (plan.near >= 0) {
-      const int last = (int)lds.first - 1;
-      const uint32_t n = last < 0 ? plan.run[near].before : counted(near, last), end = plan.run[near].before + plan.run[near].count;
-      is_sure &= n < end || end >= kept;
-      if (n < kept) kept = n, mass = last < 0 ? (double)lds.weight[near] * 0x1p-40 : weighed(near, last);
-    }
-    seek(At::weight(ask.u * mass, true));
     if (tid == 0) waves.sure = is_sure, waves.count[0] = lds.least[part], waves.count[1] = nth, waves.count[2] = kept, waves.mass[0] = mass;
   }
   __syncthreads();
@@ -1195,7 +1207,7 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
   __syncthreads();
   lds.part_count[2 * tid] = lds.part_count[2 * tid + 1] = 0;
   __syncthreads();
-  for_each(row.row, 0, row.columns, [&](float y, int column) {
+  for_each_seldom<16>(row.row, 0, row.columns, [&](float y, int column) {
     if (y == x) atomicAdd(&lds.part_count[column >> shift], 1u);
   });
   __syncthreads();
@@ -1238,7 +1250,7 @@ template <typename T> __device__ __forceinline__ void find_slowly(const Args& a,
     __syncthreads();
     lds.sum[2 * tid] = lds.sum[2 * tid + 1] = 0;
     __syncthreads();
-    for_each(row.row, at, min(kChunk, a.columns - at), [&](float x, int) {
+    for_each_seldom(row.row, at, min(kChunk, a.columns - at), [&](float x, int) {
       if (x == -INFINITY) return;
       const double d = row.scale.distance(x);
       const int bin = bin_of(d);
@@ -1421,50 +1433,64 @@ template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) r
   bool nan = false, too_many = false;
   int first = 0, count = a.columns;
   if (!SECOND) piece_of(a.columns, pieces, piece, first, count);
+  bool shared = !SECOND && pieces > 1;
   u64 best = ~(u64)0;
-  float high = -INFINITY, bound = NAN;
+  float high = -INFINITY;
+  // A piece of the row is done: true if others go on.  What all have found is here then.
+  auto is_others = [&](bool counted) {
+    if (!shared) return false;
+    give(lists, counts, counted, best, high, nan, count, state, counter, parts + piece);
+    if (!all_arrived(waves, &counter->arrived, pieces)) return true;
+    take(waves, lists, counts, counted, best, high, nan, too_many, state, counter, parts, pieces);
+    shared = false, first = 0, count = a.columns;
+    return false;
+  };
+  if (!SECOND && !shared && tid == 0) state->head.answered = 1;
   if (greedy) {
     best = best_of(waves, row, first, count, high, nan);
     if (tid == 0) lists.listed = 0;
     __syncthreads();
-  } else {
-    look(a, r, row.row, temperature, waves, counts);
-    __syncthreads();
-    bound = counts.bound;
-    row.scale.factor = waves.head.ask.factor;
-  }
-  const Steps steps = waves.head.steps;
-  const bool bounded = bound == bound, counted = !greedy && !bounded;
-  if (bounded) high = gather_above(waves, lists, row, steps, first, count, bound, nan);
-  else if (counted) high = count_steps(waves, counts, row, steps, first, count, nan);
-  if (!SECOND && pieces > 1) {
-    give(lists, counts, counted, best, high, nan, count, state, counter, parts + piece);
-    if (!all_arrived(waves, &counter->arrived, pieces)) return;
-    take(waves, lists, counts, counted, best, high, nan, too_many, state, counter, parts, pieces);
-  }
-  if (!SECOND && tid == 0) state->head.answered = 1;
-  if (greedy) {
+    if (is_others(false)) return;
+    if (!SECOND && tid == 0) state->head.answered = 1;
     is_answered(a, r, row, best, nan, true);
     return;
   }
-  if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
-  row.scale.top = high;
-  if (bounded) {
+  look(a, r, row.row, temperature, waves, counts);
+  __syncthreads();
+  float bound = counts.bound;
+  row.scale.factor = waves.head.ask.factor;
+  const Steps steps = waves.head.steps;
+  if (bound == bound) {
     const uint32_t top_k = waves.head.ask.top_k;
-    if (lists.listed > kList && !(top_k && top_k <= kBounded)) {  // (min_p alone: with the highest score known the bound is what it has to be)
+#pragma unroll 1
+    for (int turn = 0;; ++turn) {
+      high = gather_above(waves, lists, row, steps, first, count, bound, nan);
+      if (is_others(false)) return;
+      if (turn || lists.listed <= kList || (top_k && top_k <= kBounded)) break;
+      // (min_p alone: with the highest score known the bound is what it has to be)
       bound = fmaxf(steps.down((float)fmax((double)high - waves.head.ask.far / row.scale.factor, -(double)FLT_MAX)), 0.f) + 1.f;
       __syncthreads();
-      gather_above(waves, lists, row, steps, 0, a.columns, bound, nan);
     }
+    if (!SECOND && tid == 0) state->head.answered = 1;
+    if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
     const uint32_t n = lists.listed;
     if (n && n <= kList && (n >= top_k || bound == INFINITY)) {
+      row.scale.top = high;
       plan_all(waves, n, bound < kSteps - 4 ? (int)bound : kSteps - 2);
       __syncthreads();
       if (find<false>(a, r, row, waves, lists)) return;
     }
     __syncthreads();
   }
-  if (bounded || too_many) count_steps(waves, counts, row, steps, 0, a.columns, nan);
+#pragma unroll 1
+  do {
+    high = count_steps(waves, counts, row, steps, first, count, nan);
+    too_many = false;
+    if (is_others(true)) return;
+  } while (too_many);
+  if (!SECOND && tid == 0) state->head.answered = 1;
+  if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
+  row.scale.top = high;
   plan_row(waves, counts, row.scale);
   if constexpr (SECOND) {
     if (waves.head.plan.slow != kSlow) {
