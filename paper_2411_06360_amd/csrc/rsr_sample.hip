@@ -15,13 +15,14 @@
 // Where there are as many rows as CUs a row is one workgroup's, of sixteen wavefronts; few long rows are shared by several, in either pass, and
 // the last one that comes goes on.  What all sixteen compute alike costs four times what one of them takes, so one alone plans and finds, and the
 // others wait.  Every function is part of its kernel: a single call anywhere gives every launch a stack, which takes 1 to 13 us more (256 rows of 131072 with
-// top_k 50 52 us, and 46 so; with min_p 0.1 72 and 60).
+// top_k 50 52 us, and 46 without it; with min_p 0.1 72 and 60).  There is one copy of each pass for that, and no more scores on their way than a pass needs: a kernel has to
+// stay below what a short branch reaches (42 and 52 us then).
 //
-// What bounds it: with few rows the steps behind each other.  16 rows of 131072 with top_p 0.9, 37.5 us from call to call: a look 2.2, counts of 16384 scores 4.3,
-// handing them on and adding them up 7.6, the plan 5.0, until the second launch is at work 2.4, weights of 8192 scores 4.9, handing on 3.6, sorting 2.5, finding 1.4.
-// With many rows the second pass, some 14 operations in 64 bits for a score: 256 rows, 95 us, of which 22 are for counting and 40 for weighing, where
-// reading all scores twice from memory takes 53.  Other figures: one row of 131072 32.5 us; with top_k 50 one row takes 20, 16 rows 23, 256 rows 46; the highest
-// score of each of 256 rows 31; 256 rows that all ask for something else 84.
+// What bounds it: with few rows the steps behind each other.  16 rows of 131072 with top_p 0.9, 37 us from call to call: a look 2.3, counts of 16384 scores 4.2,
+// handing them on and adding them up 7.3, the plan 4.8, until the second launch is at work 3.0, weights of 8192 scores 4.5, handing on 3.4, sorting 2.4, finding 1.4.
+// With many rows the second pass, some 14 operations in 64 bits for a score: 256 rows, 88 us, of which 20 are for counting and 40 for weighing, where
+// reading all scores twice from memory takes 53.  Other figures: one row of 131072 32 us; with top_k 50 one row takes 20, 16 rows 23, 256 rows 42; the highest
+// score of each of 256 rows 29; 256 rows that all ask for something else 82 to 84.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -44,17 +45,17 @@ constexpr int kPerOctave = 32;       // bins
 constexpr int kList = 2 * kThreads;  // tokens that are sorted at once
 constexpr int kSteps = 8 * kThreads;  // of counted scores; the first has what is above all others
 constexpr int kPeaks = 2 * kThreads;  // scores above the steps
-// top_k up to here is looked up in one pass: 16 rows of 131072 take 23 us with top_k 50 (counted in steps: 32), 26 with 512 (32), 53 with 900 (33); 256
-// rows 46 (67), 62 (67), 92 (68).
+// top_k up to here is looked up in one pass: 16 rows of 131072 take 23 us with top_k 50 (counted in steps: 32), 25 with 512 (32), 53 with 900 (32); 256
+// rows 42 (65), 56 (65), some 90 (65).
 constexpr int kBounded = 512;
 constexpr int kGroups = 256;          // workgroups of a launch: one for each CU
-// Scores of a workgroup at least, where several have a row.  The second pass: one row of 131072 takes 32.5 us, with 8192 33.4, with 16384 36.0.
+// Scores of a workgroup at least, where several have a row.  The second pass: one row of 131072 takes 32 us, with 8192 a microsecond more, with 16384 four.
 constexpr int kLeastPiece = 4096;
 constexpr int kMostRows = 1024;       // of a launch
-// The first pass hands 16 KB of counts on for each piece: four to eight pieces or one.  16 rows of 131072 take 37.5 us (in one piece 46; one row in eight
-// pieces 32.5, in one 41.3, in 16 or 64 a microsecond more), 32768 scores in two pieces 30.7 us (in one 28.4), 128 rows of 131072 in two 72 (69.5).
+// The first pass hands 16 KB of counts on for each piece: four to eight pieces or one.  16 rows of 131072 take 37 us (in one piece 46; one row in eight
+// pieces 32, in one 41, in 16 or 64 a microsecond more), 32768 scores in two pieces 30.7 us (in one 28.4), 128 rows of 131072 in two 72 (69.5).
 constexpr int kLeastCounted = 1 << 14, kFewestCounts = 4, kMostCounts = 8;
-// Tokens that are rather gathered from the first one on than counted: 256 rows of 131072 with top_k 900 take 68 us (with a prefix of 64: 95).
+// Tokens that are rather gathered from the first one on than counted: 256 rows of 131072 with top_k 900 take 65 us (with a prefix of 64 some 90).
 constexpr int kPrefix = 1024;
 
 // What a bin adds up in one word: for each token a one above, and below how much less than the bin's most its weight is, in units of
@@ -1312,7 +1313,7 @@ __device__ __forceinline__ bool all_arrived(Waves& waves, uint32_t* counter, uin
   return waves.arrived == workgroups - 1;
 }
 
-// Rows that fit in the list: sorted whole.  16 rows of 2048 take 11.3 us, with steps 16.7.
+// Rows that fit in the list: sorted whole.  16 rows of 2048 take 11 us, with steps 16.
 template <typename T> __global__ void __launch_bounds__(kThreads) few_kernel(Args a) {
   __shared__ Waves waves;
   __shared__ Lists lds;
