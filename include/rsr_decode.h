@@ -91,6 +91,7 @@ int rsr_head_rotate(const rsr_rotary_t *rotary, const void *q, int64_t q_stride,
  *   kept         DEVICE [rows] int32 out, or NULL
  *   workspace    DEVICE, rsr_sample_workspace bytes, 256-byte aligned, zero before its first use; calls leave it ready for the
  *                next one.  Calls that share it must not overlap.  More rows or columns never need fewer bytes.
+ * No output may overlap an input, the workspace or another output.
  * A score of minus infinity is no token's: it is never chosen and not counted.  A row without another score has token -1,
  * probability 0 and kept 0; a row with NaN has token -1, probability NaN and kept 0.  With scores of plus infinity only these
  * tokens have weight, all the same.

@@ -1597,6 +1597,14 @@ int rsr_sample(const void* logits, int64_t rows, int64_t columns, int64_t stride
   if (stride < columns) return set_error(RSR_ERR_INVALID_ARGUMENT, "a stride is shorter than a row");
   if (rows == 0) return RSR_OK;
   if (!logits || !uniform || !token) return set_error(RSR_ERR_INVALID_ARGUMENT, "null pointer");
+  const void* const outputs[] = {token, probability, kept};
+  const void* const inputs[] = {logits, temperature, top_k, top_p, min_p, uniform, workspace};
+  for (int i = 0; i < 3; ++i) {
+    bool twice = false;
+    for (const void* p : inputs) twice |= outputs[i] == p;
+    for (int j = 0; j < i; ++j) twice |= outputs[i] == outputs[j];
+    if (outputs[i] && twice) return set_error(RSR_ERR_INVALID_ARGUMENT, "an output must not be an input, the workspace or another output");
+  }
   if (!rsr_internal::aligned(logits, rsr_internal::size_of(dtype))) return set_error(RSR_ERR_INVALID_ARGUMENT, "logits must be aligned as their elements");
   if (!workspace || !rsr_internal::aligned(workspace, 256) || workspace_bytes < need)
     return set_error(RSR_ERR_INVALID_ARGUMENT, "the workspace is missing, too small or not 256-byte aligned");

@@ -69,6 +69,13 @@ def test_samples_that_are_refused(changes):
     assert sample(**changes) == INVALID and R.rsr_last_error()
 
 
+@pytest.mark.parametrize("output", ["token", "probability", "kept"])
+@pytest.mark.parametrize("other", ["logits", "temperature", "top_k", "top_p", "min_p", "uniform", "workspace", "token", "probability", "kept"])
+def test_samples_into_what_is_read_are_refused(output, other):
+    if output != other:
+        assert sample(**{output: 8 * AT, other: 8 * AT}) == INVALID and "output" in R.rsr_last_error()
+
+
 def test_a_workspace_for_more_rows_or_columns_is_not_smaller():
     sizes = {(r, c): R.rsr_sample_workspace(r, c) for r in (0, 1, 2, 3, 7, 64, 255, 256, 257, 5000, 1 << 24) for c in (1, 64, 1000, 4096, 50000, 1 << 17, 1 << 22)}
     for (r, c), n in sizes.items():
