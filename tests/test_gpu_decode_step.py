@@ -293,3 +293,27 @@ def test_a_row_by_many_workgroups(shape):
         assert call(top_k=torch.full((rows,), 7, dtype=torch.int32, device="cuda")) == ([-1] * rows, [0] * rows)
     x.fill_(-float("inf"))
     assert call() == ([-1] * rows, [0] * rows)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_more_rows_than_a_launch_has(dtype):
+    """The last rows of many, which several workgroups share again, begin anywhere; each as it is alone, and by the definition."""
+    rows, columns = 1030, 70001
+    print("rows beyond a launch", dtype, flush=True)
+    space = torch.zeros(R.rsr_sample_workspace(rows, columns), dtype=torch.uint8, device="cuda")
+    x, u, token, kept, how, _ = sampling(rows, columns, 21, space)
+    x = x.to(dtype)
+
+    def call(r0, r1):
+        R.rsr_sample(x[r0:r1], u[r0:r1], token[r0:r1], space, kept=kept[r0:r1], stream=torch.cuda.current_stream().cuda_stream, **{n: v[r0:r1] for n, v in how.items()})
+        torch.cuda.synchronize()
+        return token.tolist(), kept.tolist()
+
+    whole = call(0, rows)
+    for r in range(rows - 8, rows):
+        given = (float(how["temperature"][r]), int(how["top_k"][r]), float(how["top_p"][r]), float(how["min_p"][r]), float(u[r]))
+        assert (whole[0][r], whole[1][r]) == oracle.sample(x[r].double().cpu().numpy(), *given)[::2]
+    token.fill_(-7), kept.fill_(-7)
+    for r0 in range(0, rows, 103):
+        alone = call(r0, r0 + 103)
+    assert alone == whole
