@@ -134,6 +134,8 @@ struct Plan {
   int slow;         // kMany: too many tokens for the list; kSlow: too many above the steps, or no steps
 };
 constexpr int kMany = 1, kSlow = 2;
+// (Not 1, so that a workspace that was not cleared, whose rows are never planned, leads nowhere.)
+constexpr int32_t kPlanned = 0x706c616e;
 
 // What a row is asked for.
 struct Ask {
@@ -146,7 +148,7 @@ struct Ask {
 
 // What is known of a row before the second pass.
 struct Head {
-  int32_t answered;
+  int32_t planned;  // kPlanned: the second pass has something to do
   float top;
   Steps steps;
   Ask ask;
@@ -1446,13 +1448,13 @@ template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) r
     shared = false, first = 0, count = a.columns;
     return false;
   };
-  if (!SECOND && !shared && tid == 0) state->head.answered = 1;
+  if (!SECOND && !shared && tid == 0) state->head.planned = 0;
   if (greedy) {
     best = best_of(waves, row, first, count, high, nan);
     if (tid == 0) lists.listed = 0;
     __syncthreads();
     if (is_others(false)) return;
-    if (!SECOND && tid == 0) state->head.answered = 1;
+    if (!SECOND && tid == 0) state->head.planned = 0;
     is_answered(a, r, row, best, nan, true);
     return;
   }
@@ -1472,7 +1474,7 @@ template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) r
       bound = fmaxf(steps.down((float)fmax((double)high - waves.head.ask.far / row.scale.factor, -(double)FLT_MAX)), 0.f) + 1.f;
       __syncthreads();
     }
-    if (!SECOND && tid == 0) state->head.answered = 1;
+    if (!SECOND && tid == 0) state->head.planned = 0;
     if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
     const uint32_t n = lists.listed;
     if (n && n <= kList && (n >= top_k || bound == INFINITY)) {
@@ -1489,7 +1491,7 @@ template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) r
     too_many = false;
     if (is_others(true)) return;
   } while (too_many);
-  if (!SECOND && tid == 0) state->head.answered = 1;
+  if (!SECOND && tid == 0) state->head.planned = 0;
   if (is_answered(a, r, row, high > -INFINITY ? 0 : ~(u64)0, nan, false)) return;
   row.scale.top = high;
   plan_row(waves, counts, row.scale);
@@ -1500,7 +1502,7 @@ template <typename T, bool SECOND> __global__ void __launch_bounds__(kThreads) r
     }
     find_slowly(a, r, row, waves, lists);
   } else {
-    if (tid == 0) waves.head.answered = 0, waves.head.top = high, state->listed = state->arrived = 0;
+    if (tid == 0) waves.head.planned = kPlanned, waves.head.top = high, state->listed = state->arrived = 0;
     if (tid <= kMostRuns) state->weight[tid] = 0;
     if (waves.head.plan.slow)
       for (int i = tid; i < kBins; i += kThreads) state->count[i] = state->most[i] = 0, state->least[i] = ~0u;
@@ -1516,7 +1518,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) gather_kernel(
   const int tid = threadIdx.x, slot = blockIdx.x / pieces, piece = blockIdx.x % pieces;
   const int64_t r = row0 + slot;
   State* const state = w.states + slot;
-  if (state->head.answered) return;
+  if (state->head.planned != kPlanned) return;
   if (tid < kHeadWords) reinterpret_cast<uint32_t*>(&waves.head)[tid] = reinterpret_cast<const uint32_t*>(&state->head)[tid];
   __syncthreads();
   const Row<T> row{static_cast<const T*>(a.logits) + r * a.stride, a.columns, a.log2_columns, {waves.head.top, waves.head.ask.factor}};
