@@ -52,6 +52,7 @@ constexpr int kGroups = 256;          // workgroups of a launch: one for each CU
 // Scores of a workgroup at least, where several have a row.  The second pass: one row of 131072 takes 32 us, with 8192 a microsecond more, with 16384 four.
 constexpr int kLeastPiece = 4096;
 constexpr int kMostRows = 1024;       // of a launch
+constexpr int64_t kMostFew = UINT32_MAX / kThreads;  // of one for short rows: a launch has fewer than 2^32 threads
 // The first pass hands 16 KB of counts on for each piece: four to eight pieces or one.  16 rows of 131072 take 37 us (in one piece 46; one row in eight
 // pieces 32, in one 41, in 16 or 64 a microsecond more), 32768 scores in two pieces 30.7 us (in one 28.4), 128 rows of 131072 in two 72 (69.5).
 constexpr int kLeastCounted = 1 << 14, kFewestCounts = 4, kMostCounts = 8;
@@ -1316,10 +1317,10 @@ __device__ __forceinline__ bool all_arrived(Waves& waves, uint32_t* counter, uin
 }
 
 // Rows that fit in the list: sorted whole.  16 rows of 2048 take 11 us, with steps 16.
-template <typename T> __global__ void __launch_bounds__(kThreads) few_kernel(Args a) {
+template <typename T> __global__ void __launch_bounds__(kThreads) few_kernel(Args a, int64_t row0) {
   __shared__ Waves waves;
   __shared__ Lists lds;
-  const int64_t r = blockIdx.x;
+  const int64_t r = row0 + blockIdx.x;
   const float temperature = parameter(a.temperature, r, 1.f);
   Row<T> row{static_cast<const T*>(a.logits) + r * a.stride, a.columns, a.log2_columns, {0.f, 0.0}};
   if (threadIdx.x < 64) waves.head.ask = ask_of(a, r, temperature);  // (all lanes write the same)
@@ -1561,7 +1562,8 @@ int64_t states_of(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(
 
 template <typename T> void launch(const Args& a, int64_t rows, void* workspace, hipStream_t stream) {
   if (a.columns <= kList) {
-    hipLaunchKernelGGL(few_kernel<T>, dim3((unsigned)rows), dim3(kThreads), 0, stream, a);
+    for (int64_t row0 = 0; row0 < rows; row0 += kMostFew)
+      hipLaunchKernelGGL(few_kernel<T>, dim3((unsigned)std::min(rows - row0, kMostFew)), dim3(kThreads), 0, stream, a, row0);
     return;
   }
   Workspace w{static_cast<Counter*>(workspace), reinterpret_cast<State*>(static_cast<char*>(workspace) + kCounterBytes), nullptr};
