@@ -131,7 +131,7 @@ struct Plan {
   uint32_t tokens;  // of all runs
   uint32_t all;     // of the row
   int weighed;      // it adds up weights
-  int behind;       // the place of top_p is behind what min_p keeps
+  int behind;       // the place of top_p is taken to be behind what min_p keeps
   int slow;         // kMany: too many tokens for the list; kSlow: too many above the steps, or no steps
 };
 constexpr int kMany = 1, kSlow = 2;
@@ -545,6 +545,8 @@ template <typename T> struct Row {
         else hi = mid;
       }
       is_sure &= lo < r.count || r.before + r.count >= kept;
+      // (top_p's place is behind them if the sum without the last of them is below it; without any of the run, with the last one)
+      if (plan.behind) is_sure &= !At::weight(ask.top_p * mass, false).reached(0, lo > 1 ? mass_at(lds, r, r.start + lo - 2) : r.mass_before);
       if (r.before + lo < kept) kept = r.before + lo, mass = lo ? mass_at(lds, r, r.start + lo - 1) : r.mass_before;
     }
     const At p = At::weight(ask.u * mass, true);
@@ -1192,7 +1194,10 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
         const int last = (int)lds.first - 1;
         const uint32_t n = last < 0 ? plan.run[near].before : counted(near, last), end = plan.run[near].before + plan.run[near].count;
         is_sure &= n < end || end >= kept;
-        if (n < kept) kept = n, mass = last < 0 ? (double)lds.weight[near] * 0x1p-40 : weighed(near, last);
+        const double upto_last = last < 0 ? (double)lds.weight[near] * 0x1p-40 : weighed(near, last);
+        // (as in Row::solve)
+        if (plan.behind) is_sure &= !At::weight(ask.top_p * mass, false).reached(0, last < 0 ? upto_last : upto_last - row.scale.weight(Key<T>::score(lds.least[last])));
+        if (n < kept) kept = n, mass = upto_last;
       }
       seek(place == 0 ? At::tokens(ask.top_k) : place == 1 ? At::weight(ask.top_p * mass, false) : At::weight(ask.u * mass, true));
       if (place == 0) kept = ask.top_k, mass = upto;
