@@ -532,6 +532,8 @@ template <typename T> struct Row {
       const uint32_t at = seek(lds, plan, p, r), n = r.before + at - r.start + 1;
       is_sure &= sure(lds, p, r, all);
       if (n < kept) kept = n, mass = mass_at(lds, r, at);
+      // (min_p was left out because its place is behind: the last one is near enough then)
+      if (plan.near < 0) is_sure &= scale.distance(score(lds.list[at])) <= ask.far;
     }
     if (plan.near >= 0) {
       r = plan.run[0];
@@ -1202,6 +1204,7 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
       seek(place == 0 ? At::tokens(ask.top_k) : place == 1 ? At::weight(ask.top_p * mass, false) : At::weight(ask.u * mass, true));
       if (place == 0) kept = ask.top_k, mass = upto;
       if (place == 1 && count < kept) kept = count, mass = upto;
+      if (place == 1 && plan.near < 0) is_sure &= row.scale.distance(Key<T>::score(lds.least[part])) <= ask.far;
     }
     if (tid == 0) waves.sure = is_sure, waves.count[0] = lds.least[part], waves.count[1] = nth, waves.count[2] = kept, waves.mass[0] = mass;
   }

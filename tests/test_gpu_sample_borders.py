@@ -60,3 +60,16 @@ def test_top_p_ends_before_min_p(columns, each, before, rows):
     near = int((total[1:] - total[:-1] >= min_p).sum()) + 1
     top_p = float(np.float32((total[near - before - 1] + total[near - before - 2]) / 2 / total[-1]))
     assert check(x, rows, top_p=top_p, min_p=min_p) == near - before
+
+
+@pytest.mark.parametrize("rows", [1, 8, 130])
+@pytest.mark.parametrize("top_k", [600, 900, 1000])
+def test_min_p_ends_before_top_p(top_k, rows):
+    """The other way round, with some empty steps between: by counts top_p's place is before min_p's, by their weights one token behind."""
+    x = row(131072, [(2, s + 0.94) for s in range(1, 150)] + [(2, s + 0.06) for s in range(156, 480)])
+    min_p = float(np.float32(math.exp(-152.5 * STEP)))
+    total = sums(x, top_k)
+    near = int((total[1:] - total[:-1] >= min_p).sum()) + 1
+    for part in (0.02, 0.1, 0.5):
+        top_p = float(np.float32((total[near - 1] + part * (total[near] - total[near - 1])) / total[-1]))
+        assert check(x, rows, top_k=top_k, top_p=top_p, min_p=min_p) == near
