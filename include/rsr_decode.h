@@ -95,8 +95,9 @@ int rsr_head_rotate(const rsr_rotary_t *rotary, const void *q, int64_t q_stride,
  * A score of minus infinity is no token's: it is never chosen and not counted.  A row without another score has token -1,
  * probability 0 and kept 0; a row with NaN has token -1, probability NaN and kept 0.  With scores of plus infinity only these
  * tokens have weight, all the same.
- * Weights and sums are held in 64 bits, off by some 2^-39 (2^-34 of each weight where thousands of different scores lie next to each other): a border of
- * a sum falls between the tokens between which it falls exactly unless it is that near to one.  A row's results depend on nothing but its own scores and
+ * Weights and sums are held in 64 bits: a weight is off by some 2^-39 of itself (2^-34 where thousands of different scores lie
+ * next to each other), a sum of weights by no more than that of itself, however many they are: a border of a sum falls between the
+ * tokens between which it falls exactly unless it is that near to one.  A row's results depend on nothing but its own scores and
  * parameters, and in their last bits on where in 16 bytes it begins; not on other rows, nor on the order in which workgroups come.
  * Errors: RSR_ERR_INVALID_ARGUMENT, RSR_ERR_HIP (launch failure).
  */

@@ -132,6 +132,7 @@ struct Plan {
   uint32_t all;     // of the row
   int weighed;      // it adds up weights
   int behind;       // the place of top_p is taken to be behind what min_p keeps
+  int shift;        // of the unit in which weights are added up
   int slow;         // kMany: too many tokens for the list; kSlow: too many above the steps, or no steps
 };
 constexpr int kMany = 1, kSlow = 2;
@@ -175,6 +176,7 @@ struct Counts {
   Mark mark[2 * kMostRuns];
   uint32_t before[2];
   uint32_t listed, all_count;
+  uint32_t first_steps;  // tokens of the first 128 steps
   float all_mass;
 };
 
@@ -292,31 +294,31 @@ struct Scale {
   __device__ __forceinline__ double distance(float x) const { return x == top ? 0.0 : ((double)top - (double)x) * factor; }
   // 2^f, f from -1/2 to 1/2, is the polynomial that has its values at nine Chebyshev nodes, off by 2^-39 of it.  A thousand octaves
   // down nothing is left of a weight.
-  static __device__ __forceinline__ void split(double distance, double& p, double& power) {
-    const double d = fmin(distance, 1000.0), n = rint(d), f = n - d;
-    p = 1.0 + f * (0.6931471805459335 + f * (0.2402265069581299 + f * (0.05550410941205934 + f * (0.009618129159402607 + f * (0.0013333450567999429 +
-        f * (0.00015403455852420792 + f * (1.5310079402541085e-05 + f * 1.3255224885567153e-06)))))));
-    power = __builtin_bit_cast(double, (u64)((uint32_t)(1023 - (int)n) << 20) << 32);
+  // `one` + 2^f - 1
+  static __device__ __forceinline__ double power(double f, double one) {
+    return one + f * (0.6931471805459335 + f * (0.2402265069581299 + f * (0.05550410941205934 + f * (0.009618129159402607 + f * (0.0013333450567999429 +
+           f * (0.00015403455852420792 + f * (1.5310079402541085e-05 + f * 1.3255224885567153e-06)))))));
   }
   __device__ __forceinline__ double weight(float x) const {
-    double p, power;
-    split(distance(x), p, power);
-    return p * power;
+    const double d = fmin(distance(x), 1000.0), n = rint(d);
+    return power(n - d, 1.0) * __builtin_bit_cast(double, (u64)((uint32_t)(1023 - (int)n) << 20) << 32);
   }
 };
 __device__ __forceinline__ int bin_of(double distance) { return (int)fmin(distance * kPerOctave, (double)(kBins - 1)); }
 
-// Sums of weights in units of 2^-40 of the highest's, in whole numbers, so that no order of additions matters: a weight is added to 2^12,
-// where 2^-40 is the last bit, and the bits of that are added up.
+// Sums of weights in whole numbers, so that no order of additions matters, in units of 2^-62 of the highest's shifted up by as much as
+// keeps the sum of all below 2^64.  What is cut off is less than a unit for each: at most 2^-40 of the sum for 2^22 scores, 2^-45 for 2^17.  (In units
+// that are the same for all rows, 2^-40, a tail of 2^17 equal scores was off by a thousand of them.)  2 + 2^f has the bits of 2^f / 2 behind its point.
 struct Weights {
   double top, factor;
-  static constexpr double kAbove = 0x1p12;
+  int shift;
   __device__ __forceinline__ u64 of(float x) const {
-    double p, power;
-    Scale::split((top - (double)x) * factor, p, power);
-    return __builtin_bit_cast(u64, fma(p, power, kAbove));
+    const double d = fmin((top - (double)x) * factor, 62.25 - shift), n = rint(d);  // (2^-62.25 is nothing)
+    return __builtin_bit_cast(u64, Scale::power(n - d, 3.0)) << 12 >> ((int)n + shift + 1);
   }
-  static __device__ __forceinline__ u64 none() { return __builtin_bit_cast(u64, kAbove); }
+  static __device__ __forceinline__ double sum(u64 units, int shift) { return (double)units * __builtin_bit_cast(double, (u64)(1023 - 62 + shift) << 52); }
+  // The shift for weights that together are less than `most`.
+  static __device__ __forceinline__ int shift_of(float most) { return max(0, __builtin_amdgcn_frexp_expf(most) - 2); }
 };
 
 // 2^34 times 1 - 2^-(f / 32) for f from 0 to 1, as a sum of powers of f ln 2 / 32 (the sixth adds less than 2^-42).  Of the last bin,
@@ -817,25 +819,26 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
   const Ask& ask = waves.head.ask;
   const Steps steps = waves.head.steps;
   const uint32_t peaks = lds.listed;
-  if (peaks > kPeaks || scale.top == INFINITY) {
+  const double wide = 2.0 * scale.factor / steps.per, above = ((double)scale.top - (double)steps.from) * scale.factor - 0.5 * wide;
+  // (steps wider than half an octave of scores next to zero tell nothing; of others, all of a step are equal then)
+  if (peaks > kPeaks || scale.top == INFINITY || (wide > 0.5 && fabsf(steps.from) < 1e-14f)) {
     if (tid == 0) waves.head.plan.slow = kSlow;
     __syncthreads();
     return;
   }
-  const Weights weights{scale.top, scale.factor};
+  const Weights weights{scale.top, scale.factor, Weights::shift_of(kPeaks)};
   u64 high = 0;  // (they lie in any order, so their sum is one of whole numbers)
 #pragma unroll
   for (int j = 0; j < 2; ++j)
-    if ((uint32_t)(tid + j * kThreads) < peaks) high += weights.of(lds.peaks[tid + j * kThreads]) - Weights::none();
+    if ((uint32_t)(tid + j * kThreads) < peaks) high += weights.of(lds.peaks[tid + j * kThreads]);
   high = sum_of_lanes(high);
   if (lane == 63) waves.best[wave] = high;
   if (tid == 0) lds.steps[0] = peaks;
   if (tid < 2 * kMostRuns) lds.mark[tid].bin = kSteps;
   __syncthreads();
-  const float peak = (float)((double)of_lane(sum_of_16(waves.best[lane & 15]), 15) * 0x1p-40);
+  const float peak = (float)Weights::sum(of_lane(sum_of_16(waves.best[lane & 15]), 15), weights.shift);
 
   // the sums of each thread's steps
-  const double wide = 2.0 * scale.factor / steps.per, above = ((double)scale.top - (double)steps.from) * scale.factor - 0.5 * wide;
   const float octaves = (float)wide;
   auto weight_of = [&](uint32_t n, int step) { return step ? (float)n * __builtin_amdgcn_exp2f(-fmaxf((float)(above + step * wide), 0.f)) : peak; };
   const float first = (float)(above + tid * kEach * wide);
@@ -856,6 +859,7 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
   if (lane == 63) waves.high[wave] = squares;
   s.scan(waves, 0, 0.f);
   if (tid == kThreads - 1) lds.all_count = s.c[0], lds.all_mass = s.m[0];
+  if (tid == 128 / kEach) lds.first_steps = s.c_before;
   // The step of a place: the wavefront in which a thread's sums reach it adds up the steps of that thread, a lane each.
   auto mark = [&](int place, const About& p) {
     const u64 here = __ballot(s.c[0] > s.c_before && p.reached(s.c[0], s.m[0]) && (!s.c_before || !p.reached(s.c_before, s.m_before)));
@@ -928,6 +932,8 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
   if (wave == 0) {
     Plan plan;
     plan.near = near, plan.all = all, plan.behind = behind;
+    // (A step's weights are less than 2^(1/4) of what is in its middle.  Of wider ones, those behind the first 128 have no weight.)
+    plan.shift = Weights::shift_of(octaves <= 0.5f ? fminf(1.25f * total, (float)all) : (float)lds.first_steps);
     if (prefix) {
       lo[0] = 0, hi[0] = last.bin, before[0] = 0, upto[0] = last.count;
 #pragma unroll
@@ -988,10 +994,9 @@ template <int RUNS, bool EQUAL, typename T> __device__ __forceinline__ void gath
   if constexpr (EQUAL)
     for (int i = threadIdx.x; i < kBins; i += kThreads) lds.count[i] = lds.most[i] = 0, lds.least[i] = ~0u;
   __syncthreads();
-  const Weights weights{row.scale.top, row.scale.factor};
+  const Weights weights{row.scale.top, row.scale.factor, plan.shift};
   float lo[kRuns], hi[kRuns], from[kRuns], per[kRuns];
   u64 before[kRuns], all = 0;
-  uint32_t pieces = 0;
 #pragma unroll
   for (int i = 0; i < kRuns; ++i) {
     const bool there = i < plan.n;
@@ -1015,10 +1020,9 @@ template <int RUNS, bool EQUAL, typename T> __device__ __forceinline__ void gath
         const u64 w = weights.of(x[j]);
         all += w;
 #pragma unroll
-        for (int i = 0; i < kRuns; ++i) before[i] += down < lo[i] ? w : Weights::none();
+        for (int i = 0; i < kRuns; ++i) before[i] += down < lo[i] ? w : 0;
       }
     }
-    ++pieces;
     if (some)
 #pragma unroll
       for (int j = 0; j < kWide; ++j)
@@ -1038,9 +1042,8 @@ template <int RUNS, bool EQUAL, typename T> __device__ __forceinline__ void gath
         }
   });
   if constexpr (RUNS) {
-    const u64 none = (u64)pieces * kWide * Weights::none();
     auto give = [&](u64 sum, u64* to) {
-      sum = sum_of_lanes(sum - none);
+      sum = sum_of_lanes(sum);
       if ((threadIdx.x & 63) == 63) atomicAdd(to, sum);
     };
 #pragma unroll
@@ -1107,7 +1110,7 @@ template <bool SPANNED, typename T> __device__ __forceinline__ bool find(const A
   const int tid = threadIdx.x;
   if (!SPANNED && tid < kMostRuns) {
     Run run = plan.run[tid];
-    run.mass_before = plan.weighed ? (double)lds.weight[tid] * 0x1p-40 : 0.0;
+    run.mass_before = plan.weighed ? Weights::sum(lds.weight[tid], plan.shift) : 0.0;
     if (tid < plan.n) {
       const float first = run.b0 ? steps.score(run.b0 - 1) : row.scale.top, last = steps.score(min(run.b1, kSteps - 2));
       run.span(row.code(first, 0), row.code(last, row.columns - 1));
@@ -1118,7 +1121,10 @@ template <bool SPANNED, typename T> __device__ __forceinline__ bool find(const A
   __syncthreads();
   row.sort(waves, lds, plan, steps);
   if (tid < 64) {
-    const Found f = row.solve(lds, waves.head.ask, plan, plan.all, plan.weighed ? (double)lds.weight[kMostRuns] * 0x1p-40 : lds.upto[plan.tokens - 1]);
+    // (where the last run ends the row, its sum of all is that of the places in it)
+    const Run& last = plan.run[plan.n - 1];
+    const bool ends = !plan.weighed || last.before + last.count == plan.all;
+    const Found f = row.solve(lds, waves.head.ask, plan, plan.all, ends ? row.mass_at(lds, last, plan.tokens - 1) : Weights::sum(lds.weight[kMostRuns], plan.shift));
     if (f.sure) answer(a, r, row.column(f.code), (float)f.share, f.kept);
     if (tid == 0) waves.sure = f.sure;
   }
@@ -1159,18 +1165,20 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
 
   if (tid < 64) {
     uint32_t kept = plan.all, before, count, nth;
-    double mass = (double)lds.weight[kMostRuns] * 0x1p-40, mass_before, upto;
+    double mass_before, upto;
     int part;
     bool is_sure = true;
     // a run's sums up to and with a part
     auto counted = [&](int i, int at) { return plan.run[i].before + lds.part_count[at] - (i ? lds.part_count[i * kEach - 1] : 0); };
-    auto weighed = [&](int i, int at) { return (double)lds.weight[i] * 0x1p-40 + (lds.upto[at] - (i ? lds.upto[i * kEach - 1] : 0.0)); };
+    auto weighed = [&](int i, int at) { return Weights::sum(lds.weight[i], plan.shift) + (lds.upto[at] - (i ? lds.upto[i * kEach - 1] : 0.0)); };
+    const int end = plan.n - 1;  // (as in find)
+    double mass = counted(end, end * kEach + kEach - 1) == plan.all ? weighed(end, end * kEach + kEach - 1) : Weights::sum(lds.weight[kMostRuns], plan.shift);
     auto seek = [&](const At& p) {
       int i = 0;
       while (i + 1 < plan.n && !p.reached(counted(i, i * kEach + kEach - 1), weighed(i, i * kEach + kEach - 1))) ++i;
       int lo = i * kEach, hi = lo + kEach - 1;
       const bool behind = p.reached(counted(i, hi), weighed(i, hi));
-      is_sure &= (!plan.run[i].before || !p.reached(plan.run[i].before, (double)lds.weight[i] * 0x1p-40)) && (behind || counted(i, hi) == plan.all);
+      is_sure &= (!plan.run[i].before || !p.reached(plan.run[i].before, Weights::sum(lds.weight[i], plan.shift))) && (behind || counted(i, hi) == plan.all);
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (p.reached(counted(i, mid), weighed(i, mid))) hi = mid;
@@ -1196,7 +1204,7 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
         const int last = (int)lds.first - 1;
         const uint32_t n = last < 0 ? plan.run[near].before : counted(near, last), end = plan.run[near].before + plan.run[near].count;
         is_sure &= n < end || end >= kept;
-        const double upto_last = last < 0 ? (double)lds.weight[near] * 0x1p-40 : weighed(near, last);
+        const double upto_last = last < 0 ? Weights::sum(lds.weight[near], plan.shift) : weighed(near, last);
         // (as in Row::solve)
         if (plan.behind) is_sure &= !At::weight(ask.top_p * mass, false).reached(0, last < 0 ? upto_last : upto_last - row.scale.weight(Key<T>::score(lds.least[last])));
         if (n < kept) kept = n, mass = upto_last;
