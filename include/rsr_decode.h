@@ -56,7 +56,7 @@ typedef struct rsr_rotary_t {
  *   q, k         DEVICE, row t at q + t * q_stride elements: [heads][head_dim], k: [kv_heads][head_dim]
  *   dtype        of q and k: RSR_F32, RSR_F16 or RSR_BF16
  *   position     DEVICE [tokens] int32 (any; negative ones rotate the other way)
- *   tokens       >= 0
+ *   tokens       0 .. 2^31 - 1
  *   heads, kv_heads   0 .. 65535, not both 0; without heads q and q_out (k and k_out) mean nothing
  *   q_out, k_out DEVICE, rows as those of q and k, with strides of their own; q_out may be q, and k_out k, with the same stride and
  *                type; otherwise no output may overlap an input or the other

@@ -31,6 +31,7 @@ int launched(const char* what) {
 // instead of 8.5), and the norm's sum is one of 32 bits by moves between lanes (in 64 bits, at half the rate: 77 us).  Loads and stores past the caches were as
 // fast, and the attention that reads the results would not find them there.
 constexpr int kRotateThreads = 256;
+constexpr int64_t kRotateTokens = UINT32_MAX / kRotateThreads * (kRotateThreads / 64);  // of a launch, which has fewer than 2^32 threads
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 
@@ -290,7 +291,7 @@ int rsr_head_rotate(const rsr_rotary_t* rotary, const void* q, int64_t q_stride,
   else if (rotary->norm && !(rotary->eps >= 0.f && std::isfinite(rotary->eps))) fault = "eps must be finite and not negative";
   else if (!is_dtype(dtype) || !is_dtype(out_dtype)) fault = "dtype and out_dtype must be RSR_F32, RSR_F16 or RSR_BF16";
   else if (heads < 0 || heads > 65535 || kv_heads < 0 || kv_heads > 65535 || heads + kv_heads == 0) fault = "heads and kv_heads must be in 0..65535, not both 0";
-  else if (tokens < 0) fault = "tokens must not be negative";
+  else if (tokens < 0 || tokens > INT32_MAX) fault = "tokens must be in 0..2^31-1";
   if (fault) return set_error(RSR_ERR_INVALID_ARGUMENT, fault);
   if (tokens == 0) return RSR_OK;
   const int64_t width = (int64_t)heads * rotary->head_dim, kv_width = (int64_t)kv_heads * rotary->head_dim;
@@ -311,11 +312,17 @@ int rsr_head_rotate(const rsr_rotary_t* rotary, const void* q, int64_t q_stride,
   const int each = 64 >> a.log2_lanes;
   const int64_t most = (heads + kv_heads + each - 1) / each;
   a.share = (int32_t)std::min(most, std::max<int64_t>(1, 4096 / tokens));
-  const int64_t groups = (tokens * a.share + kRotateThreads / 64 - 1) / (kRotateThreads / 64);
-  if (groups > UINT32_MAX / kRotateThreads) return set_error(RSR_ERR_INVALID_ARGUMENT, "tokens is too large");
   auto kern = dtype == RSR_F32 ? rotate_to<float>(out_dtype) : dtype == RSR_F16 ? rotate_to<_Float16>(out_dtype) : rotate_to<__bf16>(out_dtype);
-  hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kRotateThreads), 0, static_cast<hipStream_t>(stream), a);
-  return launched("rsr_head_rotate");
+  auto behind = [](const void* p, int64_t stride, int type) { return static_cast<const char*>(p) + kRotateTokens * stride * rsr_internal::size_of(type); };
+  for (;;) {
+    a.tokens = std::min(tokens, kRotateTokens);
+    const int64_t groups = (a.tokens * a.share + kRotateThreads / 64 - 1) / (kRotateThreads / 64);
+    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kRotateThreads), 0, static_cast<hipStream_t>(stream), a);
+    if ((tokens -= a.tokens) == 0) return launched("rsr_head_rotate");
+    if (heads) a.q = behind(a.q, q_stride, dtype), a.q_out = const_cast<char*>(behind(a.q_out, q_out_stride, out_dtype));
+    if (kv_heads) a.k = behind(a.k, k_stride, dtype), a.k_out = const_cast<char*>(behind(a.k_out, k_out_stride, out_dtype));
+    if (position) a.position += kRotateTokens;
+  }
 }
 
 int rsr_tree_keep(const int32_t* drafted, const int32_t* chosen, const int32_t* parent, const int32_t* start, int requests, int tokens, int32_t* rows,
