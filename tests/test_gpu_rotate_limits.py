@@ -5,6 +5,7 @@ import torch
 
 import paper_2411_06360_amd as R
 from oracle import decode as oracle
+from tests.test_gpu_rotate import check
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +35,9 @@ def test_more_tokens_than_a_launch_has(dtype, pairs):
             n = min(2**25, tokens - at)
             R.rsr_head_rotate(how, source[at:at + n], None, position[at:at + n], part[:n], None, stream)
             assert torch.equal(rows[at:at + n], part[:n]), at
+
+
+@pytest.mark.parametrize("act", ["f16", "bf16"])
+@pytest.mark.parametrize("tokens,norm,pairs", [(4099, True, False), (2500, False, True)])
+def test_prompts_of_sixteen_bits(act, tokens, norm, pairs):
+    check(tokens, 8, 2, 128, norm=norm, pairs=pairs, act=act, out=act, seed=tokens, far=131072)
