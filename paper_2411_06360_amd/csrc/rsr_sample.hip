@@ -132,6 +132,7 @@ struct Plan {
   uint32_t all;     // of the row
   int weighed;      // it adds up weights
   int behind;       // the place of top_p is taken to be behind what min_p keeps
+  int ends;         // the last run has the row's last token
   int shift;        // of the unit in which weights are added up
   int slow;         // kMany: too many tokens for the list; kSlow: too many above the steps, or no steps
 };
@@ -535,7 +536,7 @@ template <typename T> struct Row {
       is_sure &= sure(lds, p, r, all);
       if (n < kept) kept = n, mass = mass_at(lds, r, at);
       // (min_p was left out because its place is behind: the last one is near enough then)
-      if (plan.near < 0) is_sure &= scale.distance(score(lds.list[at])) <= ask.far;
+      if (plan.near < 0 && ask.far < INFINITY) is_sure &= scale.distance(score(lds.list[at])) <= ask.far;
     }
     if (plan.near >= 0) {
       r = plan.run[0];
@@ -969,12 +970,12 @@ __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale&
           }
         }
     }
-    plan.n = 0, plan.tokens = 0;
+    plan.n = 0, plan.tokens = 0, plan.ends = 0;
 #pragma unroll
     for (int i = 0; i < kMostRuns; ++i) {
       const bool there = lo[i] < kSteps;
       plan.run[i] = {lo[i], hi[i], plan.tokens, there ? upto[i] - before[i] : 0, before[i], 0, 0.f, 0.f, 0, 0.0};
-      plan.tokens += plan.run[i].count, plan.n += there;
+      plan.tokens += plan.run[i].count, plan.n += there, plan.ends |= there && upto[i] == all;
     }
     plan.slow = plan.tokens > kList ? kMany : 0;
     if (lane == 0) waves.head.plan = plan;
@@ -1122,9 +1123,9 @@ template <bool SPANNED, typename T> __device__ __forceinline__ bool find(const A
   row.sort(waves, lds, plan, steps);
   if (tid < 64) {
     // (where the last run ends the row, its sum of all is that of the places in it)
-    const Run& last = plan.run[plan.n - 1];
-    const bool ends = !plan.weighed || last.before + last.count == plan.all;
-    const Found f = row.solve(lds, waves.head.ask, plan, plan.all, ends ? row.mass_at(lds, last, plan.tokens - 1) : Weights::sum(lds.weight[kMostRuns], plan.shift));
+    double mass = lds.upto[plan.tokens - 1];
+    if (plan.weighed) mass = plan.ends ? row.mass_at(lds, plan.run[plan.n - 1], plan.tokens - 1) : Weights::sum(lds.weight[kMostRuns], plan.shift);
+    const Found f = row.solve(lds, waves.head.ask, plan, plan.all, mass);
     if (f.sure) answer(a, r, row.column(f.code), (float)f.share, f.kept);
     if (tid == 0) waves.sure = f.sure;
   }
@@ -1172,7 +1173,7 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
     auto counted = [&](int i, int at) { return plan.run[i].before + lds.part_count[at] - (i ? lds.part_count[i * kEach - 1] : 0); };
     auto weighed = [&](int i, int at) { return Weights::sum(lds.weight[i], plan.shift) + (lds.upto[at] - (i ? lds.upto[i * kEach - 1] : 0.0)); };
     const int end = plan.n - 1;  // (as in find)
-    double mass = counted(end, end * kEach + kEach - 1) == plan.all ? weighed(end, end * kEach + kEach - 1) : Weights::sum(lds.weight[kMostRuns], plan.shift);
+    double mass = plan.ends ? weighed(end, end * kEach + kEach - 1) : Weights::sum(lds.weight[kMostRuns], plan.shift);
     auto seek = [&](const At& p) {
       int i = 0;
       while (i + 1 < plan.n && !p.reached(counted(i, i * kEach + kEach - 1), weighed(i, i * kEach + kEach - 1))) ++i;
@@ -1212,7 +1213,7 @@ template <typename T> __device__ __forceinline__ bool find_equal(const Args& a, 
       seek(place == 0 ? At::tokens(ask.top_k) : place == 1 ? At::weight(ask.top_p * mass, false) : At::weight(ask.u * mass, true));
       if (place == 0) kept = ask.top_k, mass = upto;
       if (place == 1 && count < kept) kept = count, mass = upto;
-      if (place == 1 && plan.near < 0) is_sure &= row.scale.distance(Key<T>::score(lds.least[part])) <= ask.far;
+      if (place == 1 && plan.near < 0 && ask.far < INFINITY) is_sure &= row.scale.distance(Key<T>::score(lds.least[part])) <= ask.far;
     }
     if (tid == 0) waves.sure = is_sure, waves.count[0] = lds.least[part], waves.count[1] = nth, waves.count[2] = kept, waves.mass[0] = mass;
   }
