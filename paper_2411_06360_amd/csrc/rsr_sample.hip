@@ -15,13 +15,13 @@
 // Where there are as many rows as CUs a row is one workgroup's, of sixteen wavefronts; few long rows are shared by several, in either pass, and
 // the last one that comes goes on.  What all sixteen compute alike costs four times what one of them takes, so one alone plans and finds, and the
 // others wait.  Every function is part of its kernel: a single call anywhere gives every launch a stack, which takes 1 to 13 us more (256 rows of 131072 with
-// top_k 50 52 us, and 46 without it; with min_p 0.1 72 and 60).  There is one copy of each pass for that, and no more scores on their way than a pass needs: a kernel has to
+// top_k 50 52 us, and 46 without it; with min_p 0.1 72 and 60); what is left are two to four registers that 16-bit scores spill, 12 to 20 bytes a lane.  There is one copy of each pass for that, and no more scores on their way than a pass needs: a kernel has to
 // stay below what a short branch reaches (42 and 52 us then).
 //
 // What bounds it: with few rows the steps behind each other.  16 rows of 131072 with top_p 0.9, 37 us from call to call: a look 2.3, counts of 16384 scores 4.2,
 // handing them on and adding them up 7.3, the plan 4.8, until the second launch is at work 3.0, weights of 8192 scores 4.5, handing on 3.4, sorting 2.4, finding 1.4.
-// With many rows the second pass, some 14 operations in 64 bits for a score: 256 rows, 88 us, of which 20 are for counting and 40 for weighing, where
-// reading all scores twice from memory takes 53.  Other figures: one row of 131072 32 us; with top_k 50 one row takes 20, 16 rows 23, 256 rows 42; the highest
+// With many rows the second pass, some 14 operations in 64 bits for a score: 256 rows, 88 us, of which 20 are for counting and 40 for weighing (at a
+// copy's rate two reads of all scores would be 53; nothing was counted that says where the second one comes from).  Other figures: one row of 131072 32 us; with top_k 50 one row takes 20, 16 rows 23, 256 rows 42; the highest
 // score of each of 256 rows 29; 256 rows that all ask for something else 82 to 84.
 #include <hip/hip_runtime.h>
 
@@ -293,9 +293,8 @@ struct Scale {
   float top;
   double factor;
   __device__ __forceinline__ double distance(float x) const { return x == top ? 0.0 : ((double)top - (double)x) * factor; }
-  // 2^f, f from -1/2 to 1/2, is the polynomial that has its values at nine Chebyshev nodes, off by 2^-39 of it.  A thousand octaves
-  // down nothing is left of a weight.
-  // `one` + 2^f - 1
+  // `one` + 2^f - 1, f from -1/2 to 1/2: 2^f is the polynomial that has its values at nine Chebyshev nodes, off by 2^-39 of it.  (A thousand
+  // octaves down nothing is left of a weight.)
   static __device__ __forceinline__ double power(double f, double one) {
     return one + f * (0.6931471805459335 + f * (0.2402265069581299 + f * (0.05550410941205934 + f * (0.009618129159402607 + f * (0.0013333450567999429 +
            f * (0.00015403455852420792 + f * (1.5310079402541085e-05 + f * 1.3255224885567153e-06)))))));
@@ -810,7 +809,8 @@ template <typename T> __device__ __forceinline__ float count_steps(Waves& waves,
 // In which steps the places may be, and so which tokens are gathered.  The scores above the steps are weighed one by one, a step as its
 // count times the weight in its middle.  Where a step's scores lie in it is not known: it is off by its weight times its width (in
 // ln 2 octaves) over the root of 12, as if they all lay at one place of which any is as likely, and the sums of all are off by the root of the
-// squares of that; four and a half times as much is allowed for.  (Whether that was enough is seen in the end.)
+// squares of that; four and a half times as much is allowed for.  That is no bound: scores near the same end of all steps are off by more.  Whether it was
+// enough is seen in the end, for a place that is looked up as for one that is left out because another comes before it.
 __device__ __forceinline__ void plan_row(Waves& waves, Counts& lds, const Scale& scale) {
   constexpr int kEach = kSteps / kThreads;
   constexpr float kRounded = 2e-6f;  // of a sum: what some twenty roundings come to, and more
